@@ -296,6 +296,73 @@ int caramel_allreduce(caramel_plan* plan, void* stream);
 #define CARAMEL_STATIC_TABLE_BYTES (4u << 20)
 int caramel_allreduce_static(caramel_plan* plan, void* const* grads, void* stream);
 
+/* ---- filling a plan's gradient tensors --------------------------------------------------- */
+
+/* What the backward pass of a data-parallel program does right before the aggregation: it turns what
+ * the forward pass has kept into the gradients of every worker, in the memory the plan is bound to.
+ * One call handles the same layer at all W workers of a plan (its world); the arrays of pointers are
+ * host arrays of W DEVICE pointers, one per worker, and `tokens` is a host array of W counts, which may
+ * differ and may be 0 (such a worker's pointers are not looked at).  The plan may be used for the aggregation,
+ * in any order on one stream, between such calls.
+ *
+ * All calls are asynchronous on `stream`, allocate nothing, upload nothing and issue only kernel
+ * launches, so they can be captured.  Rows are `pitch` elements apart and may start on any element.  Buffers
+ * that a call writes must not overlap any other buffer of the call (EINVAL).  Sums are fp32 in an order that
+ * depends on the sizes alone, so results are reproducible bit for bit; each result is rounded once.
+ * Gradients are written; with `accumulate` they are added to what the tensor holds (micro-batches, tied
+ * weights), in one rounding.  The two gradient calls need a workspace: its size depends on the sizes given, its contents
+ * need not be kept from call to call, and calls that may run at the same time need one each.
+ * EINVAL: NULL or misaligned pointers (to the element, unless stated), more than 2^25 tokens, 2^20 columns, a
+ * pitch below the columns or above 2^23, 2^38 values at a worker, a workspace that is too small.  ESTATE: the plan is
+ * bound on another device than the current one; for the gradients also: not bound.  Pointers and stream must belong to
+ * the current device. */
+
+/* out[w][i, :] = scale * table[w][ids[w][i], :], rounded to the plan's dtype, which is that of the table.
+ *   table  vocab x width, rows without gaps; the workers' tables may be one and the same
+ *   ids    id_bytes (4 or 8) each, signed; an id below 0 or from vocab on is padding: its row is zeros */
+int caramel_embedding_lookup(caramel_plan* plan, const void* const* table, uint64_t vocab, uint64_t width, float scale,
+                             const void* const* ids, uint32_t id_bytes, const uint64_t* tokens, void* const* out,
+                             uint64_t out_pitch, void* stream);
+
+/* Its gradient: tensor `tensor` of the plan, as a matrix of `width` columns, becomes
+ *   grads[w][tensor][v, :] = scale * (sum of dy[w][i, :] over the i with ids[w][i] == v, in ascending order)
+ * Rows that no token names are zeros (with `accumulate`: left as they are); padding adds to no row, whatever its dy
+ * holds.  dy_dtype may differ from the plan's dtype.  The tokens are sorted by id; within a row the fp32 sum is cut
+ * into pieces at multiples of a fixed length of the sorted list. */
+int caramel_embedding_workspace(const caramel_plan* plan, uint32_t tensor, uint64_t width, const uint64_t* tokens,
+                                uint64_t* bytes);
+int caramel_embedding_gradient(caramel_plan* plan, uint32_t tensor, uint64_t width, float scale, const void* const* ids,
+                               uint32_t id_bytes, const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype,
+                               uint64_t dy_pitch, int accumulate, void* ws, uint64_t ws_bytes, void* stream);
+
+/* Activations kept in 8 bits from the forward to the backward pass.  A block is 32 consecutive tokens of one feature.
+ * With a its largest magnitude and e the smallest exponent >= -126 for which a <= 127 * 2^e, a value x is kept as
+ * q = round(x / 2^e), ties to even, and read back as q * 2^e: off by at most 2^(e-1), and exact in bf16 and fp32.  (e is at
+ * most 121; the few numbers above 127 * 2^121 = 3.376e38 are kept as that.)  A block
+ * that holds an infinity or a NaN reads back as NaN throughout.
+ * A checkpoint of `tokens` x `features` is caramel_checkpoint_bytes() bytes on a 16-byte boundary: the codes
+ * q as int8 [block][feature][32 tokens], those behind the last token 0, then e + 127 as bytes [block][feature], 255 for a
+ * block of NaN.
+ * store: x[w] (dtype, rows `pitch` elements apart) -> checkpoint[w];  load: the other way round.  The plan gives the number of
+ * workers only. */
+int caramel_checkpoint_bytes(uint64_t tokens, uint64_t features, uint64_t* bytes);
+int caramel_checkpoint_store(caramel_plan* plan, const uint64_t* tokens, uint64_t features, const void* const* x,
+                             uint32_t dtype, uint64_t pitch, void* const* checkpoint, void* stream);
+int caramel_checkpoint_load(caramel_plan* plan, const uint64_t* tokens, uint64_t features, const void* const* checkpoint,
+                            void* const* x, uint32_t dtype, uint64_t pitch, void* stream);
+
+/* Gradients of a dense layer y = x W + b from the checkpoint of its input x and the gradient dy of its output:
+ *   grads[w][weight] = x^T dy      features x outputs, where outputs = elements of the tensor / features
+ *   grads[w][bias]   = sum of the rows of dy      (bias == CARAMEL_NO_TENSOR: not computed)
+ * dy_dtype may differ from the plan's dtype.  The products are exact in both types (an fp32 dy goes through the matrix cores
+ * as the sum of three bf16 numbers). */
+#define CARAMEL_NO_TENSOR 0xFFFFFFFFu
+int caramel_weight_gradient_workspace(const caramel_plan* plan, uint32_t weight, uint64_t features, const uint64_t* tokens,
+                                      uint64_t* bytes);
+int caramel_weight_gradient(caramel_plan* plan, uint32_t weight, uint32_t bias, uint64_t features,
+                            const void* const* checkpoint, const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype,
+                            uint64_t dy_pitch, int accumulate, void* ws, uint64_t ws_bytes, void* stream);
+
 /* ---- launch tuning and timing (do not change results) ------------------------------------ */
 
 /* How the work is cut up for the GPU.  A "run" is a maximal piece of one tensor (or of the fused

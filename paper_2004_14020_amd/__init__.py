@@ -8,7 +8,7 @@ from .binding import (BIN_BACKWARD, BIN_FORWARD, BATCH_DIRECT, BATCH_STAGED, BF1
                       KIND_BATCH, KIND_CHUNK, LAUNCH_AUTO, LAUNCH_PER_STREAM, LAUNCH_PER_UNIT, OPT_BATCH_PATH,
                       PATTERN_HALVING_DOUBLING, PATTERN_RING, PATTERN_SHUFFLE, OPT_BLOCK, OPT_LAUNCH_MIN_BYTES, OPT_LAUNCH_MODE, OPT_PIPELINE_MIN_BYTES, OPT_SMALL_TILE_VECS, OPT_SMALL_BLOCK, OPT_LONG_RUN_BYTES, OPT_STREAM_MAJOR, OPT_LONG_LAUNCH_MIN_BYTES, OPT_ALIGN_TILES, OPT_MERGE_SMALL_BYTES, OPT_TAIL_TILES, OPT_SPLIT_TILES, OPT_MAX_GRID, OPT_NONTEMPORAL, OPT_TILE_VECS, OPT_UNROLL,
                       SPLIT_ADAPTIVE, SPLIT_FIXED, SPLIT_NONE, STATIC_TABLE_BYTES, CaramelError, Config, Entry, Plan, ScheduleSummary, Slot,
-                      Unit, lib, net_model_fit, schedule_transfers, stream_probe, threshold_estimate,
+                      NO_TENSOR, Unit, checkpoint_bytes, lib, net_model_fit, schedule_transfers, stream_probe, threshold_estimate,
                       PROBE_COPY, PROBE_READ, PROBE_UPDATE, PROBE_WRITE)
 
 
@@ -99,6 +99,38 @@ def caramel_allreduce_static(plan: Plan, grad_ptrs, stream: int = 0) -> None:
 
 def caramel_allreduce_loop(plan: Plan, n_calls: int, stream: int = 0):
     return plan.allreduce_loop(n_calls, stream)
+
+
+def caramel_embedding_lookup(plan: Plan, table, vocab, width, ids, tokens, out, **kw) -> None:
+    plan.embedding_lookup(table, vocab, width, ids, tokens, out, **kw)
+
+
+def caramel_embedding_workspace(plan: Plan, tensor, width, tokens) -> int:
+    return plan.embedding_workspace(tensor, width, tokens)
+
+
+def caramel_embedding_gradient(plan: Plan, tensor, width, ids, tokens, dy, ws, ws_bytes, **kw) -> None:
+    plan.embedding_gradient(tensor, width, ids, tokens, dy, ws, ws_bytes, **kw)
+
+
+def caramel_checkpoint_bytes(tokens, features) -> int:
+    return checkpoint_bytes(tokens, features)
+
+
+def caramel_checkpoint_store(plan: Plan, x, tokens, features, checkpoint, **kw) -> None:
+    plan.checkpoint_store(x, tokens, features, checkpoint, **kw)
+
+
+def caramel_checkpoint_load(plan: Plan, checkpoint, tokens, features, x, **kw) -> None:
+    plan.checkpoint_load(checkpoint, tokens, features, x, **kw)
+
+
+def caramel_weight_gradient_workspace(plan: Plan, weight, features, tokens) -> int:
+    return plan.weight_gradient_workspace(weight, features, tokens)
+
+
+def caramel_weight_gradient(plan: Plan, weight, bias, checkpoint, tokens, features, dy, ws, ws_bytes, **kw) -> None:
+    plan.weight_gradient(weight, bias, checkpoint, tokens, features, dy, ws, ws_bytes, **kw)
 
 
 def caramel_profile(plan: Plan, level: int) -> None:

@@ -25,6 +25,7 @@ PATTERN_RING, PATTERN_HALVING_DOUBLING, PATTERN_SHUFFLE = 0, 1, 2
 STATIC_TABLE_BYTES = 4 << 20
 LAUNCH_PER_UNIT, LAUNCH_PER_STREAM, LAUNCH_AUTO = 0, 1, 2
 BATCH_STAGED, BATCH_DIRECT = 0, 1
+NO_TENSOR = 0xFFFFFFFF
 K_PACK, K_REDUCE, K_UNPACK, K_SEQUENCE, K_REDUCE_SMALL, K_COUNT = 0, 1, 2, 3, 4, 5
 
 EXPORTS = (
@@ -34,6 +35,8 @@ EXPORTS = (
     "caramel_pack", "caramel_ring_reduce", "caramel_unpack", "caramel_allreduce", "caramel_allreduce_static",
     "caramel_plan_set_option", "caramel_plan_slices", "caramel_profile", "caramel_profile_read", "caramel_last_error",
     "caramel_version", "caramel_stream_probe", "caramel_allreduce_loop",
+    "caramel_embedding_lookup", "caramel_embedding_workspace", "caramel_embedding_gradient", "caramel_checkpoint_bytes",
+    "caramel_checkpoint_store", "caramel_checkpoint_load", "caramel_weight_gradient_workspace", "caramel_weight_gradient",
 )
 
 
@@ -122,6 +125,15 @@ def lib() -> C.CDLL:
     L.caramel_version.argtypes = []
     L.caramel_allreduce_loop.argtypes = [P, P, C.c_uint32, C.POINTER(C.c_double), C.POINTER(C.c_double)]
     L.caramel_stream_probe.argtypes = [C.c_uint32, C.POINTER(P), C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, P]
+    U32, U64, PU64, PP = C.c_uint32, C.c_uint64, C.POINTER(C.c_uint64), C.POINTER(P)
+    L.caramel_embedding_lookup.argtypes = [P, PP, U64, U64, C.c_float, PP, U32, PU64, PP, U64, P]
+    L.caramel_embedding_workspace.argtypes = [P, U32, U64, PU64, PU64]
+    L.caramel_embedding_gradient.argtypes = [P, U32, U64, C.c_float, PP, U32, PU64, PP, U32, U64, C.c_int, P, U64, P]
+    L.caramel_checkpoint_bytes.argtypes = [U64, U64, PU64]
+    L.caramel_checkpoint_store.argtypes = [P, PU64, U64, PP, U32, U64, PP, P]
+    L.caramel_checkpoint_load.argtypes = [P, PU64, U64, PP, PP, U32, U64, P]
+    L.caramel_weight_gradient_workspace.argtypes = [P, U32, U64, PU64, PU64]
+    L.caramel_weight_gradient.argtypes = [P, U32, U32, U64, PP, PU64, PP, U32, U64, C.c_int, P, U64, P]
     _lib = L
     return L
 
@@ -142,6 +154,7 @@ class Plan:
         self.cfg = Config(world, dtype, batch_threshold_bytes, split_mode, max_depth, split_bytes,
                           align_bytes, num_streams, pattern, 0)
         self.n_tensors = len(elems)
+        self.elems = [int(e) for e in elems]
         arr = (C.c_uint64 * max(1, len(elems)))(*[int(e) for e in elems])
         if ready_time is None:
             _check(lib().caramel_plan_create(C.byref(self.cfg), arr, len(elems), C.byref(self._h)))
@@ -261,6 +274,74 @@ class Plan:
         _check(lib().caramel_allreduce_loop(self._h, C.c_void_p(stream), n_calls, C.byref(host), C.byref(dev)))
         return host.value, dev.value
 
+    # -- filling the gradient tensors: one device address and one token count per worker
+    def _per_worker(self, kind, values, name):
+        if len(values) != self.cfg.world:
+            raise ValueError(f"{name} must have one entry per worker")
+        return (kind * self.cfg.world)(*values)
+
+    def _outputs(self, weight: int, features: int) -> int:
+        if not 0 <= weight < self.n_tensors or features < 1:
+            raise ValueError("the plan has no such tensor")
+        return self.elems[weight] // features
+
+    def embedding_lookup(self, table: Sequence[int], vocab: int, width: int, ids: Sequence[int], tokens: Sequence[int],
+                         out: Sequence[int], scale: float = 1.0, id_bytes: int = 8, out_pitch: Optional[int] = None,
+                         stream: int = 0) -> None:
+        per = self._per_worker
+        _check(lib().caramel_embedding_lookup(
+            self._h, per(C.c_void_p, table, "table"), vocab, width, scale, per(C.c_void_p, ids, "ids"), id_bytes,
+            per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, out, "out"), width if out_pitch is None else out_pitch, stream))
+
+    def embedding_workspace(self, tensor: int, width: int, tokens: Sequence[int]) -> int:
+        """Bytes of workspace that embedding_gradient needs for these sizes."""
+        n = C.c_uint64()
+        _check(lib().caramel_embedding_workspace(self._h, tensor, width, self._per_worker(C.c_uint64, tokens, "tokens"),
+                                                 C.byref(n)))
+        return n.value
+
+    def embedding_gradient(self, tensor: int, width: int, ids: Sequence[int], tokens: Sequence[int], dy: Sequence[int],
+                           ws: int, ws_bytes: int, scale: float = 1.0, id_bytes: int = 8, dy_dtype: Optional[int] = None,
+                           dy_pitch: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
+        """dy_dtype None: the plan's."""
+        per = self._per_worker
+        _check(lib().caramel_embedding_gradient(
+            self._h, tensor, width, scale, per(C.c_void_p, ids, "ids"), id_bytes, per(C.c_uint64, tokens, "tokens"),
+            per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype, width if dy_pitch is None else dy_pitch,
+            int(accumulate), ws, ws_bytes, stream))
+
+    def checkpoint_store(self, x: Sequence[int], tokens: Sequence[int], features: int, checkpoint: Sequence[int],
+                         dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
+        per = self._per_worker
+        _check(lib().caramel_checkpoint_store(
+            self._h, per(C.c_uint64, tokens, "tokens"), features, per(C.c_void_p, x, "x"),
+            self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch,
+            per(C.c_void_p, checkpoint, "checkpoint"), stream))
+
+    def checkpoint_load(self, checkpoint: Sequence[int], tokens: Sequence[int], features: int, x: Sequence[int],
+                        dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
+        per = self._per_worker
+        _check(lib().caramel_checkpoint_load(
+            self._h, per(C.c_uint64, tokens, "tokens"), features, per(C.c_void_p, checkpoint, "checkpoint"),
+            per(C.c_void_p, x, "x"), self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch, stream))
+
+    def weight_gradient_workspace(self, weight: int, features: int, tokens: Sequence[int]) -> int:
+        """Bytes of workspace that weight_gradient needs for these sizes (may be 0)."""
+        n = C.c_uint64()
+        _check(lib().caramel_weight_gradient_workspace(self._h, weight, features,
+                                                       self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        return n.value
+
+    def weight_gradient(self, weight: int, bias: Optional[int], checkpoint: Sequence[int], tokens: Sequence[int],
+                        features: int, dy: Sequence[int], ws: Optional[int], ws_bytes: int, dy_dtype: Optional[int] = None,
+                        dy_pitch: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
+        """bias None: no bias gradient; dy_dtype None: the plan's; dy_pitch None: rows without gaps."""
+        per = self._per_worker
+        _check(lib().caramel_weight_gradient(
+            self._h, weight, NO_TENSOR if bias is None else bias, features, per(C.c_void_p, checkpoint, "checkpoint"),
+            per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype,
+            self._outputs(weight, features) if dy_pitch is None else dy_pitch, int(accumulate), ws, ws_bytes, stream))
+
     def profile(self, level: int) -> None:
         _check(lib().caramel_profile(self._h, int(level)))
 
@@ -269,6 +350,13 @@ class Plan:
         _check(lib().caramel_profile_read(self._h, buf))
         return [dict(launches=s.launches, total_ms=s.total_ms, span_ms=s.span_ms, calls=s.calls, elements=s.elements)
                 for s in buf]
+
+
+def checkpoint_bytes(tokens: int, features: int) -> int:
+    """Bytes of the 8-bit checkpoint of `tokens` x `features` activations."""
+    n = C.c_uint64()
+    _check(lib().caramel_checkpoint_bytes(tokens, features, C.byref(n)))
+    return n.value
 
 
 PROBE_READ, PROBE_WRITE, PROBE_UPDATE, PROBE_COPY = 0, 1, 2, 3

@@ -16,6 +16,7 @@
 
 #include "caramel.h"
 #include "kernels.hpp"
+#include "layers.hpp"
 #include "plan.hpp"
 #include "schedule.hpp"
 #include "slices.hpp"
@@ -1058,6 +1059,366 @@ int allreduce_static(caramel_plan* p, void* const* grads, hipStream_t stream) {
 
 int caramel_allreduce_static(caramel_plan* p, void* const* grads, void* stream) {
   return guarded([&] { return allreduce_static(p, grads, hipStream_t(stream)); });
+}
+
+// ---- what fills a plan's gradient tensors ---------------------------------------------------
+
+namespace {
+
+constexpr uint64_t kMaxTokens = uint64_t(1) << 25;
+constexpr uint64_t kMaxWidth = uint64_t(1) << 20;  // columns of a table, features, outputs
+constexpr uint64_t kMaxPitch = uint64_t(1) << 23;
+constexpr uint64_t kMaxValues = uint64_t(1) << 38;  // tokens * columns of a worker
+
+uint64_t size_of(uint32_t dtype) { return dtype == CARAMEL_F32 ? 4 : 2; }
+
+// The plan may be unbound (nothing of it is on a device), but not bound on another device.
+int need_device(const caramel_plan* p) {
+  if (p->device < 0) return CARAMEL_OK;
+  int dev = -1;
+  HIP_TRY(hipGetDevice(&dev));
+  if (dev != p->device)
+    return fail(CARAMEL_ESTATE, "plan was bound with device %d current, now device %d is", p->device, dev);
+  return CARAMEL_OK;
+}
+
+// Memory a call reads and writes.  Nothing it writes may overlap anything else of the call.
+struct Memory {
+  struct Span {
+    uint64_t lo, hi;
+    bool written;
+  };
+  std::vector<Span> spans;
+
+  void add(uint64_t at, uint64_t bytes, bool written) {
+    if (bytes) spans.push_back({at, at + bytes, written});
+  }
+  int check() {
+    std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.lo < y.lo; });
+    uint64_t any = 0, written = 0;  // how far what came before reaches
+    for (const Span& s : spans) {
+      if (s.lo < written || (s.written && s.lo < any)) return fail(CARAMEL_EINVAL, "buffers overlap with one that is written");
+      any = std::max(any, s.hi);
+      if (s.written) written = std::max(written, s.hi);
+    }
+    return CARAMEL_OK;
+  }
+};
+
+int take_tokens(const caramel_plan* p, const uint64_t* tokens, uint32_t* out, uint32_t* most) {
+  if (!tokens) return fail(CARAMEL_EINVAL, "tokens is NULL");
+  *most = 0;
+  for (uint32_t w = 0; w < p->host.cfg.world; ++w) {
+    if (tokens[w] > kMaxTokens) return fail(CARAMEL_EINVAL, "tokens[%u] = %llu is more than 2^25", w, (unsigned long long)tokens[w]);
+    out[w] = uint32_t(tokens[w]);
+    *most = std::max(*most, out[w]);
+  }
+  return CARAMEL_OK;
+}
+
+// One pointer per worker; that of a worker without tokens is not used, and may be NULL.
+int take_pointers(const caramel_plan* p, const char* name, const void* const* from, const uint32_t* tokens, uint64_t align,
+                  uint64_t* out) {
+  if (!from) return fail(CARAMEL_EINVAL, "%s is NULL", name);
+  for (uint32_t w = 0; w < p->host.cfg.world; ++w) {
+    out[w] = reinterpret_cast<uint64_t>(from[w]);
+    if (tokens && !tokens[w]) continue;
+    if (!out[w]) return fail(CARAMEL_EINVAL, "%s[%u] is NULL", name, w);
+    if (out[w] % align) return fail(CARAMEL_EINVAL, "%s[%u] is not aligned to %llu bytes", name, w, (unsigned long long)align);
+  }
+  return CARAMEL_OK;
+}
+
+int check_columns(const char* name, uint64_t columns) {
+  if (columns == 0 || columns > kMaxWidth) return fail(CARAMEL_EINVAL, "%s must be 1 to 2^20, is %llu", name, (unsigned long long)columns);
+  return CARAMEL_OK;
+}
+
+int check_rows(const char* name, uint64_t pitch, uint64_t columns, uint32_t most) {
+  if (pitch < columns || pitch > kMaxPitch)
+    return fail(CARAMEL_EINVAL, "%s must be %llu to 2^23 elements, is %llu", name, (unsigned long long)columns, (unsigned long long)pitch);
+  if (uint64_t(most) * pitch > kMaxValues) return fail(CARAMEL_EINVAL, "more than 2^38 values at one worker");
+  return CARAMEL_OK;
+}
+
+int check_dtype(const char* name, uint32_t dtype) {
+  if (dtype != CARAMEL_F32 && dtype != CARAMEL_BF16) return fail(CARAMEL_EINVAL, "unknown %s %u", name, dtype);
+  return CARAMEL_OK;
+}
+
+int check_workspace(const void* ws, uint64_t have, uint64_t need) {
+  if (need == 0) return CARAMEL_OK;
+  if (!ws) return fail(CARAMEL_EINVAL, "the workspace is NULL, %llu bytes are needed", (unsigned long long)need);
+  if (reinterpret_cast<uint64_t>(ws) % 16) return fail(CARAMEL_EINVAL, "the workspace is not aligned to 16 bytes");
+  if (have < need)
+    return fail(CARAMEL_EINVAL, "the workspace has %llu bytes, %llu are needed", (unsigned long long)have, (unsigned long long)need);
+  return CARAMEL_OK;
+}
+
+// bytes of `tokens` rows, the last one without what lies behind it
+uint64_t rows_bytes(uint64_t tokens, uint64_t pitch, uint64_t columns, uint64_t es) {
+  return tokens ? ((tokens - 1) * pitch + columns) * es : 0;
+}
+
+uint64_t checkpoint_size(uint64_t tokens, uint64_t features) {
+  return (checkpoint_blocks(tokens) * features * (kCheckpointBlock + 1) + 15) / 16 * 16;
+}
+
+int check_table(uint64_t vocab, uint64_t width) {
+  if (int rc = check_columns("width", width)) return rc;
+  if (vocab == 0 || vocab >= 0x7FFFFFFFull) return fail(CARAMEL_EINVAL, "vocab must be 1 to 2^31 - 2, is %llu", (unsigned long long)vocab);
+  return CARAMEL_OK;
+}
+
+// A tensor of the plan as a matrix with `columns` columns
+int check_matrix(const caramel_plan* p, const char* name, uint32_t tensor, uint64_t columns, uint64_t* rows) {
+  if (tensor >= p->host.tensor_elems.size()) return fail(CARAMEL_EINVAL, "the plan has no tensor %u (%s)", tensor, name);
+  const uint64_t n = p->host.tensor_elems[tensor];
+  if (columns == 0 || n % columns)
+    return fail(CARAMEL_EINVAL, "tensor %u (%s) has %llu elements, no multiple of %llu", tensor, name, (unsigned long long)n,
+                (unsigned long long)columns);
+  *rows = n / columns;
+  return CARAMEL_OK;
+}
+
+int embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, uint64_t width, float scale, const void* const* ids,
+                     uint32_t id_bytes, const uint64_t* tokens, void* const* out, uint64_t out_pitch, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  const uint64_t es = p->host.elem_size();
+  LookupArgs a{};
+  if (int rc = check_table(vocab, width)) return rc;
+  if (id_bytes != 4 && id_bytes != 8) return fail(CARAMEL_EINVAL, "id_bytes must be 4 or 8, is %u", id_bytes);
+  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("out_pitch", out_pitch, width, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "table", table, a.w.tokens, es, a.w.a)) return rc;
+  if (int rc = take_pointers(p, "ids", ids, a.w.tokens, id_bytes, a.w.b)) return rc;
+  if (int rc = take_pointers(p, "out", out, a.w.tokens, es, a.w.c)) return rc;
+  a.world = p->host.cfg.world;
+  Memory m;
+  for (uint32_t w = 0; w < a.world; ++w) {
+    if (!a.w.tokens[w]) continue;
+    m.add(a.w.a[w], vocab * width * es, false);
+    m.add(a.w.b[w], uint64_t(a.w.tokens[w]) * id_bytes, false);
+    m.add(a.w.c[w], rows_bytes(a.w.tokens[w], out_pitch, width, es), true);
+  }
+  if (int rc = m.check()) return rc;
+  if (int rc = need_device(p)) return rc;
+  a.vocab = uint32_t(vocab);
+  a.width = uint32_t(width);
+  a.out_pitch = out_pitch;
+  a.scale = scale;
+  a.ids64 = id_bytes == 8;
+  a.bf16 = p->host.cfg.dtype == CARAMEL_BF16;
+  if (tracing())
+    std::fprintf(stderr, "caramel: embedding lookup stream %p, %u workers, up to %u tokens, %u columns\n", (void*)stream, a.world,
+                 a.max_tokens, a.width);
+  HIP_TRY(launch_embedding_lookup(a, stream));
+  return CARAMEL_OK;
+}
+
+int embedding_workspace(const caramel_plan* p, uint32_t tensor, uint64_t width, const uint64_t* tokens, uint64_t* bytes) {
+  if (!p || !bytes) return fail(CARAMEL_EINVAL, "NULL argument");
+  uint64_t vocab = 0;
+  uint32_t n[CARAMEL_MAX_WORLD], most = 0;
+  if (int rc = check_matrix(p, "table", tensor, width, &vocab)) return rc;
+  if (int rc = check_table(vocab, width)) return rc;
+  if (int rc = take_tokens(p, tokens, n, &most)) return rc;
+  *bytes = embedding_gradient_workspace(p->host.cfg.world, uint32_t(vocab), uint32_t(width), most);
+  return CARAMEL_OK;
+}
+
+int embedding_gradient(caramel_plan* p, uint32_t tensor, uint64_t width, float scale, const void* const* ids, uint32_t id_bytes,
+                       const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype, uint64_t dy_pitch, int accumulate,
+                       void* ws, uint64_t ws_bytes, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  const uint64_t es = p->host.elem_size();
+  uint64_t vocab = 0;
+  EmbeddingGradientArgs a{};
+  if (int rc = check_matrix(p, "table", tensor, width, &vocab)) return rc;
+  if (int rc = check_table(vocab, width)) return rc;
+  if (id_bytes != 4 && id_bytes != 8) return fail(CARAMEL_EINVAL, "id_bytes must be 4 or 8, is %u", id_bytes);
+  if (int rc = check_dtype("dy_dtype", dy_dtype)) return rc;
+  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("dy_pitch", dy_pitch, width, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "ids", ids, a.w.tokens, id_bytes, a.w.a)) return rc;
+  if (int rc = take_pointers(p, "dy", dy, a.w.tokens, size_of(dy_dtype), a.w.b)) return rc;
+  a.world = p->host.cfg.world;
+  const uint64_t need = embedding_gradient_workspace(a.world, uint32_t(vocab), uint32_t(width), a.max_tokens);
+  if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
+  if (int rc = need_bound(p, false)) return rc;
+  Memory m;
+  m.add(reinterpret_cast<uint64_t>(ws), need, true);
+  for (uint32_t w = 0; w < a.world; ++w) {
+    a.w.c[w] = p->bind.rows[tensor * a.world + w];
+    m.add(a.w.c[w], vocab * width * es, true);
+    m.add(a.w.a[w], uint64_t(a.w.tokens[w]) * id_bytes, false);
+    m.add(a.w.b[w], rows_bytes(a.w.tokens[w], dy_pitch, width, size_of(dy_dtype)), false);
+  }
+  if (int rc = m.check()) return rc;
+  a.vocab = uint32_t(vocab);
+  a.width = uint32_t(width);
+  a.dy_pitch = dy_pitch;
+  a.scale = scale;
+  a.ids64 = id_bytes == 8;
+  a.dy_bf16 = dy_dtype == CARAMEL_BF16;
+  a.out_bf16 = p->host.cfg.dtype == CARAMEL_BF16;
+  a.accumulate = accumulate != 0;
+  a.ws = static_cast<unsigned char*>(ws);
+  if (tracing())
+    std::fprintf(stderr, "caramel: embedding gradient stream %p, tensor %u, %u workers, up to %u tokens, %u x %u\n", (void*)stream,
+                 tensor, a.world, a.max_tokens, a.vocab, a.width);
+  HIP_TRY(launch_embedding_gradient(a, stream));
+  return CARAMEL_OK;
+}
+
+int checkpoint_call(caramel_plan* p, bool store, const uint64_t* tokens, uint64_t features, const void* const* x, uint32_t dtype,
+                    uint64_t pitch, const void* const* checkpoint, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  CheckpointArgs a{};
+  if (int rc = check_columns("features", features)) return rc;
+  if (int rc = check_dtype("dtype", dtype)) return rc;
+  const uint64_t es = size_of(dtype);
+  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("pitch", pitch, features, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "x", x, a.w.tokens, es, a.w.a)) return rc;
+  if (int rc = take_pointers(p, "checkpoint", checkpoint, a.w.tokens, 16, a.w.b)) return rc;
+  a.world = p->host.cfg.world;
+  Memory m;
+  for (uint32_t w = 0; w < a.world; ++w) {
+    m.add(a.w.a[w], rows_bytes(a.w.tokens[w], pitch, features, es), !store);
+    m.add(a.w.b[w], checkpoint_size(a.w.tokens[w], features), store);
+  }
+  if (int rc = m.check()) return rc;
+  if (int rc = need_device(p)) return rc;
+  a.features = uint32_t(features);
+  a.pitch = pitch;
+  a.bf16 = dtype == CARAMEL_BF16;
+  if (tracing())
+    std::fprintf(stderr, "caramel: checkpoint %s stream %p, %u workers, up to %u tokens, %u features\n", store ? "store" : "load",
+                 (void*)stream, a.world, a.max_tokens, a.features);
+  HIP_TRY(store ? launch_checkpoint_store(a, stream) : launch_checkpoint_load(a, stream));
+  return CARAMEL_OK;
+}
+
+int weight_workspace(const caramel_plan* p, uint32_t weight, uint64_t features, const uint64_t* tokens, uint64_t* bytes) {
+  if (!p || !bytes) return fail(CARAMEL_EINVAL, "NULL argument");
+  uint64_t outputs = 0;
+  uint32_t n[CARAMEL_MAX_WORLD], most = 0;
+  if (int rc = check_matrix(p, "weight", weight, features, &outputs)) return rc;
+  if (int rc = check_columns("features", features)) return rc;
+  if (int rc = check_columns("outputs", outputs)) return rc;
+  if (int rc = take_tokens(p, tokens, n, &most)) return rc;
+  *bytes = weight_gradient_workspace(p->host.cfg.world, uint32_t(features), uint32_t(outputs), most);
+  return CARAMEL_OK;
+}
+
+int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t features, const void* const* checkpoint,
+                    const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype, uint64_t dy_pitch, int accumulate, void* ws,
+                    uint64_t ws_bytes, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  const uint64_t es = p->host.elem_size();
+  uint64_t outputs = 0;
+  WeightGradientArgs a{};
+  if (int rc = check_matrix(p, "weight", weight, features, &outputs)) return rc;
+  if (int rc = check_columns("features", features)) return rc;
+  if (int rc = check_columns("outputs", outputs)) return rc;
+  a.has_bias = bias != CARAMEL_NO_TENSOR;
+  if (a.has_bias) {
+    if (bias >= p->host.tensor_elems.size() || bias == weight || p->host.tensor_elems[bias] != outputs)
+      return fail(CARAMEL_EINVAL, "tensor %u is no bias of %llu outputs", bias, (unsigned long long)outputs);
+  }
+  if (int rc = check_dtype("dy_dtype", dy_dtype)) return rc;
+  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("dy_pitch", dy_pitch, outputs, a.max_tokens)) return rc;
+  if (uint64_t(a.max_tokens) * features > kMaxValues) return fail(CARAMEL_EINVAL, "more than 2^38 values at one worker");
+  if (int rc = take_pointers(p, "checkpoint", checkpoint, a.w.tokens, 16, a.w.a)) return rc;
+  if (int rc = take_pointers(p, "dy", dy, a.w.tokens, size_of(dy_dtype), a.w.b)) return rc;
+  a.world = p->host.cfg.world;
+  const uint64_t need = weight_gradient_workspace(a.world, uint32_t(features), uint32_t(outputs), a.max_tokens);
+  if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
+  if (int rc = need_bound(p, false)) return rc;
+  Memory m;
+  m.add(reinterpret_cast<uint64_t>(ws), need, true);
+  for (uint32_t w = 0; w < a.world; ++w) {
+    a.w.c[w] = p->bind.rows[weight * a.world + w];
+    m.add(a.w.c[w], features * outputs * es, true);
+    if (a.has_bias) {
+      a.bias[w] = p->bind.rows[bias * a.world + w];
+      m.add(a.bias[w], outputs * es, true);
+    }
+    m.add(a.w.a[w], checkpoint_size(a.w.tokens[w], features), false);
+    m.add(a.w.b[w], rows_bytes(a.w.tokens[w], dy_pitch, outputs, size_of(dy_dtype)), false);
+  }
+  if (int rc = m.check()) return rc;
+  a.features = uint32_t(features);
+  a.outputs = uint32_t(outputs);
+  a.dy_pitch = dy_pitch;
+  a.dy_bf16 = dy_dtype == CARAMEL_BF16;
+  a.out_bf16 = p->host.cfg.dtype == CARAMEL_BF16;
+  a.accumulate = accumulate != 0;
+  a.ws = static_cast<unsigned char*>(ws);
+  if (tracing())
+    std::fprintf(stderr, "caramel: weight gradient stream %p, tensor %u, %u workers, up to %u tokens, %u x %u\n", (void*)stream,
+                 weight, a.world, a.max_tokens, a.features, a.outputs);
+  HIP_TRY(launch_weight_gradient(a, stream));
+  return CARAMEL_OK;
+}
+
+}  // namespace
+
+int caramel_embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, uint64_t width, float scale,
+                             const void* const* ids, uint32_t id_bytes, const uint64_t* tokens, void* const* out,
+                             uint64_t out_pitch, void* stream) {
+  return guarded([&] {
+    return embedding_lookup(p, table, vocab, width, scale, ids, id_bytes, tokens, out, out_pitch, hipStream_t(stream));
+  });
+}
+
+int caramel_embedding_workspace(const caramel_plan* p, uint32_t tensor, uint64_t width, const uint64_t* tokens, uint64_t* bytes) {
+  return guarded([&] { return embedding_workspace(p, tensor, width, tokens, bytes); });
+}
+
+int caramel_embedding_gradient(caramel_plan* p, uint32_t tensor, uint64_t width, float scale, const void* const* ids,
+                               uint32_t id_bytes, const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype,
+                               uint64_t dy_pitch, int accumulate, void* ws, uint64_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return embedding_gradient(p, tensor, width, scale, ids, id_bytes, tokens, dy, dy_dtype, dy_pitch, accumulate, ws, ws_bytes,
+                              hipStream_t(stream));
+  });
+}
+
+int caramel_checkpoint_bytes(uint64_t tokens, uint64_t features, uint64_t* bytes) {
+  return guarded([&]() -> int {
+    if (!bytes) return fail(CARAMEL_EINVAL, "NULL argument");
+    if (int rc = check_columns("features", features)) return rc;
+    if (tokens > kMaxTokens) return fail(CARAMEL_EINVAL, "tokens = %llu is more than 2^25", (unsigned long long)tokens);
+    *bytes = checkpoint_size(tokens, features);
+    return CARAMEL_OK;
+  });
+}
+
+int caramel_checkpoint_store(caramel_plan* p, const uint64_t* tokens, uint64_t features, const void* const* x, uint32_t dtype,
+                             uint64_t pitch, void* const* checkpoint, void* stream) {
+  return guarded([&] { return checkpoint_call(p, true, tokens, features, x, dtype, pitch, checkpoint, hipStream_t(stream)); });
+}
+
+int caramel_checkpoint_load(caramel_plan* p, const uint64_t* tokens, uint64_t features, const void* const* checkpoint,
+                            void* const* x, uint32_t dtype, uint64_t pitch, void* stream) {
+  return guarded([&] { return checkpoint_call(p, false, tokens, features, x, dtype, pitch, checkpoint, hipStream_t(stream)); });
+}
+
+int caramel_weight_gradient_workspace(const caramel_plan* p, uint32_t weight, uint64_t features, const uint64_t* tokens,
+                                      uint64_t* bytes) {
+  return guarded([&] { return weight_workspace(p, weight, features, tokens, bytes); });
+}
+
+int caramel_weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t features, const void* const* checkpoint,
+                            const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype, uint64_t dy_pitch, int accumulate,
+                            void* ws, uint64_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return weight_gradient(p, weight, bias, features, checkpoint, tokens, dy, dy_dtype, dy_pitch, accumulate, ws, ws_bytes,
+                           hipStream_t(stream));
+  });
 }
 
 int caramel_allreduce_loop(caramel_plan* p, void* stream, uint32_t n_calls, double* host_us_per_call,
