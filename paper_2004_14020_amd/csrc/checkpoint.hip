@@ -10,16 +10,17 @@
 // Layout: codes [block][feature][32], then the scales [block][feature] as e + 127 (255: the mark).  32 tokens
 // of a feature are 32 contiguous bytes, which is the order in which a matrix product over the tokens wants them.
 //
-// Bound: HBM, each value read and written once.  A lane keeps four features of all 32 tokens in registers: the
-// largest magnitude needs no other lane.
+// Bound: HBM, each value read and written once.  A wavefront takes one block of 256 features (128 where fp32 is
+// stored, for the registers).  A lane keeps its features of all 32 tokens in registers, so the largest magnitude needs no other lane, and all 32 loads (buffer loads,
+// whose range check takes care of rows behind the last token) are in flight at once.  The codes are exchanged through LDS, so that
+// a wavefront's memory access on their side is 1 KiB in one piece; a lane's own codes are 32 bytes a feature.
 #include "layers.hpp"
 #include "vec.hpp"
 
 namespace caramel {
 namespace {
 
-constexpr int kFeatures = 4;  // of a lane
-
+constexpr int kWaves = 4;               // of a workgroup
 constexpr uint32_t kTop = 0x7F7E0000u;  // 127 * 2^121
 
 // scale byte of a block from the bits of its largest magnitude
@@ -28,127 +29,220 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
   return largest >= 0x7F800000u ? 255u : uint32_t(min(max(e, 1), 121 + 127));
 }
 
-template <bool BF16>
-__global__ void __launch_bounds__(256) k_checkpoint_store(CheckpointArgs a) {
-  constexpr int ES = BF16 ? 2 : 4;
-  const uint32_t w = blockIdx.y, n = a.w.tokens[w], wide = (a.features + 256 * kFeatures - 1) / (256 * kFeatures);
-  const uint32_t block = blockIdx.x / wide, blocks = (n + kCheckpointBlock - 1) / kCheckpointBlock;
-  const uint32_t f = (blockIdx.x % wide * 256 + threadIdx.x) * kFeatures;
-  if (block >= blocks || f >= a.features) return;
-  const uint32_t rows = min(n - block * kCheckpointBlock, kCheckpointBlock);
-  const uint32_t cols = min(a.features - f, uint32_t(kFeatures));
-  const uint64_t src = a.w.a[w] + (uint64_t(block) * kCheckpointBlock * a.pitch + f) * ES;
-  float x[kCheckpointBlock][kFeatures];
+// Where a wavefront works: one block of tokens, FEATURES of every lane.
+struct Place {
+  uint32_t w, block, blocks, rows, f0, left;  // left: features from f0 on
+  bool any;
+};
+template <int FEATURES>
+__device__ __forceinline__ Place place(const CheckpointArgs& a) {
+  Place p;
+  const uint32_t wide = (a.features + 64 * FEATURES - 1) / (64 * FEATURES);
+  const uint32_t at = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  p.w = blockIdx.y;
+  p.block = at / wide;
+  p.f0 = (at - p.block * wide) * 64 * FEATURES;
+  const uint32_t n = a.w.tokens[p.w];
+  p.blocks = (n + kCheckpointBlock - 1) / kCheckpointBlock;
+  p.any = p.block < p.blocks;
+  p.rows = p.any ? min(n - p.block * kCheckpointBlock, kCheckpointBlock) : 0;
+  p.left = a.features - p.f0;
+  return p;
+}
+
+// 64 x PIECES pieces of 16 bytes in LDS: lane l's piece c.  The exchange of c's bits spreads the lanes' pieces over the
+// banks, which lie PIECES pieces apart.
+template <int PIECES>
+__device__ __forceinline__ uint32_t slot(uint32_t l, uint32_t c) {
+  return l * PIECES + (c ^ (l & (PIECES - 1)));
+}
+
+// ODD: bf16 rows that start or end in the middle of a pair; elements are loaded one by one.
+template <bool BF16, bool ODD>
+__global__ void __launch_bounds__(64 * kWaves) k_checkpoint_store(CheckpointArgs a) {
+  constexpr int ES = BF16 ? 2 : 4, kFeatures = BF16 ? 4 : 2, kPieces = 2 * kFeatures;
+  constexpr int WORDS = 2;  // 32-bit words of a lane's values of one token
+  typedef uint32_t raw __attribute__((ext_vector_type(WORDS)));
+  __shared__ u32x4 lds[kWaves][64 * kPieces];
+  const Place p = place<kFeatures>(a);
+  if (!p.any) return;
+  const uint32_t lane = threadIdx.x % 64, row_bytes = uint32_t(a.pitch) * ES;
+  u32x4* const mine = lds[threadIdx.x / 64];
+  const __amdgpu_buffer_rsrc_t rx = buffer(a.w.a[p.w] + (uint64_t(p.block) * kCheckpointBlock * a.pitch + p.f0) * ES,
+                                           (p.rows - 1) * row_bytes + p.left * ES);
+  raw x[kCheckpointBlock];
 #pragma unroll
   for (uint32_t r = 0; r < kCheckpointBlock; ++r) {
-    for (int j = 0; j < kFeatures; ++j) x[r][j] = 0.0f;
-    if (r < rows) {
-      const uint64_t at = src + r * a.pitch * ES;
-      if (cols == kFeatures) {
-        load_elems<BF16, kFeatures>(at, x[r]);
-      } else {
+    const int off = int(r * row_bytes + lane * kFeatures * ES);
+    if constexpr (ODD) {
 #pragma unroll
-        for (int j = 0; j < kFeatures; ++j)
-          if (uint32_t(j) < cols) load_elems<BF16, 1>(at + j * ES, &x[r][j]);
+      for (int d = 0; d < WORDS; ++d)
+        x[r][d] = uint32_t(__builtin_amdgcn_raw_buffer_load_b16(rx, off + 4 * d, 0, 0)) |
+                  uint32_t(__builtin_amdgcn_raw_buffer_load_b16(rx, off + 4 * d + 2, 0, 0)) << 16;
+    } else {
+      x[r] = __builtin_amdgcn_raw_buffer_load_b64(rx, off, 0, 0);
+    }
+  }
+  // largest magnitudes: as integers, magnitudes are in order, and NaN above infinity above the numbers
+  uint32_t largest[kFeatures];
+  if constexpr (BF16) {
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    u16x4 m = 0;
+#pragma unroll
+    for (uint32_t r = 0; r < kCheckpointBlock; ++r)
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x4, x[r] & 0x7FFF7FFFu));
+#pragma unroll
+    for (int j = 0; j < kFeatures; ++j) largest[j] = uint32_t(m[j]) << 16;
+  } else {
+    raw m = 0;
+#pragma unroll
+    for (uint32_t r = 0; r < kCheckpointBlock; ++r) m = __builtin_elementwise_max(m, x[r] & 0x7FFFFFFFu);
+#pragma unroll
+    for (int j = 0; j < kFeatures; ++j) largest[j] = m[j];
+  }
+  // numbers above 127 * 2^121 become that
+  bool beyond = false;
+#pragma unroll
+  for (int j = 0; j < kFeatures; ++j) beyond = beyond || largest[j] > kTop;
+  if (__ballot(beyond)) {
+#pragma unroll
+    for (uint32_t r = 0; r < kCheckpointBlock; ++r) {
+      if constexpr (BF16) {
+        typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+        const u16x4 top = uint16_t(kTop >> 16);
+        const u16x4 m = __builtin_elementwise_min(top, __builtin_bit_cast(u16x4, x[r] & 0x7FFF7FFFu));
+        x[r] = (x[r] & 0x80008000u) | __builtin_bit_cast(raw, m);
+      } else {
+        const raw top = kTop;
+        x[r] = (x[r] & 0x80000000u) | __builtin_elementwise_min(top, x[r] & 0x7FFFFFFFu);
       }
     }
   }
-  const uint64_t codes = a.w.b[w], scales = codes + uint64_t(blocks) * a.features * kCheckpointBlock;
+  uint32_t scale[kFeatures];
 #pragma unroll
   for (int j = 0; j < kFeatures; ++j) {
-    if (uint32_t(j) >= cols) break;
-    uint32_t largest = 0;
-#pragma unroll
-    for (uint32_t r = 0; r < kCheckpointBlock; ++r)
-      largest = max(largest, as_bits(x[r][j]) & 0x7FFFFFFFu);
-    const uint32_t s = scale_byte(largest);
-    if (largest > kTop) {
-      const float top = as_float(kTop);
-#pragma unroll
-      for (uint32_t r = 0; r < kCheckpointBlock; ++r) x[r][j] = fminf(fmaxf(x[r][j], -top), top);
-    }
+    const uint32_t s = scale_byte(largest[j]);
     const uint32_t keep = s == 255u ? 0u : 0xFFFFFFFFu;
     // 2^-e; adding 1.5 * 2^23 leaves round(x / 2^e), ties to even, in the low bits (the product is exact)
     const float inv = as_float((254u - min(s, 253u)) << 23);
-    uint32_t q[8];
+    u32x4 q[2];
 #pragma unroll
     for (int d = 0; d < 8; ++d) {
       uint32_t t[4];
-      for (int k = 0; k < 4; ++k) t[k] = as_bits(__builtin_fmaf(x[4 * d + k][j], inv, 12582912.0f));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float v;
+        if constexpr (BF16) v = j % 2 ? bf16_high(x[4 * d + k][j / 2]) : bf16_low(x[4 * d + k][j / 2]);
+        else v = as_float(x[4 * d + k][j]);
+        t[k] = as_bits(__builtin_fmaf(v, inv, 12582912.0f));
+      }
       const uint32_t lo = __builtin_amdgcn_perm(t[1], t[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(t[3], t[2], 0x04000C0Cu);
-      q[d] = (lo | hi) & keep;
+      q[d / 4][d % 4] = (lo | hi) & keep;
     }
-    const uint64_t feature = uint64_t(block) * a.features + f + j;
-    typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(4)));
-    CARAMEL_GLOBAL vec* const to = reinterpret_cast<CARAMEL_GLOBAL vec*>(codes + feature * kCheckpointBlock);
-    to[0] = vec{q[0], q[1], q[2], q[3]};
-    to[1] = vec{q[4], q[5], q[6], q[7]};
-    *reinterpret_cast<CARAMEL_GLOBAL uint8_t*>(scales + feature) = uint8_t(s);
+    mine[slot<kPieces>(lane, 2 * j)] = q[0];
+    mine[slot<kPieces>(lane, 2 * j + 1)] = q[1];
+    scale[j] = s;
+  }
+  wave_sync();
+  const uint64_t codes = a.w.b[p.w], feature = uint64_t(p.block) * a.features + p.f0;
+  const __amdgpu_buffer_rsrc_t rq = buffer(codes + feature * kCheckpointBlock, p.left * kCheckpointBlock);
+  const __amdgpu_buffer_rsrc_t rs = buffer(codes + uint64_t(p.blocks) * a.features * kCheckpointBlock + feature, p.left);
+#pragma unroll
+  for (uint32_t i = 0; i < kPieces; ++i) {
+    const uint32_t at = i * 64 + lane;
+    __builtin_amdgcn_raw_buffer_store_b128(mine[slot<kPieces>(at / kPieces, at % kPieces)], rq, int(at * 16), 0, 0);
+  }
+  if (a.features % kFeatures == 0) {  // both the rows of scales and this lane's part of one start on a whole store
+    if constexpr (BF16)
+      __builtin_amdgcn_raw_buffer_store_b32(scale[0] | scale[1] << 8 | scale[2] << 16 | scale[3] << 24, rs, int(lane * 4), 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b16(uint16_t(scale[0] | scale[1] << 8), rs, int(lane * 2), 0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kFeatures; ++j) __builtin_amdgcn_raw_buffer_store_b8(uint8_t(scale[j]), rs, int(lane * kFeatures + j), 0, 0);
   }
 }
 
 template <bool BF16>
-__global__ void __launch_bounds__(256) k_checkpoint_load(CheckpointArgs a) {
-  constexpr int ES = BF16 ? 2 : 4;
-  const uint32_t w = blockIdx.y, n = a.w.tokens[w], wide = (a.features + 256 * kFeatures - 1) / (256 * kFeatures);
-  const uint32_t block = blockIdx.x / wide, blocks = (n + kCheckpointBlock - 1) / kCheckpointBlock;
-  const uint32_t f = (blockIdx.x % wide * 256 + threadIdx.x) * kFeatures;
-  if (block >= blocks || f >= a.features) return;
-  const uint32_t rows = min(n - block * kCheckpointBlock, kCheckpointBlock);
-  const uint32_t cols = min(a.features - f, uint32_t(kFeatures));
-  const uint64_t codes = a.w.b[w], scales = codes + uint64_t(blocks) * a.features * kCheckpointBlock;
-  typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(4)));
-  vec q[kFeatures][2];
+__global__ void __launch_bounds__(64 * kWaves) k_checkpoint_load(CheckpointArgs a) {
+  constexpr int ES = BF16 ? 2 : 4, kFeatures = 4, kPieces = 2 * kFeatures;
+  __shared__ u32x4 lds[kWaves][64 * kPieces];
+  const Place p = place<kFeatures>(a);
+  if (!p.any) return;
+  const uint32_t lane = threadIdx.x % 64, row_bytes = uint32_t(a.pitch) * ES;
+  u32x4* const mine = lds[threadIdx.x / 64];
+  const uint64_t codes = a.w.b[p.w], feature = uint64_t(p.block) * a.features + p.f0;
+  const __amdgpu_buffer_rsrc_t rq = buffer(codes + feature * kCheckpointBlock, p.left * kCheckpointBlock);
+  const __amdgpu_buffer_rsrc_t rs = buffer(codes + uint64_t(p.blocks) * a.features * kCheckpointBlock + feature, p.left);
+  u32x4 in[8];
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) in[i] = __builtin_amdgcn_raw_buffer_load_b128(rq, int(i * 1024 + lane * 16), 0, 0);
   float size[kFeatures];
 #pragma unroll
   for (int j = 0; j < kFeatures; ++j) {
-    q[j][0] = q[j][1] = vec{0, 0, 0, 0};
-    size[j] = 0.0f;
-    if (uint32_t(j) < cols) {
-      const uint64_t feature = uint64_t(block) * a.features + f + j;
-      const CARAMEL_GLOBAL vec* const from = reinterpret_cast<const CARAMEL_GLOBAL vec*>(codes + feature * kCheckpointBlock);
-      q[j][0] = from[0];
-      q[j][1] = from[1];
-      const uint32_t s = *reinterpret_cast<const CARAMEL_GLOBAL uint8_t*>(scales + feature);
-      size[j] = as_float(s == 255u ? 0x7FC00000u : s << 23);
-    }
+    const uint32_t s = __builtin_amdgcn_raw_buffer_load_b8(rs, int(lane * 4 + j), 0, 0);
+    size[j] = as_float(s == 255u ? 0x7FC00000u : s << 23);
   }
-  const uint64_t dst = a.w.a[w] + (uint64_t(block) * kCheckpointBlock * a.pitch + f) * ES;
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) mine[slot<kPieces>(i * 8 + lane / 8, lane % 8)] = in[i];
+  wave_sync();
+  u32x4 q[kFeatures][2];
+#pragma unroll
+  for (int j = 0; j < kFeatures; ++j) {
+    q[j][0] = mine[slot<kPieces>(lane, 2 * j)];
+    q[j][1] = mine[slot<kPieces>(lane, 2 * j + 1)];
+  }
+  const uint64_t dst = a.w.a[p.w] + (uint64_t(p.block) * kCheckpointBlock * a.pitch + p.f0) * ES;
+  const __amdgpu_buffer_rsrc_t rx = buffer(dst, (p.rows - 1) * row_bytes + p.left * ES);
+  const uint32_t f = lane * kFeatures;
+  if (f >= p.left) return;
+  // The last features of a row, if they are no whole four, and bf16 rows that do not start on a pair, element by element.
+  const bool whole = f + kFeatures <= p.left && (!BF16 || (dst | row_bytes) % 4 == 0);
 #pragma unroll
   for (uint32_t r = 0; r < kCheckpointBlock; ++r) {
-    if (r < rows) {
-      float y[kFeatures];
+    float y[kFeatures];
 #pragma unroll
-      for (int j = 0; j < kFeatures; ++j) y[j] = float(int8_t(q[j][r / 16][r % 16 / 4] >> (8 * (r % 4)))) * size[j];
-      const uint64_t at = dst + r * a.pitch * ES;
-      if (cols == kFeatures) {
-        store_elems<BF16, kFeatures>(at, y);
-      } else {
+    for (int j = 0; j < kFeatures; ++j) y[j] = float(int8_t(q[j][r / 16][r % 16 / 4] >> (8 * (r % 4)))) * size[j];
+    const int off = int(r * row_bytes + f * ES);
+    if (whole) {
+      if constexpr (BF16)
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])}, rx, off, 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{as_bits(y[0]), as_bits(y[1]), as_bits(y[2]), as_bits(y[3])}, rx, off, 0, 0);
+    } else {
 #pragma unroll
-        for (int j = 0; j < kFeatures; ++j)
-          if (uint32_t(j) < cols) store_elems<BF16, 1>(at + j * ES, &y[j]);
+      for (int j = 0; j < kFeatures; ++j) {
+        const int at = f + j < p.left ? off + j * ES : int(kNowhere);
+        if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(uint16_t(bf16_pair(y[j], y[j])), rx, at, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b32(as_bits(y[j]), rx, at, 0, 0);
       }
     }
   }
 }
 
-dim3 grid_of(const CheckpointArgs& a) {
-  return dim3((a.features + 256 * kFeatures - 1) / (256 * kFeatures) * uint32_t(checkpoint_blocks(a.max_tokens)), a.world);
+dim3 grid_of(const CheckpointArgs& a, uint32_t features) {  // of a lane
+  const uint64_t waves = (a.features + 64 * features - 1) / (64 * features) * checkpoint_blocks(a.max_tokens);
+  return dim3(uint32_t((waves + kWaves - 1) / kWaves), a.world);
 }
 
 }  // namespace
 
 hipError_t launch_checkpoint_store(const CheckpointArgs& a, hipStream_t s) {
   if (a.max_tokens == 0) return hipSuccess;
-  if (a.bf16) hipLaunchKernelGGL((k_checkpoint_store<true>), grid_of(a), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_checkpoint_store<false>), grid_of(a), dim3(256), 0, s, a);
+  bool odd = a.pitch % 2 || a.features % 2;
+  for (uint32_t w = 0; w < a.world; ++w) odd = odd || a.w.a[w] % 4;
+  const dim3 block(64 * kWaves);
+  if (!a.bf16) hipLaunchKernelGGL((k_checkpoint_store<false, false>), grid_of(a, 2), block, 0, s, a);
+  else if (odd) hipLaunchKernelGGL((k_checkpoint_store<true, true>), grid_of(a, 4), block, 0, s, a);
+  else hipLaunchKernelGGL((k_checkpoint_store<true, false>), grid_of(a, 4), block, 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_checkpoint_load(const CheckpointArgs& a, hipStream_t s) {
   if (a.max_tokens == 0) return hipSuccess;
-  if (a.bf16) hipLaunchKernelGGL((k_checkpoint_load<true>), grid_of(a), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_checkpoint_load<false>), grid_of(a), dim3(256), 0, s, a);
+  const dim3 block(64 * kWaves);
+  if (a.bf16) hipLaunchKernelGGL((k_checkpoint_load<true>), grid_of(a, 4), block, 0, s, a);
+  else hipLaunchKernelGGL((k_checkpoint_load<false>), grid_of(a, 4), block, 0, s, a);
   return hipGetLastError();
 }
 

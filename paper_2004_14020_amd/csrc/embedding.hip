@@ -42,8 +42,10 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
     }
   }
   const uint64_t dst = a.w.c[w];
-  for (uint32_t col = lane * N; col < a.width; col += lanes * N) {
-    if (col + N <= a.width) {
+  if (a.width >= N) {
+    for (uint32_t at = lane * N; at < a.width; at += lanes * N) {
+      // the last lane takes the last N columns, some of them a second time
+      const uint32_t col = min(at, a.width - N);
       float x[kLookupRows][N];
 #pragma unroll
       for (int r = 0; r < kLookupRows; ++r) {
@@ -58,18 +60,18 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
           for (int j = 0; j < N; ++j) x[r][j] *= a.scale;
         store_elems<BF16, N>(dst + (i * a.out_pitch + col) * ES, x[r]);
       }
-    } else {
-      for (int r = 0; r < kLookupRows; ++r) {
-        const uint32_t i = first + r * groups;
-        if (i >= n) continue;
-        for (uint32_t k = col; k < a.width; ++k) {
-          float x = 0.0f;
-          if (there[r]) {
-            load_elems<BF16, 1>(src[r] + uint64_t(k) * ES, &x);
-            x *= a.scale;
-          }
-          store_elems<BF16, 1>(dst + (i * a.out_pitch + k) * ES, &x);
+    }
+  } else if (lane == 0) {
+    for (int r = 0; r < kLookupRows; ++r) {
+      const uint32_t i = first + r * groups;
+      if (i >= n) continue;
+      for (uint32_t k = 0; k < a.width; ++k) {
+        float x = 0.0f;
+        if (there[r]) {
+          load_elems<BF16, 1>(src[r] + uint64_t(k) * ES, &x);
+          x *= a.scale;
         }
+        store_elems<BF16, 1>(dst + (i * a.out_pitch + k) * ES, &x);
       }
     }
   }
@@ -87,8 +89,9 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
 //                      no token names.
 //   k_embedding_join   adds the partial sums of the rows that were cut, in the chunks' order.
 
-constexpr int kSortWaves = 16;
-constexpr uint32_t kSortRange = 960;  // most ids of a workgroup: one lane each in the scan, 60 KiB of counters
+constexpr int kSortWaves = 8;
+constexpr int kSortAhead = 8;          // ids per lane that are fetched at once
+constexpr uint32_t kSortRange = 1024;  // most ids of a workgroup: two per lane in the scan, 32 KiB of counters
 
 struct Layout {
   uint64_t start, order, sorted, partial, stride;  // bytes; stride from worker to worker
@@ -120,90 +123,142 @@ __device__ __forceinline__ uint32_t read_id(uint64_t ids, uint32_t i, uint32_t v
   }
 }
 
+// Bound: latency (a few thousand ids from the caches).  With one round per different id among 64 tokens in place of
+// the comparison by bits, and one id in flight per lane: 46.8 us for 8 x 4096 tokens of 30522 words.
 template <bool IDS64>
-__global__ void __launch_bounds__(64 * kSortWaves) k_embedding_sort(EmbeddingGradientArgs a, Layout l, uint32_t range) {
-  extern __shared__ uint32_t lds[];
-  uint32_t* const count = lds;                        // [wave][id - lo]
-  uint32_t* const sums = lds + kSortWaves * range;    // one per wave
-  uint32_t* const lower = sums + kSortWaves;
+__global__ void __launch_bounds__(64 * kSortWaves) k_embedding_sort(EmbeddingGradientArgs a, Layout l, uint32_t range, uint32_t bits) {
+  constexpr uint32_t kLanes = 64 * kSortWaves, kNone = 0xFFFFFFFFu;
+  __shared__ uint32_t count[kSortWaves * kSortRange];  // [wave][id - lo]
+  __shared__ uint32_t sums[2][kSortWaves];
   const uint32_t w = blockIdx.y, n = a.w.tokens[w];
   const uint32_t lo = blockIdx.x * range, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   const uint64_t ids = a.w.a[w];
   unsigned char* const ws = a.ws + w * l.stride;
-  for (uint32_t i = threadIdx.x; i < kSortWaves * range; i += blockDim.x) count[i] = 0;
-  if (threadIdx.x == 0) *lower = 0;
-  __syncthreads();
-  // each wave counts a stretch of the tokens
-  const uint32_t part = (n + 64 * kSortWaves - 1) / (64 * kSortWaves) * 64;
+  // each wave has a stretch of the tokens
+  const uint32_t part = (n + kLanes - 1) / kLanes * 64;
   const uint32_t begin = min(wave * part, n), end = min(begin + part, n);
-  uint32_t below = 0;
-  for (uint32_t i = begin + lane; i < end; i += 64) {
-    const uint32_t id = read_id<IDS64>(ids, i, a.vocab);
-    if (id - lo < range) {
-      if (id != 0xFFFFFFFFu) atomicAdd(&count[wave * range + id - lo], 1u);
-    } else if (id < lo) {
-      ++below;
+  uint32_t id[kSortAhead];
+  auto fetch = [&](uint32_t i0) {
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) {
+      const uint32_t i = i0 + j * 64 + lane;
+      id[j] = i < end ? read_id<IDS64>(ids, i, a.vocab) : kNone;
+    }
+  };
+  // One step of a wavefront's walk: every lane's place among the tokens of its id, in order; the counters move on.
+  volatile uint32_t* const next = count + wave * range;  // one lane moves it on for the others of its wavefront
+  auto rank = [&](uint32_t v) -> uint32_t {
+    const uint32_t key = v - lo;  // kNone - lo is more than any range
+    const bool in = key < range;
+    uint64_t same = __ballot(in);
+    if (!same) return 0;
+    for (uint32_t b = 0; b < bits; ++b) {  // the lanes with the same id
+      const bool one = key >> b & 1;
+      const uint64_t ones = __ballot(one);
+      same &= one ? ones : ~ones;
+    }
+    uint32_t at = 0;
+    if (in) {
+      at = next[key] + __popcll(same & ((uint64_t(1) << lane) - 1));
+      if ((same >> lane) == 1) next[key] = at + 1;  // the last of them
+    }
+    return at;
+  };
+  fetch(begin);
+  for (uint32_t i = threadIdx.x; i < kSortWaves * range; i += kLanes) count[i] = 0;
+  __syncthreads();
+  uint32_t below = 0, place[kSortAhead];
+  for (uint32_t i0 = begin; i0 < end; i0 += 64 * kSortAhead) {
+    if (i0 != begin) fetch(i0);
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) {
+      place[j] = rank(id[j]);
+      below += id[j] < lo;
     }
   }
-  if (below) atomicAdd(lower, below);
+  for (int d = 32; d; d /= 2) below += __shfl_xor(below, d);
+  if (lane == 0) sums[0][wave] = below;
   __syncthreads();
-  // one lane per id: where its tokens go, wave by wave
-  uint32_t mine = 0;
-  if (threadIdx.x < range)
-    for (int v = 0; v < kSortWaves; ++v) {
-      const uint32_t c = count[v * range + threadIdx.x];
-      count[v * range + threadIdx.x] = mine;
-      mine += c;
-    }
-  uint32_t incl = mine;
+  // two ids per lane: where their tokens go, wave by wave
+  const uint32_t r0 = threadIdx.x * 2;
+  uint32_t mine[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (r0 + k < range)
+      for (int v = 0; v < kSortWaves; ++v) {
+        const uint32_t c = count[v * range + r0 + k];
+        count[v * range + r0 + k] = mine[k];
+        mine[k] += c;
+      }
+  uint32_t incl = mine[0] + mine[1];
   for (int d = 1; d < 64; d *= 2) {
     const uint32_t up = __shfl_up(incl, d);
     if (lane >= uint32_t(d)) incl += up;
   }
-  if (lane == 63) sums[wave] = incl;
+  if (lane == 63) sums[1][wave] = incl;
   __syncthreads();
-  uint32_t base = *lower + incl - mine;
-  for (uint32_t v = 0; v < wave; ++v) base += sums[v];
+  uint32_t base = incl - mine[0] - mine[1];
+  for (uint32_t v = 0; v < kSortWaves; ++v) base += sums[0][v] + (v < wave ? sums[1][v] : 0);
   uint32_t* const start = reinterpret_cast<uint32_t*>(ws + l.start);
-  if (threadIdx.x < range) {
-    for (int v = 0; v < kSortWaves; ++v) count[v * range + threadIdx.x] += base;
-    if (lo + threadIdx.x < a.vocab) {
-      start[lo + threadIdx.x] = base;
-      if (lo + threadIdx.x == a.vocab - 1) start[a.vocab] = base + mine;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (r0 + k < range) {
+      for (int v = 0; v < kSortWaves; ++v) count[v * range + r0 + k] += base;
+      if (lo + r0 + k < a.vocab) {
+        start[lo + r0 + k] = base;
+        if (lo + r0 + k == a.vocab - 1) start[a.vocab] = base + mine[k];
+      }
     }
+    base += mine[k];
   }
   __syncthreads();
   // each wave deals out its stretch, in order
   uint32_t* const order = reinterpret_cast<uint32_t*>(ws + l.order);
   uint32_t* const sorted = reinterpret_cast<uint32_t*>(ws + l.sorted);
-  volatile uint32_t* const next = count + wave * range;  // one lane moves it on for the others of its wavefront
-  for (uint32_t i0 = begin; i0 < end; i0 += 64) {
-    const uint32_t i = i0 + lane;
-    const uint32_t id = i < end ? read_id<IDS64>(ids, i, a.vocab) : 0xFFFFFFFFu;
-    const bool in = id != 0xFFFFFFFFu && id - lo < range;
-    uint64_t left = __ballot(in);
-    while (left) {  // one round per different id among the 64
-      const uint32_t who = __ffsll((unsigned long long)left) - 1;
-      const uint32_t v = __builtin_amdgcn_readlane(id, who);
-      const uint64_t same = __ballot(in && id == v);
-      const uint32_t at = next[v - lo];
-      if (in && id == v) {
-        const uint32_t rank = __popcll(same & ((uint64_t(1) << lane) - 1));
-        order[at + rank] = i;
-        sorted[at + rank] = v;
+  const bool kept = end - begin <= 64 * kSortAhead;  // ids and places are still in registers
+  for (uint32_t i0 = begin; i0 < end; i0 += 64 * kSortAhead) {
+    if (!kept) fetch(i0);
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) {
+      const uint32_t key = id[j] - lo;
+      uint32_t to;
+      if (kept) to = key < range ? next[key] + place[j] : 0;
+      else to = rank(id[j]);
+      if (key < range) {
+        order[to] = i0 + j * 64 + lane;
+        sorted[to] = id[j];
       }
-      if (lane == who) next[v - lo] = at + uint32_t(__popcll(same));
-      left &= ~same;
     }
   }
 }
 
+// Columns of one lane: N from `col` on, of which the first `twice` belong to the lane before as well (the last lane takes the
+// last N columns of the row), or fewer than N where a row is that short.
+struct Columns {
+  uint32_t col, count, twice;
+};
+template <int N>
+__device__ __forceinline__ Columns columns(uint32_t at, uint32_t width) {
+  if (width < N) return {0, width, 0};
+  const uint32_t col = min(at, width - N);
+  return {col, N, at - col};
+}
+
+template <int N>
+__device__ __forceinline__ void write_sum(uint64_t at, Columns c, const float* sum) {
+  if (c.count == N) store_elems<false, N>(at, sum);
+  else
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (uint32_t(j) < c.count) store_elems<false, 1>(at + 4 * j, sum + j);
+}
+
 template <bool OUT_BF16, int N>
-__device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64_t out, uint32_t row, uint32_t col,
-                                          uint32_t cols, const float* sum) {
+__device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64_t out, uint32_t row, Columns c, const float* sum) {
   constexpr int ES = OUT_BF16 ? 2 : 4;
-  const uint64_t at = out + (uint64_t(row) * a.width + col) * ES;
-  if (cols >= N) {
+  const uint64_t at = out + (uint64_t(row) * a.width + c.col) * ES;
+  // columns that two lanes have are written by both, with the same value, but added to by one
+  if (c.count == N && !(a.accumulate && c.twice)) {
     float y[N];
     if (a.accumulate) {
       load_elems<OUT_BF16, N>(at, y);
@@ -215,7 +270,7 @@ __device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      if (uint32_t(j) >= cols) break;
+      if (uint32_t(j) < c.twice || uint32_t(j) >= c.count) continue;
       float y = a.scale * sum[j], old = 0.0f;
       if (a.accumulate) {
         load_elems<OUT_BF16, 1>(at + j * ES, &old);
@@ -229,91 +284,120 @@ __device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64
 constexpr int kSumBlock = 256;
 constexpr int kAhead = 8;  // tokens whose rows are fetched at once
 
-template <bool DY_BF16, bool OUT_BF16>
-__global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientArgs a, Layout l, uint32_t lanes,
-                                                             uint32_t sum_blocks) {
-  constexpr int N = DY_BF16 ? 8 : 4, ES = DY_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4;
-  const uint32_t w = blockIdx.y;
+// Clears the rows that no token names: a wavefront looks at `rows` of them, and `lanes` lanes write one.
+template <bool OUT_BF16>
+__device__ __forceinline__ void clear_rows(const EmbeddingGradientArgs& a, const uint32_t* start, uint64_t out, uint32_t first,
+                                           uint32_t rows, uint32_t lanes) {
+  constexpr int OS = OUT_BF16 ? 2 : 4, N = 16 / OS;
+  if (first >= a.vocab) return;
+  const uint32_t lane = threadIdx.x % 64, r = min(first + lane, a.vocab - 1);
+  const uint64_t empty = __ballot(lane < rows && first + lane < a.vocab && start[r] == start[r + 1]);
+  const float zero[N] = {};
+  for (uint32_t k = lane / lanes; k < rows; k += 64 / lanes) {
+    if (!(empty >> k & 1)) continue;
+    const uint64_t at = out + uint64_t(first + k) * a.width * OS;
+    if (a.width >= N) {
+      for (uint32_t c = lane % lanes * N; c < a.width; c += lanes * N) store_elems<OUT_BF16, N>(at + min(c, a.width - N) * OS, zero);
+    } else {
+      for (uint32_t c = lane % lanes; c < a.width; c += lanes) store_elems<OUT_BF16, 1>(at + c * OS, zero);
+    }
+  }
+}
+
+struct SumShape {
+  uint32_t lanes, sum_blocks;       // lanes of a chunk
+  uint32_t clear_lanes, clear_rows;
+};
+
+// FULL: 64 lanes per chunk, so that the walk along the list is the wavefront's own: its tokens are fetched by one load
+// and handed round through scalar registers.
+template <bool DY_BF16, bool OUT_BF16, bool FULL>
+__global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientArgs a, Layout l, SumShape h) {
+  constexpr int N = DY_BF16 ? 8 : 4, ES = DY_BF16 ? 2 : 4;
+  const uint32_t w = blockIdx.y, lanes = FULL ? 64 : h.lanes;
   const unsigned char* const ws = a.ws + w * l.stride;
   const uint32_t* const start = reinterpret_cast<const uint32_t*>(ws + l.start);
   const uint64_t out = a.w.c[w];
-  const uint32_t lane = threadIdx.x & (lanes - 1);
-  const uint32_t col = (blockIdx.z * lanes + lane) * N;
-  if (blockIdx.x >= sum_blocks) {
-    // rows that no token names: a wavefront looks at 64 of them
-    const uint32_t row0 = ((blockIdx.x - sum_blocks) * (kSumBlock / 64) + threadIdx.x / 64) * 64;
-    if (row0 >= a.vocab) return;
-    const uint32_t r = row0 + threadIdx.x % 64;
-    uint64_t empty = __ballot(r < a.vocab && start[min(r, a.vocab - 1)] == start[min(r, a.vocab - 1) + 1]);
-    const uint32_t c0 = blockIdx.z * lanes * N, c1 = min(c0 + lanes * N, a.width);
-    const float zero[N] = {};
-    while (empty) {
-      const uint32_t row = row0 + __ffsll((unsigned long long)empty) - 1;
-      empty &= empty - 1;
-      const uint64_t at = out + uint64_t(row) * a.width * OS;
-      for (uint32_t c = c0 + threadIdx.x % 64 * N; c < c1; c += 64 * N) {
-        if (c + N <= c1) {
-          store_elems<OUT_BF16, N>(at + uint64_t(c) * OS, zero);
-        } else {
-          for (uint32_t k = c; k < c1; ++k) store_elems<OUT_BF16, 1>(at + uint64_t(k) * OS, zero);
-        }
-      }
-    }
+  if (blockIdx.x >= h.sum_blocks) {
+    const uint32_t wave = ((blockIdx.x - h.sum_blocks) * gridDim.z + blockIdx.z) * (kSumBlock / 64) + threadIdx.x / 64;
+    clear_rows<OUT_BF16>(a, start, out, wave * h.clear_rows, h.clear_rows, h.clear_lanes);
     return;
   }
+  const uint32_t at_col = (blockIdx.z * lanes + threadIdx.x % lanes) * N;
   const uint32_t total = start[a.vocab];
-  const uint32_t chunk = blockIdx.x * (kSumBlock / lanes) + threadIdx.x / lanes;
+  uint32_t chunk = blockIdx.x * (kSumBlock / lanes) + threadIdx.x / lanes;
+  if constexpr (FULL) chunk = __builtin_amdgcn_readfirstlane(chunk);
   const uint32_t c0 = min(chunk, l.chunks) * l.chunk;
-  if (c0 >= total || col >= a.width) return;
+  if (c0 >= total) return;
   const uint32_t c1 = min(c0 + l.chunk, total);
-  const uint32_t cols = min(a.width - col, uint32_t(N));
   const uint32_t* const order = reinterpret_cast<const uint32_t*>(ws + l.order);
   const uint32_t* const sorted = reinterpret_cast<const uint32_t*>(ws + l.sorted);
   const uint64_t partial = reinterpret_cast<uint64_t>(ws + l.partial);
-  const uint64_t dy = a.w.b[w] + uint64_t(col) * ES;
+  const Columns c = columns<N>(at_col, a.width);
+  const bool idle = at_col >= a.width;
+  const uint64_t dy = a.w.b[w] + uint64_t(c.col) * ES;
+  uint32_t list_id = 0, list_token = 0;
+  if constexpr (FULL) {  // a chunk is at most 64 tokens
+    const uint32_t e = min(c0 + threadIdx.x % 64, c1 - 1);
+    list_id = sorted[e];
+    list_token = order[e];
+  } else if (idle) {
+    return;
+  }
+  auto id_of = [&](uint32_t e) -> uint32_t {
+    if constexpr (FULL) return __builtin_amdgcn_readlane(list_id, e - c0);
+    else return sorted[e];
+  };
+  auto token_of = [&](uint32_t e) -> uint32_t {
+    if constexpr (FULL) return __builtin_amdgcn_readlane(list_token, e - c0);
+    else return order[e];
+  };
   float sum[N] = {};
-  uint32_t row = sorted[c0];
+  uint32_t row = id_of(c0);
   auto leave = [&](bool cut_end) {
     const bool cut_begin = start[row] < c0;
+    if (idle) return;
     if (!cut_begin && !cut_end) {
-      write_row<OUT_BF16, N>(a, out, row, col, cols, sum);
+      write_row<OUT_BF16, N>(a, out, row, c, sum);
     } else {
       // the part of a row that began earlier goes into the chunk's first place, one that begins here into the second
-      const uint64_t at = partial + ((uint64_t(chunk) * 2 + (cut_begin ? 0 : 1)) * a.width + col) * 4;
-      if (cols >= N) store_elems<false, N>(at, sum);
-      else
-        for (uint32_t j = 0; j < cols; ++j) store_elems<false, 1>(at + 4 * j, sum + j);
+      write_sum<N>(partial + ((uint64_t(chunk) * 2 + (cut_begin ? 0 : 1)) * a.width + c.col) * 4, c, sum);
     }
   };
-  for (uint32_t e = c0; e < c1; e += kAhead) {
-    float x[kAhead][N];
-    uint32_t id[kAhead];
+  auto walk = [&](auto&& fetch) {
+    for (uint32_t e = c0; e < c1; e += kAhead) {
+      float x[kAhead][N];
+      uint32_t id[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      id[j] = 0xFFFFFFFFu;
-      if (e + j < c1) {
-        id[j] = sorted[e + j];
-        const uint64_t at = dy + uint64_t(order[e + j]) * a.dy_pitch * ES;
-        if (cols >= N) {
-          load_elems<DY_BF16, N>(at, x[j]);
-        } else {
-          for (int k = 0; k < N; ++k) {
-            x[j][k] = 0.0f;
-            if (uint32_t(k) < cols) load_elems<DY_BF16, 1>(at + k * ES, &x[j][k]);
-          }
+      for (int j = 0; j < kAhead; ++j) {
+        // behind the end: the last token again, which is not added
+        const uint32_t at = min(e + j, c1 - 1);
+        id[j] = id_of(at);
+        fetch(dy + uint64_t(token_of(at)) * a.dy_pitch * ES, x[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (e + j >= c1) break;
+        if (id[j] != row) {
+          leave(false);
+          for (int k = 0; k < N; ++k) sum[k] = 0.0f;
+          row = id[j];
         }
+        for (int k = 0; k < N; ++k) sum[k] += x[j][k];
       }
     }
+  };
+  // The choice is made out here: beside each load it would make every load wait for the one before.
+  if (a.width >= N) {
+    walk([&](uint64_t from, float* x) { load_elems<DY_BF16, N>(from, x); });
+  } else {
+    walk([&](uint64_t from, float* x) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (e + j >= c1) break;
-      if (id[j] != row) {
-        leave(false);
-        for (int k = 0; k < N; ++k) sum[k] = 0.0f;
-        row = id[j];
+      for (int k = 0; k < N; ++k) {
+        x[k] = 0.0f;
+        if (uint32_t(k) < a.width) load_elems<DY_BF16, 1>(from + k * ES, x + k);
       }
-      for (int k = 0; k < N; ++k) sum[k] += x[j][k];
-    }
+    });
   }
   leave(start[row + 1] > c1);
 }
@@ -334,28 +418,29 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_join(EmbeddingGra
   const uint32_t row = sorted[c1 - 1], end = start[row + 1];
   if (end <= c1 || start[row] < chunk * l.chunk) return;
   const uint32_t pieces = (end - 1) / l.chunk - chunk + 1;
-  const uint32_t wave = threadIdx.x / 64, col = blockIdx.z * 256 + threadIdx.x % 64 * 4;
-  const uint32_t cols = col < a.width ? min(a.width - col, 4u) : 0u;
+  const uint32_t wave = threadIdx.x / 64, at_col = blockIdx.z * 256 + threadIdx.x % 64 * 4;
+  const Columns c = columns<4>(at_col, a.width);
   const uint32_t share = (pieces + kJoinWaves - 1) / kJoinWaves;
   const uint32_t p0 = min(wave * share, pieces), p1 = min(p0 + share, pieces);
-  const uint64_t partial = reinterpret_cast<uint64_t>(ws + l.partial) + uint64_t(col) * 4;
+  const uint64_t partial = reinterpret_cast<uint64_t>(ws + l.partial) + uint64_t(c.col) * 4;
   float sum[4] = {};
 #pragma unroll 4
   for (uint32_t p = p0; p < p1; ++p) {
     // the first piece lies in the second place of its chunk, the others in the first
     const uint64_t at = partial + (uint64_t(chunk + p) * 2 + (p == 0 ? 1 : 0)) * a.width * 4;
     float x[4] = {};
-    if (cols == 4) load_elems<false, 4>(at, x);
+    if (a.width >= 4) load_elems<false, 4>(at, x);
     else
-      for (uint32_t j = 0; j < cols; ++j) load_elems<false, 1>(at + 4 * j, x + j);
+      for (int j = 0; j < 4; ++j)
+        if (uint32_t(j) < a.width) load_elems<false, 1>(at + 4 * j, x + j);
     for (int j = 0; j < 4; ++j) sum[j] += x[j];
   }
   for (int j = 0; j < 4; ++j) part[wave][threadIdx.x % 64 * 4 + j] = sum[j];
   __syncthreads();
-  if (wave || !cols) return;
+  if (wave || at_col >= a.width) return;
   for (int v = 1; v < kJoinWaves; ++v)
     for (int j = 0; j < 4; ++j) sum[j] += part[v][threadIdx.x * 4 + j];
-  write_row<OUT_BF16, 4>(a, a.w.c[w], row, col, cols, sum);
+  write_row<OUT_BF16, 4>(a, a.w.c[w], row, c, sum);
 }
 
 uint32_t lanes_for(uint32_t width, uint32_t per_lane, uint32_t most) {
@@ -391,23 +476,41 @@ hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& a, hipStream_t
   // enough workgroups to fill the chip, each with as few ids as that allows
   const uint64_t even = (uint64_t(a.vocab) * a.world + 255) / 256;
   const uint32_t range = uint32_t(std::min<uint64_t>(kSortRange, std::max<uint64_t>(64, even)));
+  uint32_t bits = 0;
+  while ((1u << bits) < range) ++bits;
   const dim3 sort_grid((a.vocab + range - 1) / range, a.world);
-  const size_t lds = (kSortWaves * range + kSortWaves + 1) * sizeof(uint32_t);
-  if (a.ids64) hipLaunchKernelGGL((k_embedding_sort<true>), sort_grid, dim3(64 * kSortWaves), lds, s, a, l, range);
-  else hipLaunchKernelGGL((k_embedding_sort<false>), sort_grid, dim3(64 * kSortWaves), lds, s, a, l, range);
+  if (a.ids64) hipLaunchKernelGGL((k_embedding_sort<true>), sort_grid, dim3(64 * kSortWaves), 0, s, a, l, range, bits);
+  else hipLaunchKernelGGL((k_embedding_sort<false>), sort_grid, dim3(64 * kSortWaves), 0, s, a, l, range, bits);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const uint32_t per_lane = a.dy_bf16 ? 8 : 4, lanes = lanes_for(a.width, per_lane, 64);
-  const uint32_t groups = kSumBlock / lanes, sum_blocks = (l.chunks + groups - 1) / groups;
-  const uint32_t fill_blocks = a.accumulate ? 0 : (a.vocab + kSumBlock - 1) / kSumBlock;
-  const dim3 sum_grid(sum_blocks + fill_blocks, a.world, (a.width + lanes * per_lane - 1) / (lanes * per_lane));
-  if (a.dy_bf16) {
-    if (a.out_bf16) hipLaunchKernelGGL((k_embedding_sum<true, true>), sum_grid, dim3(kSumBlock), 0, s, a, l, lanes, sum_blocks);
-    else hipLaunchKernelGGL((k_embedding_sum<true, false>), sum_grid, dim3(kSumBlock), 0, s, a, l, lanes, sum_blocks);
+  const uint32_t per_lane = a.dy_bf16 ? 8 : 4;
+  SumShape h{};
+  h.lanes = lanes_for(a.width, per_lane, 64);
+  const uint32_t groups = kSumBlock / h.lanes, slices = (a.width + h.lanes * per_lane - 1) / (h.lanes * per_lane);
+  h.sum_blocks = (l.chunks + groups - 1) / groups;
+  h.clear_lanes = lanes_for(a.width, a.out_bf16 ? 8 : 4, 64);
+  h.clear_rows = std::min(64u, 1024 / h.clear_lanes);
+  const uint32_t cleared = h.clear_rows * (kSumBlock / 64) * slices;  // by the workgroups of one x
+  const dim3 sum_grid(h.sum_blocks + (a.accumulate ? 0 : (a.vocab + cleared - 1) / cleared), a.world, slices);
+#define CARAMEL_SUM(DY, OUT, FULL) hipLaunchKernelGGL((k_embedding_sum<DY, OUT, FULL>), sum_grid, dim3(kSumBlock), 0, s, a, l, h)
+  if (h.lanes == 64) {
+    if (a.dy_bf16) {
+      if (a.out_bf16) CARAMEL_SUM(true, true, true);
+      else CARAMEL_SUM(true, false, true);
+    } else {
+      if (a.out_bf16) CARAMEL_SUM(false, true, true);
+      else CARAMEL_SUM(false, false, true);
+    }
   } else {
-    if (a.out_bf16) hipLaunchKernelGGL((k_embedding_sum<false, true>), sum_grid, dim3(kSumBlock), 0, s, a, l, lanes, sum_blocks);
-    else hipLaunchKernelGGL((k_embedding_sum<false, false>), sum_grid, dim3(kSumBlock), 0, s, a, l, lanes, sum_blocks);
+    if (a.dy_bf16) {
+      if (a.out_bf16) CARAMEL_SUM(true, true, false);
+      else CARAMEL_SUM(true, false, false);
+    } else {
+      if (a.out_bf16) CARAMEL_SUM(false, true, false);
+      else CARAMEL_SUM(false, false, false);
+    }
   }
+#undef CARAMEL_SUM
   e = hipGetLastError();
   if (e != hipSuccess || l.chunks < 2) return e;
   const dim3 join_grid(l.chunks - 1, a.world, (a.width + 255) / 256);

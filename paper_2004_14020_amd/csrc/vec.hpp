@@ -16,7 +16,16 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kRawBuffer = 0x00027000;  // word 3 of a buffer resource: untyped data
+// A value that is the same in all lanes, into a scalar register.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return uint32_t(__builtin_amdgcn_readfirstlane(int(v))); }
+
+// A stretch of memory whose accesses the hardware checks, 32 bits by 32 bits: loads behind its end give zeros, stores
+// there are dropped.
+constexpr int kRawBuffer = 0x00027000;      // word 3 of a buffer resource: untyped data
+constexpr uint32_t kNowhere = 0x60000000u;  // an offset behind every end, also with a tile's rows added to it
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(uint64_t base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, int(bytes), kRawBuffer);
+}
 
 // fp32 -> bf16, round to nearest, ties to even, NaN stays NaN
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
@@ -27,6 +36,12 @@ __device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cas
 __device__ __forceinline__ uint32_t as_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
 __device__ __forceinline__ float bf16_low(uint32_t v) { return as_float(v << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t v) { return as_float(v & 0xFFFF0000u); }
+
+// What a wavefront's lanes have written to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // N (1, 4 or 8) consecutive elements, widened to fp32.  Rows may start on any element (odd widths), so the
 // vectors promise the alignment of one element only; the hardware takes such accesses as they are.

@@ -16,6 +16,7 @@
 // of the operand.  The tokens are dealt to the operand's places in the same permuted order on both sides.
 // Outputs are dealt to lanes in pairs, so that a lane ends with two neighbours to store.
 #include <algorithm>
+#include <type_traits>
 
 #include "layers.hpp"
 #include "vec.hpp"
@@ -27,7 +28,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kXcds = 8;
-constexpr uint32_t kNowhere = 0x7FFFFFF0u;  // an offset that every range check drops
 
 struct Tiling {
   uint32_t nk, nn;        // tiles along features and outputs
@@ -37,114 +37,141 @@ struct Tiling {
   uint64_t bias_stride;
 };
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(uint64_t base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, int(bytes), kRawBuffer);
+// A byte of a word as a number.  One instruction; written down, because the compiler otherwise makes vectors of shifts
+// out of a row of them, which takes twice the instructions and more registers than there are.
+__device__ __forceinline__ float signed_byte(uint32_t word, int n) {
+  float f;
+  switch (n) {
+    case 0: asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(word)); break;
+    case 1: asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(word)); break;
+    case 2: asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(word)); break;
+    default: asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(word));
+  }
+  return f;
 }
 
-// WK x WN wavefronts, each with FK * 32 features and TB * 64 outputs.  ODD: bf16 rows of dy start on odd
-// elements or end in the middle of a pair, so elements are loaded one by one.
-template <int WK, int WN, int FK, bool DY_BF16, bool OUT_BF16, bool ODD>
-__global__ void __launch_bounds__(WK * WN * 64, 2) k_weight_gradient(WeightGradientArgs a, Tiling t) {
-  constexpr int TB = WK / 2, TK = WK * FK * 32, TN = WN * TB * 64, THREADS = WK * WN * 64;
-  static_assert(TN * 2 == THREADS, "each lane brings eight tokens of two outputs per step");
+// How bf16 rows of dy are loaded, two outputs at a time.  kPairs: an even number of outputs.  kShift: an odd number; the lane
+// whose pair would reach behind the row takes the pair before and shifts.  kSingle: one output, loaded as such.  (Rows may
+// start on any element.)
+enum Load { kPairs, kShift, kSingle };
+
+// WK x WN wavefronts, each with FK * 32 features and TB * 64 outputs.
+template <int WK, int WN, int FK, int TB, int OCCUPANCY, bool DY_BF16, bool OUT_BF16, Load LOAD>
+__global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(WeightGradientArgs a, Tiling t) {
+  constexpr int TK = WK * FK * 32, TN = WN * TB * 64, THREADS = WK * WN * 64;
+  // a task is eight tokens of two outputs of dy; a lane has TASKS of them per block
+  constexpr int TASKS = 2 * TN / THREADS, OCTETS = 4 / TASKS;
+  static_assert(TASKS * THREADS == 2 * TN && OCTETS * TASKS == 4, "the lanes share a block of dy evenly");
   constexpr int P = DY_BF16 ? 1 : 3, ES = DY_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4;
-  __shared__ u32x4 lds[2][P][4][TN];
+  __shared__ u32x4 lds[3][P][4][TN];
 
   // workgroups go round robin over the XCDs: each XCD gets a contiguous range of tiles, so that the tiles that
   // share dy and x share an L2
   const uint32_t xcd = blockIdx.x % kXcds, per = t.total / kXcds, more = t.total % kXcds;
   uint32_t tile = xcd * per + min(xcd, more) + blockIdx.x / kXcds;
   const uint32_t tiles = t.nk * t.nn;
-  const uint32_t w = tile / (tiles * t.splits);
+  const uint32_t w = uniform(tile / (tiles * t.splits));
   tile -= w * tiles * t.splits;
-  const uint32_t split = tile / tiles;
+  const uint32_t split = uniform(tile / tiles);
   tile -= split * tiles;
   // bands of four tiles along the features
-  const uint32_t band = tile / (4 * t.nn), in_band = tile - band * 4 * t.nn;
+  const uint32_t band = uniform(tile / (4 * t.nn)), in_band = tile - band * 4 * t.nn;
   const uint32_t high = min(t.nk - band * 4, 4u);
-  const uint32_t kt = band * 4 + in_band % high, nt = in_band / high;
+  const uint32_t nt = uniform(in_band / high), kt = band * 4 + in_band - nt * high;
   const uint32_t k0 = kt * TK, n0 = nt * TN;
 
   const uint32_t M = a.w.tokens[w], K = a.features, N = a.outputs;
   const uint32_t blocks = (M + kCheckpointBlock - 1) / kCheckpointBlock;
   const uint32_t share = (blocks + t.splits - 1) / t.splits;
-  const uint32_t b0 = min(split * share, blocks), b1 = min(b0 + share, blocks);
+  const uint32_t b0 = uniform(min(split * share, blocks)), b1 = uniform(min(b0 + share, blocks));
 
-  const uint32_t tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const uint32_t tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
   const uint32_t wk = wave / WN, wn = wave % WN, l32 = lane % 32, half = lane / 32;
   const uint32_t octet = tid / (TN / 2), pair = tid % (TN / 2);
 
   const uint64_t codes = a.w.a[w], scales = codes + uint64_t(blocks) * K * kCheckpointBlock;
-  const uint64_t dy = a.w.b[w] + uint64_t(n0) * ES;
   const uint32_t row_bytes = uint32_t(a.dy_pitch) * ES;
-  const uint32_t dy_off = octet * 8 * row_bytes + pair * 2 * ES;
+  const uint32_t lead = n0 ? 2 : 0;  // outputs before the tile that kShift may reach back to
+  const bool last_pair = LOAD == kShift && n0 + pair * 2 + 1 == N;
+  const uint64_t dy = a.w.b[w] + uint64_t(n0 - lead) * ES;
+  const uint32_t dy_off = octet * 8 * row_bytes + (pair * 2 + lead - (last_pair ? 1 : 0)) * ES;
 
-  typedef uint32_t raw __attribute__((ext_vector_type(DY_BF16 ? 8 : 16)));
-  auto load_dy = [&](uint32_t b) {
-    const uint32_t rows = min(M - b * kCheckpointBlock, kCheckpointBlock);
-    const __amdgpu_buffer_rsrc_t r = buffer(dy + uint64_t(b) * kCheckpointBlock * row_bytes, (rows - 1) * row_bytes + (N - n0) * ES);
-    raw v;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int off = int(dy_off + j * row_bytes);
-      if constexpr (!DY_BF16) {
-        const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
-        v[2 * j] = x[0];
-        v[2 * j + 1] = x[1];
-      } else if constexpr (ODD) {
-        v[j] = uint32_t(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0)) |
-               uint32_t(__builtin_amdgcn_raw_buffer_load_b16(r, off + 2, 0, 0)) << 16;
-      } else {
-        v[j] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
-      }
+  typedef uint32_t task __attribute__((ext_vector_type(DY_BF16 ? 8 : 16)));
+  struct raw {
+    task v[TASKS];
+  };
+  // Behind the last block, loads are made as well, of an empty stretch: they give zeros and fetch nothing.  (A branch around
+  // them would make the compiler wait for all loads where the ways meet.)
+  const uint32_t end_token = uniform(min(M, b1 * kCheckpointBlock)), behind = row_bytes - (N - n0 + lead) * ES;
+  auto dy_block = [&](uint32_t b) {
+    const uint32_t rows = min(end_token - min(b * kCheckpointBlock, end_token), kCheckpointBlock);
+    return buffer(dy + uint64_t(b) * kCheckpointBlock * row_bytes, max(int(rows * row_bytes - behind), 0));
+  };
+  auto load_row = [&](__amdgpu_buffer_rsrc_t r, raw& v, int n) {  // n: 0 to 8 * TASKS - 1
+    const int i = n / 8, j = n % 8, off = int(dy_off + (i * OCTETS * 8 + j) * row_bytes);
+    if constexpr (!DY_BF16) {
+      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+      v.v[i][2 * j] = x[0];
+      v.v[i][2 * j + 1] = x[1];
+    } else if constexpr (LOAD == kSingle) {
+      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
+    } else {
+      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
     }
+  };
+  auto load_dy = [&](uint32_t b) {
+    raw v;
+    const __amdgpu_buffer_rsrc_t r = dy_block(b);
+#pragma unroll
+    for (int n = 0; n < 8 * TASKS; ++n) load_row(r, v, n);
     return v;
   };
 
+  // dy goes to LDS as operands, eight tokens of an output to a piece; and is summed where the bias is due.
   const bool sums_dy = a.has_bias && kt == 0;
   float bias[2] = {0.0f, 0.0f};
-  auto keep_dy = [&](const raw& v, int buf) {
+  constexpr int kPacks = 2 * TASKS * (DY_BF16 ? 1 : 4);
+  u32x4 parts[P];  // fp32: of the output that is being packed
+  auto pack = [&](raw& v, uint32_t buf, int n, auto with_bias) {  // n: 0 to kPacks - 1
+    const int i = DY_BF16 ? n : n / 4, odd = i % 2;
+    task& in = v.v[i / 2];
+    u32x4* const to = &lds[buf][0][octet + i / 2 * OCTETS][odd * (TN / 2) + pair];
+    if constexpr (DY_BF16) {
+      if constexpr (LOAD == kShift)
+        if (!odd) in >>= last_pair ? 16u : 0u;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if constexpr (DY_BF16) {
-        u32x4 y;
+      for (int d = 0; d < 4; ++d) parts[0][d] = __builtin_amdgcn_perm(in[2 * d + 1], in[2 * d], odd ? 0x07060302u : 0x05040100u);
+      *to = parts[0];
+      if constexpr (with_bias)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) y[d] = __builtin_amdgcn_perm(v[2 * d + 1], v[2 * d], i ? 0x07060302u : 0x05040100u);
-        lds[buf][0][octet][i * (TN / 2) + pair] = y;
-      } else {
-        // v = hi + mid + lo: the upper half of a float is a bf16 number, and the rest is exact
-        u32x4 y[3];
+        for (int j = 0; j < 8; ++j) bias[odd] += odd ? bf16_high(in[j]) : bf16_low(in[j]);
+    } else {
+      // v = hi + mid + lo: the upper half of a float is a bf16 number, and the rest is exact
+      const int d = n % 4;
+      uint32_t part[3][2];
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          uint32_t part[3][2];
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t bits = in[2 * (2 * d + e) + odd];
+        const float x = as_float(bits), hi = bf16_high(bits);
+        const float rest = x == hi ? 0.0f : x - hi;  // an infinity is all in its upper half
+        const float mid = bf16_high(as_bits(rest));
+        part[0][e] = bits;
+        part[1][e] = as_bits(rest);
+        part[2][e] = as_bits(rest - mid);
+        if constexpr (with_bias) bias[odd] += x;
+      }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t bits = v[2 * (2 * d + e) + i];
-            const float x = as_float(bits), hi = bf16_high(bits);
-            const float rest = x == hi ? 0.0f : x - hi;  // an infinity is all in its upper half
-            const float mid = bf16_high(as_bits(rest));
-            part[0][e] = bits;
-            part[1][e] = as_bits(rest);
-            part[2][e] = as_bits(rest - mid);
-          }
-#pragma unroll
-          for (int p = 0; p < 3; ++p) y[p][d] = __builtin_amdgcn_perm(part[p][1], part[p][0], 0x07060302u);
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) lds[buf][p][octet][i * (TN / 2) + pair] = y[p];
+      for (int p = 0; p < 3; ++p) {
+        parts[p][d] = __builtin_amdgcn_perm(part[p][1], part[p][0], 0x07060302u);
+        if (d == 3) to[p * 4 * TN] = parts[p];
       }
     }
-    if (sums_dy) {
+  };
+  auto pack_all = [&](raw& v, uint32_t buf) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (DY_BF16) {
-          bias[0] += bf16_low(v[j]);
-          bias[1] += bf16_high(v[j]);
-        } else {
-          bias[0] += as_float(v[2 * j]);
-          bias[1] += as_float(v[2 * j + 1]);
-        }
-      }
+    for (int n = 0; n < kPacks; ++n) {
+      if (sums_dy) pack(v, buf, n, std::true_type{});
+      else pack(v, buf, n, std::false_type{});
     }
   };
 
@@ -152,16 +179,17 @@ __global__ void __launch_bounds__(WK * WN * 64, 2) k_weight_gradient(WeightGradi
     u32x4 q[FK];
     uint32_t s[FK];
   };
+  auto load_codes = [&](Codes& c, uint32_t b, int f) {
+    const __amdgpu_buffer_rsrc_t rq = buffer(codes + (uint64_t(b) * K + k0) * kCheckpointBlock, b < b1 ? (K - k0) * kCheckpointBlock : 0);
+    const __amdgpu_buffer_rsrc_t rs = buffer(scales + uint64_t(b) * K + k0, b < b1 ? K - k0 : 0);
+    const uint32_t k = (wk * FK + f) * 32 + l32;
+    c.q[f] = __builtin_amdgcn_raw_buffer_load_b128(rq, int(k * kCheckpointBlock + half * 16), 0, 0);
+    c.s[f] = __builtin_amdgcn_raw_buffer_load_b8(rs, int(k), 0, 0);
+  };
   auto load_x = [&](uint32_t b) {
     Codes c;
-    const __amdgpu_buffer_rsrc_t rq = buffer(codes + (uint64_t(b) * K + k0) * kCheckpointBlock, (K - k0) * kCheckpointBlock);
-    const __amdgpu_buffer_rsrc_t rs = buffer(scales + uint64_t(b) * K + k0, K - k0);
 #pragma unroll
-    for (int f = 0; f < FK; ++f) {
-      const uint32_t k = (wk * FK + f) * 32 + l32;
-      c.q[f] = __builtin_amdgcn_raw_buffer_load_b128(rq, int(k * kCheckpointBlock + half * 16), 0, 0);
-      c.s[f] = __builtin_amdgcn_raw_buffer_load_b8(rs, int(k), 0, 0);
-    }
+    for (int f = 0; f < FK; ++f) load_codes(c, b, f);
     return c;
   };
 
@@ -173,103 +201,161 @@ __global__ void __launch_bounds__(WK * WN * 64, 2) k_weight_gradient(WeightGradi
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[f][c][r] = 0.0f;
 
-  if (b0 < b1) {
-    raw next = load_dy(b0);
-    Codes x = load_x(b0);
-    keep_dy(next, 0);
-    if (b0 + 1 < b1) next = load_dy(b0 + 1);
-    int buf = 0;
-    for (uint32_t b = b0; b < b1; ++b) {
-      __syncthreads();
-      bf16x8 xs[FK][2];
+  // x as operands: FK * 32 features times two steps of 16 tokens, widened from the codes four bytes to two at a time
+  struct Widened {
+    u32x4 v[FK][2];
+  };
+  constexpr int kWidens = FK * 8;
+  auto widen = [&](const Codes& x, Widened& to, int n) {  // n: 0 to kWidens - 1
+    const int f = n / 8, s = n / 4 % 2, d = n % 4;
+    const float size = as_float(x.s[f] == 255u ? 0x7FC00000u : x.s[f] << 23);
+    uint32_t v[2];
 #pragma unroll
-      for (int f = 0; f < FK; ++f) {
-        const float size = as_float(x.s[f] == 255u ? 0x7FC00000u : x.s[f] << 23);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          u32x4 y;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            uint32_t v[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int byte = s * 8 + d * 2 + e;
-              v[e] = as_bits(float(int8_t(x.q[f][byte / 4] >> (8 * (byte % 4)))) * size);
-            }
-            y[d] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
-          }
-          xs[f][s] = __builtin_bit_cast(bf16x8, y);
-        }
-      }
-      if (b + 1 < b1) x = load_x(b + 1);
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int p = P - 1; p >= 0; --p)
-#pragma unroll
-          for (int c = 0; c < TB * 2; ++c) {
-            const uint32_t slot = (c % 2) * (TN / 2) + (wn * TB + c / 2) * 32 + l32;
-            const bf16x8 y = __builtin_bit_cast(bf16x8, lds[buf][p][half * 2 + s][slot]);
-#pragma unroll
-            for (int f = 0; f < FK; ++f) acc[f][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xs[f][s], y, acc[f][c], 0, 0, 0);
-          }
-      if (b + 1 < b1) {
-        keep_dy(next, buf ^ 1);
-        if (b + 2 < b1) next = load_dy(b + 2);
-      }
-      buf ^= 1;
+    for (int e = 0; e < 2; ++e) {
+      const int byte = s * 8 + d * 2 + e;
+      v[e] = as_bits(signed_byte(x.q[f][byte / 4], byte % 4) * size);
     }
+    to.v[f][s][d] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
+  };
+
+  // The products of a block, in the order in which they are made: two steps of 16 tokens, the parts of dy from the smallest
+  // on, the wavefront's outputs.
+  constexpr int kSlots = 2 * P * TB * 2, kDepth = 4;
+  auto read = [&](uint32_t buf, int slot) {
+    const int c = slot % (TB * 2), p = P - 1 - slot / (TB * 2) % P, s = slot / (TB * 2 * P);
+    return __builtin_bit_cast(bf16x8, lds[buf][p][half * 2 + s][(c % 2) * (TN / 2) + (wn * TB + c / 2) * 32 + l32]);
+  };
+
+  if (b0 < b1) {
+    raw y[2];
+    Codes x[2];
+    Widened xs[2];
+    y[0] = load_dy(b0);
+    x[0] = load_x(b0);
+    y[1] = load_dy(b0 + 1);
+    x[1] = load_x(b0 + 1);
+    pack_all(y[0], 0);
+    y[0] = load_dy(b0 + 2);
+#pragma unroll
+    for (int n = 0; n < kWidens; ++n) widen(x[0], xs[0], n);
+    x[0] = load_x(b0 + 2);
+    pack_all(y[1], 1);
+    y[1] = load_dy(b0 + 3);
+    __syncthreads();
+    bf16x8 ahead[kDepth];
+#pragma unroll
+    for (int q = 0; q < kDepth; ++q) ahead[q] = read(0, q);
+    uint32_t buf = 0, next = 1, write = 2;
+    // Block b is multiplied while x of block b + 1 is widened, dy of block b + 2 goes to LDS, and x of block b + 3 and dy of block
+    // b + 4 are fetched.  The order of the instructions is laid down: a few others after every product, which run in its shadow.
+    // A wavefront issues in order, so a row of loads, or of conversions, would hold up the products behind it.
+    constexpr int kLoads = 8 * TASKS, kPieces = kPacks + kLoads + kWidens + FK;
+    auto turn = [&](uint32_t b, Widened& now, Widened& then, Codes& x_in, raw& dy_in, auto with_bias) {
+      const __amdgpu_buffer_rsrc_t r = dy_block(b + 4);
+      auto piece = [&](int n) {
+        if (n < kPacks) return pack(dy_in, write, n, with_bias);
+        n -= kPacks;
+        if (n < kLoads + kWidens) {  // in turn, while there are both
+          constexpr int kBoth = kLoads < kWidens ? kLoads : kWidens;
+          const bool load = n < 2 * kBoth ? n % 2 == 0 : kLoads > kWidens;
+          const int at = n < 2 * kBoth ? n / 2 : n - kBoth;
+          return load ? load_row(r, dy_in, at) : widen(x_in, then, at);
+        }
+        return load_codes(x_in, b + 3, n - kLoads - kWidens);
+      };
+#pragma unroll
+      for (int q = 0; q < kSlots; ++q) {
+        const bf16x8 o = ahead[q % kDepth];
+#pragma unroll
+        for (int f = 0; f < FK; ++f)
+          acc[f][q % (TB * 2)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, now.v[f][q / (kSlots / 2)]), o,
+                                                                        acc[f][q % (TB * 2)], 0, 0, 0);
+        ahead[q % kDepth] = q + kDepth < kSlots ? read(buf, q + kDepth) : read(next, q + kDepth - kSlots);
+#pragma unroll
+        for (int n = q * kPieces / kSlots; n < (q + 1) * kPieces / kSlots; ++n) piece(n);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __syncthreads();
+      const uint32_t free = buf;
+      buf = next;
+      next = write;
+      write = free;
+    };
+    auto walk = [&](auto with_bias) {
+      for (uint32_t b = b0; b < b1; b += 2) {  // after an odd last block, one of zeros
+        turn(b, xs[0], xs[1], x[1], y[0], with_bias);
+        turn(b + 1, xs[1], xs[0], x[0], y[1], with_bias);
+      }
+    };
+    if (sums_dy) walk(std::true_type{});
+    else walk(std::false_type{});
   }
 
   // a lane holds outputs n, n + 1 of features 8 (r / 4) + 4 half + r % 4
   const uint64_t out = a.w.c[w] + split * t.split_stride + (uint64_t(k0) * N + n0) * OS;
   const uint32_t out_row = N * OS;
   const __amdgpu_buffer_rsrc_t ro = buffer(out, (min(K - k0, uint32_t(TK)) * N - n0) * OS);
-  const bool pairs = N % 2 == 0;
 #pragma unroll
   for (int f = 0; f < FK; ++f)
 #pragma unroll
     for (int c = 0; c < TB; ++c) {
       const uint32_t col = ((wn * TB + c) * 32 + l32) * 2;
       const uint32_t left = n0 + col < N ? N - n0 - col : 0;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const uint32_t row = (wk * FK + f) * 32 + 8 * (r / 4) + 4 * half + r % 4;
-        const uint32_t off = row * out_row + col * OS;
-        float y0 = acc[f][2 * c][r], y1 = acc[f][2 * c + 1][r];
-        // lanes behind the last output get an offset that the range check drops
-        const int at0 = int(left > 0 ? off : kNowhere), at1 = int(left > 1 ? off + OS : kNowhere);
-        if (pairs) {
-          if constexpr (OUT_BF16) {
-            if (a.accumulate) {
-              const uint32_t old = __builtin_amdgcn_raw_buffer_load_b32(ro, at0, 0, 0);
-              y0 += bf16_low(old);
-              y1 += bf16_high(old);
-            }
-            __builtin_amdgcn_raw_buffer_store_b32(bf16_pair(y0, y1), ro, at0, 0, 0);
-          } else {
-            if (a.accumulate) {
-              const u32x2 old = __builtin_amdgcn_raw_buffer_load_b64(ro, at0, 0, 0);
-              y0 += as_float(old[0]);
-              y1 += as_float(old[1]);
-            }
-            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{y0, y1}), ro, at0, 0, 0);
-          }
-        } else if constexpr (OUT_BF16) {
+      const uint32_t off = ((wk * FK + f) * 32 + 4 * half) * out_row + col * OS;
+      // lanes behind the last output get an offset that the range check drops
+      const uint32_t at0 = left > 0 ? off : kNowhere, at1 = left > 1 ? off + OS : kNowhere;
+      auto row = [&](int r) { return (8 * (r / 4) + r % 4) * out_row; };
+      f32x16 &y0 = acc[f][2 * c], &y1 = acc[f][2 * c + 1];
+      if (N % 2 == 0) {
+        if constexpr (OUT_BF16) {
           if (a.accumulate) {
-            y0 += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, at0, 0, 0)));
-            y1 += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, at1, 0, 0)));
+            uint32_t old[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b32(ro, int(at0 + row(r)), 0, 0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              y0[r] += bf16_low(old[r]);
+              y1[r] += bf16_high(old[r]);
+            }
           }
-          const uint32_t v = bf16_pair(y0, y1);
-          __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v), ro, at0, 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v >> 16), ro, at1, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) __builtin_amdgcn_raw_buffer_store_b32(bf16_pair(y0[r], y1[r]), ro, int(at0 + row(r)), 0, 0);
         } else {
           if (a.accumulate) {
-            y0 += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, at0, 0, 0));
-            y1 += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, at1, 0, 0));
+            u32x2 old[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b64(ro, int(at0 + row(r)), 0, 0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              y0[r] += as_float(old[r][0]);
+              y1[r] += as_float(old[r][1]);
+            }
           }
-          __builtin_amdgcn_raw_buffer_store_b32(as_bits(y0), ro, at0, 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b32(as_bits(y1), ro, at1, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            __builtin_amdgcn_raw_buffer_store_b64(u32x2{as_bits(y0[r]), as_bits(y1[r])}, ro, int(at0 + row(r)), 0, 0);
+        }
+      } else {
+        // rows start on any element: one by one
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int p0 = int(at0 + row(r)), p1 = int(at1 + row(r));
+          if constexpr (OUT_BF16) {
+            if (a.accumulate) {
+              y0[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p0, 0, 0)));
+              y1[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p1, 0, 0)));
+            }
+            const uint32_t v = bf16_pair(y0[r], y1[r]);
+            __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v), ro, p0, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v >> 16), ro, p1, 0, 0);
+          } else {
+            if (a.accumulate) {
+              y0[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p0, 0, 0));
+              y1[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p1, 0, 0));
+            }
+            __builtin_amdgcn_raw_buffer_store_b32(as_bits(y0[r]), ro, p0, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b32(as_bits(y1[r]), ro, p1, 0, 0);
+          }
         }
       }
     }
@@ -281,7 +367,9 @@ __global__ void __launch_bounds__(WK * WN * 64, 2) k_weight_gradient(WeightGradi
     part[octet * TN + pair * 2 + 1] = bias[1];
     __syncthreads();
     if (tid < TN && n0 + tid < N) {
-      float y = ((part[tid] + part[TN + tid]) + part[2 * TN + tid]) + part[3 * TN + tid];
+      float y = part[tid];
+#pragma unroll
+      for (int o = 1; o < OCTETS; ++o) y += part[o * TN + tid];
       const uint64_t at = a.bias[w] + split * t.bias_stride + uint64_t(n0 + tid) * OS;
       if (a.accumulate) {
         float old;
@@ -350,31 +438,29 @@ struct Shape {
 Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_tokens) {
   auto tiles = [&](uint32_t side) { return uint64_t(world) * ((features + side - 1) / side) * ((outputs + side - 1) / side); };
   const uint32_t blocks = uint32_t(checkpoint_blocks(max_tokens));
-  if (tiles(256) >= 192 && blocks >= 8) return {true, 1};
+  if (tiles(256) >= 192 && blocks >= 8 && outputs > 1) return {true, 1};
   const uint64_t want = (512 + tiles(128) - 1) / tiles(128);
   return {false, uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(want, blocks / 8)))};
 }
 
 uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
 
-template <int WK, int WN, int FK>
+template <int WK, int WN, int FK, int TB, int OCCUPANCY>
 hipError_t launch(const WeightGradientArgs& a, const Tiling& t, bool out_bf16, hipStream_t s) {
   const dim3 grid(t.total), block(WK * WN * 64);
-  // pairs of bf16 outputs are loaded together where every row starts and ends on a pair
-  bool odd = a.dy_pitch % 2 || a.outputs % 2;
-  for (uint32_t w = 0; w < a.world; ++w) odd = odd || a.w.b[w] % 4;
-#define CARAMEL_WG(DY, OUT, ODD) hipLaunchKernelGGL((k_weight_gradient<WK, WN, FK, DY, OUT, ODD>), grid, block, 0, s, a, t)
-  if (a.dy_bf16) {
-    if (odd) {
-      if (out_bf16) CARAMEL_WG(true, true, true);
-      else CARAMEL_WG(true, false, true);
-    } else {
-      if (out_bf16) CARAMEL_WG(true, true, false);
-      else CARAMEL_WG(true, false, false);
-    }
-  } else {
-    if (out_bf16) CARAMEL_WG(false, true, false);
-    else CARAMEL_WG(false, false, false);
+#define CARAMEL_WG(DY, OUT, LOAD) hipLaunchKernelGGL((k_weight_gradient<WK, WN, FK, TB, OCCUPANCY, DY, OUT, LOAD>), grid, block, 0, s, a, t)
+  if (!a.dy_bf16) {
+    if (out_bf16) CARAMEL_WG(false, true, kPairs);
+    else CARAMEL_WG(false, false, kPairs);
+  } else if (a.outputs % 2 == 0) {
+    if (out_bf16) CARAMEL_WG(true, true, kPairs);
+    else CARAMEL_WG(true, false, kPairs);
+  } else if (a.outputs > 1) {
+    if (out_bf16) CARAMEL_WG(true, true, kShift);
+    else CARAMEL_WG(true, false, kShift);
+  } else if constexpr (WK == 2) {  // one output is never worth the large tile
+    if (out_bf16) CARAMEL_WG(true, true, kSingle);
+    else CARAMEL_WG(true, false, kSingle);
   }
 #undef CARAMEL_WG
   return hipGetLastError();
@@ -397,7 +483,7 @@ hipError_t launch_weight_gradient(const WeightGradientArgs& a, hipStream_t s) {
   t.nn = (a.outputs + side - 1) / side;
   t.splits = c.splits;
   t.total = t.nk * t.nn * t.splits * a.world;
-  if (c.splits == 1) return c.large ? launch<4, 2, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2>(a, t, a.out_bf16, s);
+  if (c.splits == 1) return c.large ? launch<8, 1, 1, 4, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2, 1, 2>(a, t, a.out_bf16, s);
 
   t.split_stride = up256(uint64_t(a.features) * a.outputs * 4);
   t.bias_stride = up256(uint64_t(a.outputs) * 4);
@@ -408,7 +494,7 @@ hipError_t launch_weight_gradient(const WeightGradientArgs& a, hipStream_t s) {
     p.w.c[w] = parts + w * t.splits * t.split_stride;
     p.bias[w] = bias_parts + w * t.splits * t.bias_stride;
   }
-  const hipError_t e = c.large ? launch<4, 2, 2>(p, t, false, s) : launch<2, 2, 2>(p, t, false, s);
+  const hipError_t e = c.large ? launch<8, 1, 1, 4, 2>(p, t, false, s) : launch<2, 2, 2, 1, 2>(p, t, false, s);
   if (e != hipSuccess) return e;
   const uint64_t vecs = (uint64_t(a.features) * a.outputs + 3) / 4 + (a.has_bias ? (a.outputs + 3) / 4 : 0);
   const dim3 grid(uint32_t((vecs + 255) / 256), a.world);
