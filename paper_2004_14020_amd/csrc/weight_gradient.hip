@@ -55,6 +55,190 @@ __device__ __forceinline__ float signed_byte(uint32_t word, int n) {
 // start on any element.)
 enum Load { kPairs, kShift, kSingle };
 
+// The rows of dy of one workgroup: TN outputs, brought in by its lanes 32 tokens at a time.  A task is eight tokens of two
+// outputs; a lane has TASKS of them.
+template <bool BF16, Load LOAD, int TN, int TASKS>
+struct Dy {
+  static constexpr int ES = BF16 ? 2 : 4, P = BF16 ? 1 : 3, kOctets = 4 / TASKS;
+  static constexpr int kPacks = 2 * TASKS * (BF16 ? 1 : 4);
+  typedef uint32_t task __attribute__((ext_vector_type(BF16 ? 8 : 16)));
+  struct raw {
+    task v[TASKS];
+  };
+  uint64_t base;
+  uint32_t row_bytes, behind, end_token, off, octet, pair;
+  bool last_pair;
+  float bias[2] = {0.0f, 0.0f};  // sums of this lane's two outputs
+  u32x4 parts[P];                // of the output that is being packed
+
+  __device__ __forceinline__ Dy(const WeightGradientArgs& a, uint32_t w, uint32_t n0, uint32_t end, uint32_t tid) {
+    const uint32_t lead = n0 ? 2 : 0;  // outputs before the tile that kShift may reach back to
+    octet = tid / (TN / 2);
+    pair = tid % (TN / 2);
+    end_token = uniform(end);
+    row_bytes = uint32_t(a.dy_pitch) * ES;
+    behind = row_bytes - (a.outputs - n0 + lead) * ES;
+    base = a.w.b[w] + uint64_t(n0 - lead) * ES;
+    last_pair = LOAD == kShift && n0 + pair * 2 + 1 == a.outputs;
+    off = octet * 8 * row_bytes + (pair * 2 + lead - (last_pair ? 1 : 0)) * ES;
+  }
+  // A block's memory.  Behind the last block, loads are made as well, of an empty stretch: they give zeros and fetch nothing.
+  // (A branch around them would make the compiler wait for all loads where the ways meet.)
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t block(uint32_t b) const {
+    const uint32_t rows = min(end_token - min(b * kCheckpointBlock, end_token), kCheckpointBlock);
+    return buffer(base + uint64_t(b) * kCheckpointBlock * row_bytes, max(int(rows * row_bytes - behind), 0));
+  }
+  __device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t r, raw& v, int n) const {  // n: 0 to 8 * TASKS - 1
+    const int i = n / 8, j = n % 8, at = int(off + (i * kOctets * 8 + j) * row_bytes);
+    if constexpr (!BF16) {
+      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
+      v.v[i][2 * j] = x[0];
+      v.v[i][2 * j + 1] = x[1];
+    } else if constexpr (LOAD == kSingle) {
+      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+    } else {
+      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+    }
+  }
+  __device__ __forceinline__ raw load(uint32_t b) const {
+    raw v;
+    const __amdgpu_buffer_rsrc_t r = block(b);
+#pragma unroll
+    for (int n = 0; n < 8 * TASKS; ++n) load_row(r, v, n);
+    return v;
+  }
+  // To LDS as operands, eight tokens of an output to a piece, and into the sums where the bias is due; in kPacks steps.
+  template <typename BIAS>
+  __device__ __forceinline__ void pack(raw& v, u32x4 (*lds)[4][TN], int n, BIAS) {
+    const int i = BF16 ? n : n / 4, odd = i % 2;
+    task& in = v.v[i / 2];
+    u32x4* const to = &lds[0][octet + i / 2 * kOctets][odd * (TN / 2) + pair];
+    if constexpr (BF16) {
+      if constexpr (LOAD == kShift)
+        if (!odd) in >>= last_pair ? 16u : 0u;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) parts[0][d] = __builtin_amdgcn_perm(in[2 * d + 1], in[2 * d], odd ? 0x07060302u : 0x05040100u);
+      *to = parts[0];
+      if constexpr (BIAS::value)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bias[odd] += odd ? bf16_high(in[j]) : bf16_low(in[j]);
+    } else {
+      // v = hi + mid + lo: the upper half of a float is a bf16 number, and the rest is exact
+      const int d = n % 4;
+      uint32_t part[3][2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t bits = in[2 * (2 * d + e) + odd];
+        const float x = as_float(bits), hi = bf16_high(bits);
+        const float rest = x == hi ? 0.0f : x - hi;  // an infinity is all in its upper half
+        const float mid = bf16_high(as_bits(rest));
+        part[0][e] = bits;
+        part[1][e] = as_bits(rest);
+        part[2][e] = as_bits(rest - mid);
+        if constexpr (BIAS::value) bias[odd] += x;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        parts[p][d] = __builtin_amdgcn_perm(part[p][1], part[p][0], 0x07060302u);
+        if (d == 3) to[p * 4 * TN] = parts[p];
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ float scale_of(uint32_t byte) { return as_float(byte == 255u ? 0x7FC00000u : byte << 23); }
+
+// Two codes of a word (the lower or the upper ones) as a pair of bf16 numbers: eight bits times a power of two, nothing to round.
+__device__ __forceinline__ uint32_t widen_two(uint32_t codes, int upper, float scale) {
+  const uint32_t lo = as_bits(signed_byte(codes, 2 * upper) * scale), hi = as_bits(signed_byte(codes, 2 * upper + 1) * scale);
+  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+
+// 32 features of this lane's outputs n (y0) and n + 1 (y1): a lane of the first half holds features 8 (r / 4) + r % 4, one of the
+// second half those 4 further on.  off: of the first of them; left: outputs from n on; even: every row starts on a pair.
+// AUX: cache policy of the stores (2: streaming).
+template <bool OUT_BF16, int AUX>
+__device__ __forceinline__ void write_strip(__amdgpu_buffer_rsrc_t ro, uint32_t off, uint32_t left, uint32_t out_row, bool even,
+                                            bool accumulate, f32x16 y0, f32x16 y1) {
+  constexpr int OS = OUT_BF16 ? 2 : 4;
+  // lanes behind the last output get an offset that the range check drops
+  const uint32_t at0 = left > 0 ? off : kNowhere, at1 = left > 1 ? off + OS : kNowhere;
+  auto row = [&](int r) { return (8 * (r / 4) + r % 4) * out_row; };
+  if (even) {
+    if constexpr (OUT_BF16) {
+      if (accumulate) {
+        uint32_t old[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b32(ro, int(at0 + row(r)), 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          y0[r] += bf16_low(old[r]);
+          y1[r] += bf16_high(old[r]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) __builtin_amdgcn_raw_buffer_store_b32(bf16_pair(y0[r], y1[r]), ro, int(at0 + row(r)), 0, AUX);
+    } else {
+      if (accumulate) {
+        u32x2 old[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b64(ro, int(at0 + row(r)), 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          y0[r] += as_float(old[r][0]);
+          y1[r] += as_float(old[r][1]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{as_bits(y0[r]), as_bits(y1[r])}, ro, int(at0 + row(r)), 0, AUX);
+    }
+  } else {
+    // rows start on any element: one by one
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int p0 = int(at0 + row(r)), p1 = int(at1 + row(r));
+      if constexpr (OUT_BF16) {
+        if (accumulate) {
+          y0[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p0, 0, 0)));
+          y1[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p1, 0, 0)));
+        }
+        const uint32_t v = bf16_pair(y0[r], y1[r]);
+        __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v), ro, p0, 0, AUX);
+        __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v >> 16), ro, p1, 0, AUX);
+      } else {
+        if (accumulate) {
+          y0[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p0, 0, 0));
+          y1[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p1, 0, 0));
+        }
+        __builtin_amdgcn_raw_buffer_store_b32(as_bits(y0[r]), ro, p0, 0, AUX);
+        __builtin_amdgcn_raw_buffer_store_b32(as_bits(y1[r]), ro, p1, 0, AUX);
+      }
+    }
+  }
+}
+
+// The bias of a workgroup's outputs from its lanes' sums; LDS has to be free.
+template <bool OUT_BF16, int TN, int OCTETS>
+__device__ __forceinline__ void write_bias(const WeightGradientArgs& a, float* part, uint32_t tid, uint32_t n0, uint64_t to,
+                                           uint32_t octet, uint32_t pair, const float* sums) {
+  constexpr int OS = OUT_BF16 ? 2 : 4;
+  part[octet * TN + pair * 2] = sums[0];
+  part[octet * TN + pair * 2 + 1] = sums[1];
+  __syncthreads();
+  if (tid >= TN || n0 + tid >= a.outputs) return;
+  float y = part[tid];
+#pragma unroll
+  for (int o = 1; o < OCTETS; ++o) y += part[o * TN + tid];
+  const uint64_t at = to + uint64_t(n0 + tid) * OS;
+  if (a.accumulate) {
+    float old;
+    load_elems<OUT_BF16, 1>(at, &old);
+    y += old;
+  }
+  store_elems<OUT_BF16, 1>(at, &y);
+}
+
 // WK x WN wavefronts, each with FK * 32 features and TB * 64 outputs.
 template <int WK, int WN, int FK, int TB, int OCCUPANCY, bool DY_BF16, bool OUT_BF16, Load LOAD>
 __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(WeightGradientArgs a, Tiling t) {
@@ -62,7 +246,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
   // a task is eight tokens of two outputs of dy; a lane has TASKS of them per block
   constexpr int TASKS = 2 * TN / THREADS, OCTETS = 4 / TASKS;
   static_assert(TASKS * THREADS == 2 * TN && OCTETS * TASKS == 4, "the lanes share a block of dy evenly");
-  constexpr int P = DY_BF16 ? 1 : 3, ES = DY_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4;
+  constexpr int P = DY_BF16 ? 1 : 3, OS = OUT_BF16 ? 2 : 4;
   __shared__ u32x4 lds[3][P][4][TN];
 
   // workgroups go round robin over the XCDs: each XCD gets a contiguous range of tiles, so that the tiles that
@@ -87,86 +271,14 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
 
   const uint32_t tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
   const uint32_t wk = wave / WN, wn = wave % WN, l32 = lane % 32, half = lane / 32;
-  const uint32_t octet = tid / (TN / 2), pair = tid % (TN / 2);
 
   const uint64_t codes = a.w.a[w], scales = codes + uint64_t(blocks) * K * kCheckpointBlock;
-  const uint32_t row_bytes = uint32_t(a.dy_pitch) * ES;
-  const uint32_t lead = n0 ? 2 : 0;  // outputs before the tile that kShift may reach back to
-  const bool last_pair = LOAD == kShift && n0 + pair * 2 + 1 == N;
-  const uint64_t dy = a.w.b[w] + uint64_t(n0 - lead) * ES;
-  const uint32_t dy_off = octet * 8 * row_bytes + (pair * 2 + lead - (last_pair ? 1 : 0)) * ES;
-
-  typedef uint32_t task __attribute__((ext_vector_type(DY_BF16 ? 8 : 16)));
-  struct raw {
-    task v[TASKS];
-  };
-  // Behind the last block, loads are made as well, of an empty stretch: they give zeros and fetch nothing.  (A branch around
-  // them would make the compiler wait for all loads where the ways meet.)
-  const uint32_t end_token = uniform(min(M, b1 * kCheckpointBlock)), behind = row_bytes - (N - n0 + lead) * ES;
-  auto dy_block = [&](uint32_t b) {
-    const uint32_t rows = min(end_token - min(b * kCheckpointBlock, end_token), kCheckpointBlock);
-    return buffer(dy + uint64_t(b) * kCheckpointBlock * row_bytes, max(int(rows * row_bytes - behind), 0));
-  };
-  auto load_row = [&](__amdgpu_buffer_rsrc_t r, raw& v, int n) {  // n: 0 to 8 * TASKS - 1
-    const int i = n / 8, j = n % 8, off = int(dy_off + (i * OCTETS * 8 + j) * row_bytes);
-    if constexpr (!DY_BF16) {
-      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
-      v.v[i][2 * j] = x[0];
-      v.v[i][2 * j + 1] = x[1];
-    } else if constexpr (LOAD == kSingle) {
-      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
-    } else {
-      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
-    }
-  };
-  auto load_dy = [&](uint32_t b) {
-    raw v;
-    const __amdgpu_buffer_rsrc_t r = dy_block(b);
-#pragma unroll
-    for (int n = 0; n < 8 * TASKS; ++n) load_row(r, v, n);
-    return v;
-  };
-
-  // dy goes to LDS as operands, eight tokens of an output to a piece; and is summed where the bias is due.
+  typedef Dy<DY_BF16, LOAD, TN, TASKS> Rows;
+  typedef typename Rows::raw raw;
+  constexpr int kPacks = Rows::kPacks;
+  Rows dy(a, w, n0, min(M, b1 * kCheckpointBlock), tid);
   const bool sums_dy = a.has_bias && kt == 0;
-  float bias[2] = {0.0f, 0.0f};
-  constexpr int kPacks = 2 * TASKS * (DY_BF16 ? 1 : 4);
-  u32x4 parts[P];  // fp32: of the output that is being packed
-  auto pack = [&](raw& v, uint32_t buf, int n, auto with_bias) {  // n: 0 to kPacks - 1
-    const int i = DY_BF16 ? n : n / 4, odd = i % 2;
-    task& in = v.v[i / 2];
-    u32x4* const to = &lds[buf][0][octet + i / 2 * OCTETS][odd * (TN / 2) + pair];
-    if constexpr (DY_BF16) {
-      if constexpr (LOAD == kShift)
-        if (!odd) in >>= last_pair ? 16u : 0u;
-#pragma unroll
-      for (int d = 0; d < 4; ++d) parts[0][d] = __builtin_amdgcn_perm(in[2 * d + 1], in[2 * d], odd ? 0x07060302u : 0x05040100u);
-      *to = parts[0];
-      if constexpr (with_bias)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) bias[odd] += odd ? bf16_high(in[j]) : bf16_low(in[j]);
-    } else {
-      // v = hi + mid + lo: the upper half of a float is a bf16 number, and the rest is exact
-      const int d = n % 4;
-      uint32_t part[3][2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t bits = in[2 * (2 * d + e) + odd];
-        const float x = as_float(bits), hi = bf16_high(bits);
-        const float rest = x == hi ? 0.0f : x - hi;  // an infinity is all in its upper half
-        const float mid = bf16_high(as_bits(rest));
-        part[0][e] = bits;
-        part[1][e] = as_bits(rest);
-        part[2][e] = as_bits(rest - mid);
-        if constexpr (with_bias) bias[odd] += x;
-      }
-#pragma unroll
-      for (int p = 0; p < 3; ++p) {
-        parts[p][d] = __builtin_amdgcn_perm(part[p][1], part[p][0], 0x07060302u);
-        if (d == 3) to[p * 4 * TN] = parts[p];
-      }
-    }
-  };
+  auto pack = [&](raw& v, uint32_t buf, int n, auto with_bias) { dy.pack(v, lds[buf], n, with_bias); };
   auto pack_all = [&](raw& v, uint32_t buf) {
 #pragma unroll
     for (int n = 0; n < kPacks; ++n) {
@@ -208,14 +320,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
   constexpr int kWidens = FK * 8;
   auto widen = [&](const Codes& x, Widened& to, int n) {  // n: 0 to kWidens - 1
     const int f = n / 8, s = n / 4 % 2, d = n % 4;
-    const float size = as_float(x.s[f] == 255u ? 0x7FC00000u : x.s[f] << 23);
-    uint32_t v[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int byte = s * 8 + d * 2 + e;
-      v[e] = as_bits(signed_byte(x.q[f][byte / 4], byte % 4) * size);
-    }
-    to.v[f][s][d] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
+    to.v[f][s][d] = widen_two(x.q[f][s * 2 + d / 2], d % 2, scale_of(x.s[f]));
   };
 
   // The products of a block, in the order in which they are made: two steps of 16 tokens, the parts of dy from the smallest
@@ -227,31 +332,36 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
   };
 
   if (b0 < b1) {
-    raw y[2];
-    Codes x[2];
+    // A turn of fp32 takes three times as long: there, fetching one block ahead is enough, and registers are short.
+    constexpr int kSets = DY_BF16 ? 2 : 1;
+    raw y[kSets];
+    Codes x[kSets];
     Widened xs[2];
-    y[0] = load_dy(b0);
     x[0] = load_x(b0);
-    y[1] = load_dy(b0 + 1);
-    x[1] = load_x(b0 + 1);
-    pack_all(y[0], 0);
-    y[0] = load_dy(b0 + 2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (i == 0 || kSets == 1) y[0] = dy.load(b0 + i);
+      if (i == 0 && kSets == 2) y[1] = dy.load(b0 + 1);
+      pack_all(y[i % kSets], i);
+    }
 #pragma unroll
     for (int n = 0; n < kWidens; ++n) widen(x[0], xs[0], n);
-    x[0] = load_x(b0 + 2);
-    pack_all(y[1], 1);
-    y[1] = load_dy(b0 + 3);
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+      x[i] = load_x(b0 + 1 + i);
+      y[i] = dy.load(b0 + 2 + i);
+    }
     __syncthreads();
     bf16x8 ahead[kDepth];
 #pragma unroll
     for (int q = 0; q < kDepth; ++q) ahead[q] = read(0, q);
     uint32_t buf = 0, next = 1, write = 2;
-    // Block b is multiplied while x of block b + 1 is widened, dy of block b + 2 goes to LDS, and x of block b + 3 and dy of block
-    // b + 4 are fetched.  The order of the instructions is laid down: a few others after every product, which run in its shadow.
+    // Block b is multiplied while x of block b + 1 is widened, dy of block b + 2 goes to LDS, and x of block b + 1 + kSets and dy
+    // of block b + 2 + kSets are fetched.  The order of the instructions is laid down: a few others after every product, which run in its shadow.
     // A wavefront issues in order, so a row of loads, or of conversions, would hold up the products behind it.
     constexpr int kLoads = 8 * TASKS, kPieces = kPacks + kLoads + kWidens + FK;
     auto turn = [&](uint32_t b, Widened& now, Widened& then, Codes& x_in, raw& dy_in, auto with_bias) {
-      const __amdgpu_buffer_rsrc_t r = dy_block(b + 4);
+      const __amdgpu_buffer_rsrc_t r = dy.block(b + 2 + kSets);
       auto piece = [&](int n) {
         if (n < kPacks) return pack(dy_in, write, n, with_bias);
         n -= kPacks;
@@ -259,9 +369,9 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
           constexpr int kBoth = kLoads < kWidens ? kLoads : kWidens;
           const bool load = n < 2 * kBoth ? n % 2 == 0 : kLoads > kWidens;
           const int at = n < 2 * kBoth ? n / 2 : n - kBoth;
-          return load ? load_row(r, dy_in, at) : widen(x_in, then, at);
+          return load ? dy.load_row(r, dy_in, at) : widen(x_in, then, at);
         }
-        return load_codes(x_in, b + 3, n - kLoads - kWidens);
+        return load_codes(x_in, b + 1 + kSets, n - kLoads - kWidens);
       };
 #pragma unroll
       for (int q = 0; q < kSlots; ++q) {
@@ -283,8 +393,8 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
     };
     auto walk = [&](auto with_bias) {
       for (uint32_t b = b0; b < b1; b += 2) {  // after an odd last block, one of zeros
-        turn(b, xs[0], xs[1], x[1], y[0], with_bias);
-        turn(b + 1, xs[1], xs[0], x[0], y[1], with_bias);
+        turn(b, xs[0], xs[1], x[0], y[0], with_bias);
+        turn(b + 1, xs[1], xs[0], x[kSets - 1], y[kSets - 1], with_bias);
       }
     };
     if (sums_dy) walk(std::true_type{});
@@ -301,83 +411,99 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
     for (int c = 0; c < TB; ++c) {
       const uint32_t col = ((wn * TB + c) * 32 + l32) * 2;
       const uint32_t left = n0 + col < N ? N - n0 - col : 0;
-      const uint32_t off = ((wk * FK + f) * 32 + 4 * half) * out_row + col * OS;
-      // lanes behind the last output get an offset that the range check drops
-      const uint32_t at0 = left > 0 ? off : kNowhere, at1 = left > 1 ? off + OS : kNowhere;
-      auto row = [&](int r) { return (8 * (r / 4) + r % 4) * out_row; };
-      f32x16 &y0 = acc[f][2 * c], &y1 = acc[f][2 * c + 1];
-      if (N % 2 == 0) {
-        if constexpr (OUT_BF16) {
-          if (a.accumulate) {
-            uint32_t old[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b32(ro, int(at0 + row(r)), 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              y0[r] += bf16_low(old[r]);
-              y1[r] += bf16_high(old[r]);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) __builtin_amdgcn_raw_buffer_store_b32(bf16_pair(y0[r], y1[r]), ro, int(at0 + row(r)), 0, 0);
-        } else {
-          if (a.accumulate) {
-            u32x2 old[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b64(ro, int(at0 + row(r)), 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              y0[r] += as_float(old[r][0]);
-              y1[r] += as_float(old[r][1]);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            __builtin_amdgcn_raw_buffer_store_b64(u32x2{as_bits(y0[r]), as_bits(y1[r])}, ro, int(at0 + row(r)), 0, 0);
-        }
-      } else {
-        // rows start on any element: one by one
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int p0 = int(at0 + row(r)), p1 = int(at1 + row(r));
-          if constexpr (OUT_BF16) {
-            if (a.accumulate) {
-              y0[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p0, 0, 0)));
-              y1[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p1, 0, 0)));
-            }
-            const uint32_t v = bf16_pair(y0[r], y1[r]);
-            __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v), ro, p0, 0, 0);
-            __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v >> 16), ro, p1, 0, 0);
-          } else {
-            if (a.accumulate) {
-              y0[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p0, 0, 0));
-              y1[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p1, 0, 0));
-            }
-            __builtin_amdgcn_raw_buffer_store_b32(as_bits(y0[r]), ro, p0, 0, 0);
-            __builtin_amdgcn_raw_buffer_store_b32(as_bits(y1[r]), ro, p1, 0, 0);
-          }
-        }
-      }
+      write_strip<OUT_BF16, 0>(ro, ((wk * FK + f) * 32 + 4 * half) * out_row + col * OS, left, out_row, N % 2 == 0, a.accumulate,
+                            acc[f][2 * c], acc[f][2 * c + 1]);
     }
 
   if (sums_dy) {  // the same for all lanes of the workgroup
     __syncthreads();
-    float* const part = reinterpret_cast<float*>(lds);
-    part[octet * TN + pair * 2] = bias[0];
-    part[octet * TN + pair * 2 + 1] = bias[1];
-    __syncthreads();
-    if (tid < TN && n0 + tid < N) {
-      float y = part[tid];
+    write_bias<OUT_BF16, TN, OCTETS>(a, reinterpret_cast<float*>(lds), tid, n0, a.bias[w] + split * t.bias_stride, dy.octet, dy.pair,
+                                     dy.bias);
+  }
+}
+
+// Few tokens: what is written outweighs the product.  A workgroup keeps dy of all tokens in LDS, 128 outputs of it, and goes
+// along the features, each wavefront by itself, 32 features at a time: codes come in and sums go out without a barrier.
+struct ShortTiling {
+  uint32_t nn, share;  // tiles along the outputs; steps of 32 features per workgroup
+};
+
+template <int BLOCKS, bool DY_BF16, bool OUT_BF16, Load LOAD>
+__global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradientArgs a, ShortTiling t) {
+  constexpr int TN = 128, TB = 2, P = DY_BF16 ? 1 : 3, OS = OUT_BF16 ? 2 : 4;
+  __shared__ u32x4 lds[BLOCKS][P][4][TN];
+  const uint32_t w = blockIdx.y, part = uniform(blockIdx.x / t.nn), n0 = (blockIdx.x - part * t.nn) * TN;
+  const uint32_t M = a.w.tokens[w], K = a.features, N = a.outputs;
+  const uint32_t blocks = (M + kCheckpointBlock - 1) / kCheckpointBlock;
+  const uint32_t tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64), l32 = lane % 32, half = lane / 32;
+  const uint32_t steps = (K + 31) / 32, s1 = min((part + 1) * t.share, steps);
+  const uint64_t codes = a.w.a[w], scales = codes + uint64_t(blocks) * K * kCheckpointBlock;
+
+  struct Codes {
+    u32x4 q;
+    uint32_t s;
+  };
+  auto load_codes = [&](uint32_t step, uint32_t b) {
+    const bool there = step < s1 && b < blocks;
+    const uint64_t at = uint64_t(b) * K + step * 32;
+    Codes c;
+    c.q = __builtin_amdgcn_raw_buffer_load_b128(buffer(codes + at * kCheckpointBlock, there ? (K - step * 32) * kCheckpointBlock : 0),
+                                                int(l32 * kCheckpointBlock + half * 16), 0, 0);
+    c.s = __builtin_amdgcn_raw_buffer_load_b8(buffer(scales + at, there ? K - step * 32 : 0), int(l32), 0, 0);
+    return c;
+  };
+  uint32_t step = part * t.share + wave;
+  Codes next = load_codes(step, 0);
+
+  typedef Dy<DY_BF16, LOAD, TN, 1> Rows;
+  Rows dy(a, w, n0, M, tid);
+  const bool sums_dy = a.has_bias && part == 0;
+  typename Rows::raw v[BLOCKS];
 #pragma unroll
-      for (int o = 1; o < OCTETS; ++o) y += part[o * TN + tid];
-      const uint64_t at = a.bias[w] + split * t.bias_stride + uint64_t(n0 + tid) * OS;
-      if (a.accumulate) {
-        float old;
-        load_elems<OUT_BF16, 1>(at, &old);
-        y += old;
+  for (int b = 0; b < BLOCKS; ++b) v[b] = dy.load(b);
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int n = 0; n < Rows::kPacks; ++n) dy.pack(v[b], lds[b], n, std::true_type{});
+  __syncthreads();
+
+  for (; step < s1; step += 4) {
+    f32x16 acc[TB * 2];
+#pragma unroll
+    for (int c = 0; c < TB * 2; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[c][r] = 0.0f;
+    for (uint32_t b = 0; b < blocks; ++b) {
+      const Codes x = next;
+      const bool more = b + 1 < blocks;
+      next = load_codes(more ? step : step + 4, more ? b + 1 : 0);
+      const float size = scale_of(x.s);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 xs;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) xs[d] = widen_two(x.q[s * 2 + d / 2], d % 2, size);
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+          for (int c = 0; c < TB * 2; ++c) {
+            const u32x4 y = lds[b][p][half * 2 + s][(c % 2) * (TN / 2) + c / 2 * 32 + l32];
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xs), __builtin_bit_cast(bf16x8, y), acc[c], 0, 0, 0);
+          }
       }
-      store_elems<OUT_BF16, 1>(at, &y);
     }
+    const uint32_t k0 = step * 32, out_row = N * OS;
+    const __amdgpu_buffer_rsrc_t ro = buffer(a.w.c[w] + (uint64_t(k0) * N + n0) * OS, (min(K - k0, 32u) * N - n0) * OS);
+#pragma unroll
+    for (int c = 0; c < TB; ++c) {
+      const uint32_t col = (c * 32 + l32) * 2, left = n0 + col < N ? N - n0 - col : 0;
+      write_strip<OUT_BF16, 2>(ro, 4 * half * out_row + col * OS, left, out_row, N % 2 == 0, a.accumulate, acc[2 * c], acc[2 * c + 1]);
+    }
+  }
+
+  if (sums_dy) {
+    __syncthreads();
+    write_bias<OUT_BF16, TN, 4>(a, reinterpret_cast<float*>(lds), tid, n0, a.bias[w], dy.octet, dy.pair, dy.bias);
   }
 }
 
@@ -429,18 +555,20 @@ __global__ void __launch_bounds__(256) k_weight_join(WeightGradientArgs a, Tilin
   }
 }
 
-// Which tile, and in how many parts the tokens are summed.
+// Which kernel, and in how many parts the tokens are summed.
+enum Kernel { kShort, kSmallTile, kLargeTile };
 struct Shape {
-  bool large;  // 256 x 256 by eight wavefronts, or 128 x 128 by four
+  Kernel kernel;
   uint32_t splits;
 };
 
-Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_tokens) {
+Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_tokens, bool dy_bf16) {
   auto tiles = [&](uint32_t side) { return uint64_t(world) * ((features + side - 1) / side) * ((outputs + side - 1) / side); };
   const uint32_t blocks = uint32_t(checkpoint_blocks(max_tokens));
-  if (tiles(256) >= 192 && blocks >= 8 && outputs > 1) return {true, 1};
+  if (blocks <= (dy_bf16 ? 6u : 2u)) return {kShort, 1};
+  if (tiles(256) >= 192 && blocks >= 8 && outputs > 1) return {kLargeTile, 1};
   const uint64_t want = (512 + tiles(128) - 1) / tiles(128);
-  return {false, uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(want, blocks / 8)))};
+  return {kSmallTile, uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(want, blocks / 8)))};
 }
 
 uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
@@ -466,24 +594,54 @@ hipError_t launch(const WeightGradientArgs& a, const Tiling& t, bool out_bf16, h
   return hipGetLastError();
 }
 
+hipError_t launch_short(const WeightGradientArgs& a, hipStream_t s) {
+  ShortTiling t{};
+  t.nn = (a.outputs + 127) / 128;
+  const uint32_t steps = (a.features + 31) / 32;
+  const uint64_t tiles = uint64_t(t.nn) * a.world;
+  const uint32_t parts = uint32_t(std::min<uint64_t>((steps + 3) / 4, (512 + tiles - 1) / tiles));
+  t.share = (steps + parts - 1) / parts;
+  t.share = (t.share + 3) / 4 * 4;
+  const dim3 grid(t.nn * ((steps + t.share - 1) / t.share), a.world), block(256);
+#define CARAMEL_WG(BLOCKS, DY, OUT, LOAD) hipLaunchKernelGGL((k_weight_gradient_short<BLOCKS, DY, OUT, LOAD>), grid, block, 0, s, a, t)
+  if (!a.dy_bf16) {
+    if (a.out_bf16) CARAMEL_WG(2, false, true, kPairs);
+    else CARAMEL_WG(2, false, false, kPairs);
+  } else if (a.outputs % 2 == 0) {
+    if (a.out_bf16) CARAMEL_WG(6, true, true, kPairs);
+    else CARAMEL_WG(6, true, false, kPairs);
+  } else if (a.outputs > 1) {
+    if (a.out_bf16) CARAMEL_WG(6, true, true, kShift);
+    else CARAMEL_WG(6, true, false, kShift);
+  } else {
+    if (a.out_bf16) CARAMEL_WG(6, true, true, kSingle);
+    else CARAMEL_WG(6, true, false, kSingle);
+  }
+#undef CARAMEL_WG
+  return hipGetLastError();
+}
+
 }  // namespace
 
 uint64_t weight_gradient_workspace(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_tokens) {
-  const Shape c = choose(world, features, outputs, max_tokens);
+  // of whichever type dy turns out to have: the two differ only in that few tokens need none
+  const Shape c = choose(world, features, outputs, max_tokens, false);
   if (c.splits < 2) return 0;
   return uint64_t(world) * c.splits * (up256(uint64_t(features) * outputs * 4) + up256(uint64_t(outputs) * 4));
 }
 
 hipError_t launch_weight_gradient(const WeightGradientArgs& a, hipStream_t s) {
   if (a.max_tokens == 0 && a.accumulate) return hipSuccess;
-  const Shape c = choose(a.world, a.features, a.outputs, a.max_tokens);
-  const uint32_t side = c.large ? 256 : 128;
+  const Shape c = choose(a.world, a.features, a.outputs, a.max_tokens, a.dy_bf16);
+  if (c.kernel == kShort) return launch_short(a, s);
+  const bool large = c.kernel == kLargeTile;
+  const uint32_t side = large ? 256 : 128;
   Tiling t{};
   t.nk = (a.features + side - 1) / side;
   t.nn = (a.outputs + side - 1) / side;
   t.splits = c.splits;
   t.total = t.nk * t.nn * t.splits * a.world;
-  if (c.splits == 1) return c.large ? launch<8, 1, 1, 4, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2, 1, 2>(a, t, a.out_bf16, s);
+  if (c.splits == 1) return large ? launch<8, 1, 1, 4, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2, 1, 2>(a, t, a.out_bf16, s);
 
   t.split_stride = up256(uint64_t(a.features) * a.outputs * 4);
   t.bias_stride = up256(uint64_t(a.outputs) * 4);
@@ -494,7 +652,7 @@ hipError_t launch_weight_gradient(const WeightGradientArgs& a, hipStream_t s) {
     p.w.c[w] = parts + w * t.splits * t.split_stride;
     p.bias[w] = bias_parts + w * t.splits * t.bias_stride;
   }
-  const hipError_t e = c.large ? launch<8, 1, 1, 4, 2>(p, t, false, s) : launch<2, 2, 2, 1, 2>(p, t, false, s);
+  const hipError_t e = large ? launch<8, 1, 1, 4, 2>(p, t, false, s) : launch<2, 2, 2, 1, 2>(p, t, false, s);
   if (e != hipSuccess) return e;
   const uint64_t vecs = (uint64_t(a.features) * a.outputs + 3) / 4 + (a.has_bias ? (a.outputs + 3) / 4 : 0);
   const dim3 grid(uint32_t((vecs + 255) / 256), a.world);
