@@ -74,22 +74,26 @@ __device__ __forceinline__ void load_elems(uint64_t at, float* v) {
   }
 }
 
-// ... and back, rounded once
-template <bool BF16, int N>
+// ... and back, rounded once; STREAM: streaming stores
+template <bool BF16, int N, bool STREAM = false>
 __device__ __forceinline__ void store_elems(uint64_t at, const float* v) {
+// (written out: as the argument of a function, a pointer loses the alignment its type promises)
+#define CARAMEL_PUT(type, to, x)                                                                          \
+  if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<CARAMEL_GLOBAL type*>(to)); \
+  else *reinterpret_cast<CARAMEL_GLOBAL type*>(to) = x
   if constexpr (BF16) {
     if constexpr (N == 1) {
-      *reinterpret_cast<CARAMEL_GLOBAL uint16_t*>(at) = uint16_t(bf16_pair(v[0], v[0]));
+      CARAMEL_PUT(uint16_t, at, uint16_t(bf16_pair(v[0], v[0])));
     } else {
       typedef uint32_t vec __attribute__((ext_vector_type(N / 2), aligned(2)));
       vec x;
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) x[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-      *reinterpret_cast<CARAMEL_GLOBAL vec*>(at) = x;
+      CARAMEL_PUT(vec, at, x);
     }
   } else {
     if constexpr (N == 1) {
-      *reinterpret_cast<CARAMEL_GLOBAL float*>(at) = v[0];
+      CARAMEL_PUT(float, at, v[0]);
     } else {
       typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
@@ -97,10 +101,11 @@ __device__ __forceinline__ void store_elems(uint64_t at, const float* v) {
         vec x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = v[q + i];
-        *reinterpret_cast<CARAMEL_GLOBAL vec*>(at + 4 * q) = x;
+        CARAMEL_PUT(vec, at + 4 * q, x);
       }
     }
   }
 }
+#undef CARAMEL_PUT
 
 }  // namespace caramel

@@ -231,7 +231,8 @@ def whole(rng, n, k):
 WGRAD = [  # world, tokens, features, outputs, gap
     (1, 1, 1, 1, 0), (2, 5, 3, 10, 0), (3, 33, 33, 2, 4), (8, 64, 32, 64, 0), (2, 100, 130, 129, 1), (1, 300, 257, 200, 0),
     (2, 31, 784, 256, 0), (1, 1500, 40, 70, 2), (1, 2100, 300, 131, 3), (64, 20, 17, 12, 0), (8, 260, 1100, 1060, 0),
-    (8, 289, 1030, 1301, 0)]
+    (8, 289, 1030, 1301, 0), (12, 2050, 500, 510, 0), (12, 2050, 500, 511, 1), (2, 190, 70, 1, 0), (2, 230, 70, 1, 3),
+    (1, 64, 1000, 130, 0), (3, 192, 40, 300, 2)]
 TYPES = [(cm.F32, cm.F32), (cm.BF16, cm.BF16), (cm.BF16, cm.F32), (cm.F32, cm.BF16)]
 
 
