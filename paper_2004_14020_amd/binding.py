@@ -337,6 +337,8 @@ class Plan:
                         dy_pitch: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
         """bias None: no bias gradient; dy_dtype None: the plan's; dy_pitch None: rows without gaps."""
         per = self._per_worker
+        if bias is not None and not 0 <= bias < self.n_tensors:
+            raise ValueError("the plan has no such tensor")
         _check(lib().caramel_weight_gradient(
             self._h, weight, NO_TENSOR if bias is None else bias, features, per(C.c_void_p, checkpoint, "checkpoint"),
             per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype,

@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
 
 // ---- gradient -------------------------------------------------------------------------------
 
-// Three launches.
+// Up to 64 tokens: one launch, k_embedding_few (below).  Otherwise three.
 //   k_embedding_sort   a stable counting sort of the tokens by id.  A workgroup owns a range of ids and reads
 //                      all of its worker's ids twice (they are a few ten KiB and stay in the caches), so no
 //                      workgroup needs another's counts.
@@ -104,7 +104,8 @@ struct Layout {
 Layout layout(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_tokens) {
   auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
   Layout l{};
-  l.chunk = max_tokens <= 32 || uint64_t(world) * max_tokens >= 16384 ? 32 : 8;
+  // sums and joining, 8 x 4096 tokens of 1024 bf16: 32 to a chunk 91 + 6 us, 16 87 + 10; 4 x 2050 of 1001: 8 8.0 + 5.8, 16 9.9 + 3.9
+  l.chunk = uint64_t(world) * max_tokens >= 16384 ? 32 : 8;
   l.chunks = (max_tokens + l.chunk - 1) / l.chunk;
   l.start = 0;
   l.order = up((uint64_t(vocab) + 1) * 4);
@@ -125,8 +126,8 @@ __device__ __forceinline__ uint32_t read_id(uint64_t ids, uint32_t i, uint32_t v
   }
 }
 
-// Bound: latency (a few thousand ids from the caches).  With one round per different id among 64 tokens in place of
-// the comparison by bits, and one id in flight per lane: 46.8 us for 8 x 4096 tokens of 30522 words.
+// Bound: latency (a few thousand ids from the caches).  8 x 4096 tokens of 30522 words 12.0 us; with eight wavefronts 15, and with
+// one round per different id among 64 tokens in place of the comparison by bits, and one id in flight per lane, 46.8.
 template <bool IDS64>
 __global__ void __launch_bounds__(64 * kSortWaves) k_embedding_sort(EmbeddingGradientArgs a, Layout l, uint32_t range, uint32_t bits) {
   constexpr uint32_t kLanes = 64 * kSortWaves, kNone = 0xFFFFFFFFu;
@@ -402,6 +403,81 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientAr
   leave(start[row + 1] > c1);
 }
 
+// Up to 64 tokens per worker: a wavefront owns a few rows, holds all ids in one register, and needs neither a list nor
+// partial sums.  64 tokens, and 65 in three launches: 8 x (30522 x 1024) bf16 85.9 and 95.6 us, 2 x (2 x 1024) fp32 9.0 and
+// 11.4; 20 tokens of 1000 x 768 fp32 5.9.
+constexpr uint32_t kFew = 64;
+
+template <bool IDS64, bool DY_BF16, bool OUT_BF16>
+__global__ void __launch_bounds__(kSumBlock) k_embedding_few(EmbeddingGradientArgs a, SumShape h) {
+  constexpr int N = DY_BF16 ? 8 : 4, ES = DY_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4, Z = 16 / OS;
+  const uint32_t w = blockIdx.y, n = a.w.tokens[w], lane = threadIdx.x % 64;
+  const uint32_t row0 = uniform((blockIdx.x * (kSumBlock / 64) + threadIdx.x / 64) * h.clear_rows);
+  if (row0 >= a.vocab) return;
+  const uint32_t rows = min(h.clear_rows, a.vocab - row0);
+  const uint64_t out = a.w.c[w];
+  const uint32_t id = lane < n ? read_id<IDS64>(a.w.a[w], lane, a.vocab) : 0xFFFFFFFFu;
+  const uint64_t mine = __ballot(id - row0 < rows);
+  // rows that no token names; the slices of columns share them
+  uint64_t named = 0;
+  for (uint64_t left = mine; left; left &= left - 1) named |= uint64_t(1) << (__builtin_amdgcn_readlane(id, __ffsll((unsigned long long)left) - 1) - row0);
+  if (!a.accumulate) {
+    const float zero[Z] = {};
+    const uint32_t share = (rows + gridDim.z - 1) / gridDim.z, last = min((blockIdx.z + 1) * share, rows);
+    for (uint32_t k = blockIdx.z * share + lane / h.clear_lanes; k < last; k += 64 / h.clear_lanes) {
+      if (named >> k & 1) continue;
+      const uint64_t at = out + uint64_t(row0 + k) * a.width * OS;
+      if (a.width >= Z) {
+        for (uint32_t c = lane % h.clear_lanes * Z; c < a.width; c += h.clear_lanes * Z)
+          store_elems<OUT_BF16, Z, true>(at + min(c, a.width - Z) * OS, zero);
+      } else {
+        for (uint32_t c = lane % h.clear_lanes; c < a.width; c += h.clear_lanes) store_elems<OUT_BF16, 1>(at + c * OS, zero);
+      }
+    }
+  }
+  const uint32_t at_col = (blockIdx.z * 64 + lane) * N;
+  if (!mine || (blockIdx.z * 64) * N >= a.width) return;
+  const Columns c = columns<N>(at_col, a.width);
+  const uint64_t dy = a.w.b[w] + uint64_t(c.col) * ES;
+  for (uint64_t left = mine; left;) {
+    const uint32_t row = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)left) - 1);
+    uint64_t same = __ballot(id == row);
+    left &= ~same;
+    float sum[N] = {};
+    auto walk = [&](auto&& fetch) {
+      while (same) {
+        float x[kAhead][N];
+        bool there[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          there[j] = same != 0;
+          // behind the last one: some token again, which is not added
+          const uint32_t token = there[j] ? __ffsll((unsigned long long)same) - 1 : 0;
+          same &= same - 1;
+          fetch(dy + uint64_t(token) * a.dy_pitch * ES, x[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          if (!there[j]) break;
+          for (int k = 0; k < N; ++k) sum[k] += x[j][k];
+        }
+      }
+    };
+    if (a.width >= N) {
+      walk([&](uint64_t from, float* x) { load_elems<DY_BF16, N>(from, x); });
+    } else {
+      walk([&](uint64_t from, float* x) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          x[k] = 0.0f;
+          if (uint32_t(k) < a.width) load_elems<DY_BF16, 1>(from + k * ES, x + k);
+        }
+      });
+    }
+    if (at_col < a.width) write_row<OUT_BF16, N>(a, out, row, c, sum);
+  }
+}
+
 constexpr int kJoinWaves = 8;
 
 // One workgroup per chunk and 256 columns; it works if a row begins in the chunk and runs past its end.  The
@@ -483,6 +559,36 @@ uint64_t embedding_gradient_workspace(uint32_t world, uint32_t vocab, uint32_t w
 
 hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& a, hipStream_t s) {
   if (a.max_tokens == 0 && a.accumulate) return hipSuccess;
+  const uint32_t per_lane = a.dy_bf16 ? 8 : 4;
+  SumShape h{};
+  h.clear_lanes = lanes_for(a.width, a.out_bf16 ? 8 : 4, 64);
+  h.clear_rows = std::min(64u, 1024 / h.clear_lanes);
+  if (a.max_tokens <= kFew) {
+    const uint32_t slices = (a.width + 64 * per_lane - 1) / (64 * per_lane);
+    // few rows: one to a wavefront, as long as that gives no more than eight wavefronts per SIMD
+    const uint64_t even = (uint64_t(a.vocab) * a.world * slices + 8191) / 8192;
+    h.clear_rows = uint32_t(std::min<uint64_t>(h.clear_rows, even));
+    const uint32_t rows = h.clear_rows * (kSumBlock / 64);  // of a workgroup
+    const dim3 grid((a.vocab + rows - 1) / rows, a.world, slices);
+#define CARAMEL_FEW(IDS64, DY, OUT) hipLaunchKernelGGL((k_embedding_few<IDS64, DY, OUT>), grid, dim3(kSumBlock), 0, s, a, h)
+    if (a.ids64) {
+      if (a.dy_bf16) {
+        if (a.out_bf16) CARAMEL_FEW(true, true, true);
+        else CARAMEL_FEW(true, true, false);
+      } else {
+        if (a.out_bf16) CARAMEL_FEW(true, false, true);
+        else CARAMEL_FEW(true, false, false);
+      }
+    } else if (a.dy_bf16) {
+      if (a.out_bf16) CARAMEL_FEW(false, true, true);
+      else CARAMEL_FEW(false, true, false);
+    } else {
+      if (a.out_bf16) CARAMEL_FEW(false, false, true);
+      else CARAMEL_FEW(false, false, false);
+    }
+#undef CARAMEL_FEW
+    return hipGetLastError();
+  }
   const Layout l = layout(a.world, a.vocab, a.width, a.max_tokens);
   // enough workgroups to fill the chip, each with as few ids as that allows
   const uint64_t even = (uint64_t(a.vocab) * a.world + 255) / 256;
@@ -494,13 +600,9 @@ hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& a, hipStream_t
   else hipLaunchKernelGGL((k_embedding_sort<false>), sort_grid, dim3(64 * kSortWaves), 0, s, a, l, range, bits);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const uint32_t per_lane = a.dy_bf16 ? 8 : 4;
-  SumShape h{};
   h.lanes = lanes_for(a.width, per_lane, 64);
   const uint32_t groups = kSumBlock / h.lanes, slices = (a.width + h.lanes * per_lane - 1) / (h.lanes * per_lane);
   h.sum_blocks = (l.chunks + groups - 1) / groups;
-  h.clear_lanes = lanes_for(a.width, a.out_bf16 ? 8 : 4, 64);
-  h.clear_rows = std::min(64u, 1024 / h.clear_lanes);
   const uint32_t cleared = h.clear_rows * (kSumBlock / 64) * slices;  // by the workgroups of one x
   const dim3 sum_grid(h.sum_blocks + (a.accumulate ? 0 : (a.vocab + cleared - 1) / cleared), a.world, slices);
 #define CARAMEL_SUM(DY, OUT, FULL) hipLaunchKernelGGL((k_embedding_sum<DY, OUT, FULL>), sum_grid, dim3(kSumBlock), 0, s, a, l, h)

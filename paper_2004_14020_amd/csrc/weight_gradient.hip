@@ -325,7 +325,8 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
 
   // The products of a block, in the order in which they are made: two steps of 16 tokens, the parts of dy from the smallest
   // on, the wavefront's outputs.
-  constexpr int kSlots = 2 * P * TB * 2, kDepth = 4;
+  constexpr int kSlots = 2 * P * TB * 2, kDepth = 4;  // operands in flight (two: the same within 2 %)
+  static_assert(kSlots % kDepth == 0, "a turn ends with the operands where the next one looks for them");
   auto read = [&](uint32_t buf, int slot) {
     const int c = slot % (TB * 2), p = P - 1 - slot / (TB * 2) % P, s = slot / (TB * 2 * P);
     return __builtin_bit_cast(bf16x8, lds[buf][p][half * 2 + s][(c % 2) * (TN / 2) + (wn * TB + c / 2) * 32 + l32]);

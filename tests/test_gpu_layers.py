@@ -468,6 +468,63 @@ def test_overlap_with_the_bound_tensors_is_refused():
     plan.close()
 
 
+@pytest.mark.parametrize("accumulate", [False, True], ids=["write", "add"])
+def test_no_tokens_at_all(accumulate):
+    """Gradients of nothing: zeros, or what was there; no pointer of a worker without tokens is looked at."""
+    plan, grads = bound_plan(2, [30 * 20, 20], cm.F32, fill=0.75)
+    need = plan.embedding_workspace(0, 20, [0, 0])
+    ws = workspace(need)
+    none = [None, None]
+    plan.embedding_lookup(none, 30, 20, none, [0, 0], none, stream=stream())
+    plan.checkpoint_store(none, [0, 0], 30, none, stream=stream())
+    plan.checkpoint_load(none, [0, 0], 30, none, stream=stream())
+    plan.embedding_gradient(0, 20, none, [0, 0], none, ws.data_ptr(), need, accumulate=accumulate, stream=stream())
+    want = 0.75 if accumulate else 0.0
+    assert all(bool((row[0] == want).all()) and bool((row[1] == 0.75).all()) for row in grads)
+    for row in grads:
+        row[0].fill_(0.75)
+    plan.weight_gradient(0, 1, none, [0, 0], 30, none, None, 0, accumulate=accumulate, stream=stream())
+    assert all(bool((t == want).all()) for row in grads for t in row)
+    plan.close()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+def test_rows_that_start_on_any_element(dtype):
+    """Every buffer of rows one element behind an aligned address, even and odd widths."""
+    rng = np.random.default_rng(11)
+    n, vocab = 77, 40
+    for width in (64, 63, 130):
+        plan, grads = bound_plan(1, [vocab * width, 48 * width], cm.F32)
+        at = lambda t: [t.data_ptr() + t.element_size()]                               # noqa: E731
+        shifted = lambda v: torch.cat([v.new_zeros(1), v.reshape(-1)]).to(DEV)         # noqa: E731
+        typed = cm.Plan(1, [1], dtype=dtype)
+        table = torch.tensor(rng.integers(-8, 9, (vocab, width)).astype(np.float32)).to(TORCH[dtype])
+        rows_ = torch.tensor(rng.integers(-8, 9, (n, width)).astype(np.float32)).to(TORCH[dtype])
+        ids = torch.tensor(rng.integers(0, vocab, n), device=DEV)
+        src, dy, out = shifted(table), shifted(rows_), torch.full((n * width + 2,), 7.0, dtype=TORCH[dtype], device=DEV)
+        typed.embedding_lookup(at(src), vocab, width, [ids.data_ptr()], [n], at(out), stream=stream())
+        assert torch.equal(out[1:-1].cpu().view(n, width), table[ids.cpu()]) and float(out[0]) == float(out[-1]) == 7.0
+        need = plan.embedding_workspace(0, width, [n])
+        ws = workspace(need)
+        plan.embedding_gradient(0, width, [ids.data_ptr()], [n], at(dy), ws.data_ptr(), need, dy_dtype=dtype, stream=stream())
+        assert np.array_equal(f64(grads[0][0]).reshape(vocab, width), embedding_gradient(vocab, ids.tolist(), f64(rows_), 1.0)[0])
+        saved = torch.empty(cm.checkpoint_bytes(n, width), dtype=torch.uint8, device=DEV)
+        plan.checkpoint_store(at(dy), [n], width, [saved.data_ptr()], dtype=dtype, stream=stream())
+        out.fill_(7.0)
+        plan.checkpoint_load([saved.data_ptr()], [n], width, at(out), dtype=dtype, stream=stream())
+        assert torch.equal(out[1:-1].cpu().view(n, width), rows_) and float(out[0]) == float(out[-1]) == 7.0
+        for tokens in (n, 300):                              # few tokens, and a second kernel
+            x = whole(rng, tokens, 48)
+            d = torch.tensor(rng.integers(-8, 9, (tokens, width)).astype(np.float32)).to(TORCH[dtype])
+            kept, moved = saved_checkpoints([x]), shifted(d)
+            need = plan.weight_gradient_workspace(1, 48, [tokens])
+            ws = workspace(need)
+            plan.weight_gradient(1, None, addresses(kept), [tokens], 48, at(moved), ws.data_ptr(), need, dy_dtype=dtype, stream=stream())
+            assert np.array_equal(f64(grads[0][1]).reshape(48, width), x.T @ f64(d))
+        plan.close()
+        typed.close()
+
+
 # ---- offsets beyond 32 bits -----------------------------------------------------------------
 def test_a_table_of_more_than_four_gib():
     vocab, width = 2_200_000, 1024                           # 4.5 GB in bf16
