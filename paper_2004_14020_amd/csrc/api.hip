@@ -1090,6 +1090,7 @@ struct Memory {
   };
   std::vector<Span> spans;
 
+  explicit Memory(uint32_t world) { spans.reserve(4 * world + 1); }
   void add(uint64_t at, uint64_t bytes, bool written) {
     if (bytes) spans.push_back({at, at + bytes, written});
   }
@@ -1186,20 +1187,21 @@ int embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, 
   if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
   const uint64_t es = p->host.elem_size();
   LookupArgs a{};
+  AllWorkers v{};
   if (int rc = check_table(vocab, width)) return rc;
   if (id_bytes != 4 && id_bytes != 8) return fail(CARAMEL_EINVAL, "id_bytes must be 4 or 8, is %u", id_bytes);
-  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
   if (int rc = check_rows("out_pitch", out_pitch, width, a.max_tokens)) return rc;
-  if (int rc = take_pointers(p, "table", table, a.w.tokens, es, a.w.a)) return rc;
-  if (int rc = take_pointers(p, "ids", ids, a.w.tokens, id_bytes, a.w.b)) return rc;
-  if (int rc = take_pointers(p, "out", out, a.w.tokens, es, a.w.c)) return rc;
-  a.world = p->host.cfg.world;
-  Memory m;
-  for (uint32_t w = 0; w < a.world; ++w) {
-    if (!a.w.tokens[w]) continue;
-    m.add(a.w.a[w], vocab * width * es, false);
-    m.add(a.w.b[w], uint64_t(a.w.tokens[w]) * id_bytes, false);
-    m.add(a.w.c[w], rows_bytes(a.w.tokens[w], out_pitch, width, es), true);
+  if (int rc = take_pointers(p, "table", table, v.tokens, es, v.a)) return rc;
+  if (int rc = take_pointers(p, "ids", ids, v.tokens, id_bytes, v.b)) return rc;
+  if (int rc = take_pointers(p, "out", out, v.tokens, es, v.c)) return rc;
+  a.all = p->host.cfg.world;
+  Memory m(a.all);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    if (!v.tokens[w]) continue;
+    m.add(v.a[w], vocab * width * es, false);
+    m.add(v.b[w], uint64_t(v.tokens[w]) * id_bytes, false);
+    m.add(v.c[w], rows_bytes(v.tokens[w], out_pitch, width, es), true);
   }
   if (int rc = m.check()) return rc;
   if (int rc = need_device(p)) return rc;
@@ -1210,9 +1212,9 @@ int embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, 
   a.ids64 = id_bytes == 8;
   a.bf16 = p->host.cfg.dtype == CARAMEL_BF16;
   if (tracing())
-    std::fprintf(stderr, "caramel: embedding lookup stream %p, %u workers, up to %u tokens, %u columns\n", (void*)stream, a.world,
+    std::fprintf(stderr, "caramel: embedding lookup stream %p, %u workers, up to %u tokens, %u columns\n", (void*)stream, a.all,
                  a.max_tokens, a.width);
-  HIP_TRY(launch_embedding_lookup(a, stream));
+  HIP_TRY(launch_embedding_lookup(a, v, stream));
   return CARAMEL_OK;
 }
 
@@ -1234,25 +1236,26 @@ int embedding_gradient(caramel_plan* p, uint32_t tensor, uint64_t width, float s
   const uint64_t es = p->host.elem_size();
   uint64_t vocab = 0;
   EmbeddingGradientArgs a{};
+  AllWorkers v{};
   if (int rc = check_matrix(p, "table", tensor, width, &vocab)) return rc;
   if (int rc = check_table(vocab, width)) return rc;
   if (id_bytes != 4 && id_bytes != 8) return fail(CARAMEL_EINVAL, "id_bytes must be 4 or 8, is %u", id_bytes);
   if (int rc = check_dtype("dy_dtype", dy_dtype)) return rc;
-  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
   if (int rc = check_rows("dy_pitch", dy_pitch, width, a.max_tokens)) return rc;
-  if (int rc = take_pointers(p, "ids", ids, a.w.tokens, id_bytes, a.w.a)) return rc;
-  if (int rc = take_pointers(p, "dy", dy, a.w.tokens, size_of(dy_dtype), a.w.b)) return rc;
-  a.world = p->host.cfg.world;
-  const uint64_t need = embedding_gradient_workspace(a.world, uint32_t(vocab), uint32_t(width), a.max_tokens);
+  if (int rc = take_pointers(p, "ids", ids, v.tokens, id_bytes, v.a)) return rc;
+  if (int rc = take_pointers(p, "dy", dy, v.tokens, size_of(dy_dtype), v.b)) return rc;
+  a.all = p->host.cfg.world;
+  const uint64_t need = embedding_gradient_workspace(a.all, uint32_t(vocab), uint32_t(width), a.max_tokens);
   if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
   if (int rc = need_bound(p, false)) return rc;
-  Memory m;
+  Memory m(a.all);
   m.add(reinterpret_cast<uint64_t>(ws), need, true);
-  for (uint32_t w = 0; w < a.world; ++w) {
-    a.w.c[w] = p->bind.rows[tensor * a.world + w];
-    m.add(a.w.c[w], vocab * width * es, true);
-    m.add(a.w.a[w], uint64_t(a.w.tokens[w]) * id_bytes, false);
-    m.add(a.w.b[w], rows_bytes(a.w.tokens[w], dy_pitch, width, size_of(dy_dtype)), false);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    v.c[w] = p->bind.rows[tensor * a.all + w];
+    m.add(v.c[w], vocab * width * es, true);
+    m.add(v.a[w], uint64_t(v.tokens[w]) * id_bytes, false);
+    m.add(v.b[w], rows_bytes(v.tokens[w], dy_pitch, width, size_of(dy_dtype)), false);
   }
   if (int rc = m.check()) return rc;
   a.vocab = uint32_t(vocab);
@@ -1266,8 +1269,8 @@ int embedding_gradient(caramel_plan* p, uint32_t tensor, uint64_t width, float s
   a.ws = static_cast<unsigned char*>(ws);
   if (tracing())
     std::fprintf(stderr, "caramel: embedding gradient stream %p, tensor %u, %u workers, up to %u tokens, %u x %u\n", (void*)stream,
-                 tensor, a.world, a.max_tokens, a.vocab, a.width);
-  HIP_TRY(launch_embedding_gradient(a, stream));
+                 tensor, a.all, a.max_tokens, a.vocab, a.width);
+  HIP_TRY(launch_embedding_gradient(a, v, stream));
   return CARAMEL_OK;
 }
 
@@ -1275,18 +1278,19 @@ int checkpoint_call(caramel_plan* p, bool store, const uint64_t* tokens, uint64_
                     uint64_t pitch, const void* const* checkpoint, hipStream_t stream) {
   if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
   CheckpointArgs a{};
+  AllWorkers v{};
   if (int rc = check_columns("features", features)) return rc;
   if (int rc = check_dtype("dtype", dtype)) return rc;
   const uint64_t es = size_of(dtype);
-  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
   if (int rc = check_rows("pitch", pitch, features, a.max_tokens)) return rc;
-  if (int rc = take_pointers(p, "x", x, a.w.tokens, es, a.w.a)) return rc;
-  if (int rc = take_pointers(p, "checkpoint", checkpoint, a.w.tokens, 16, a.w.b)) return rc;
-  a.world = p->host.cfg.world;
-  Memory m;
-  for (uint32_t w = 0; w < a.world; ++w) {
-    m.add(a.w.a[w], rows_bytes(a.w.tokens[w], pitch, features, es), !store);
-    m.add(a.w.b[w], checkpoint_size(a.w.tokens[w], features), store);
+  if (int rc = take_pointers(p, "x", x, v.tokens, es, v.a)) return rc;
+  if (int rc = take_pointers(p, "checkpoint", checkpoint, v.tokens, 16, v.b)) return rc;
+  a.all = p->host.cfg.world;
+  Memory m(a.all);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    m.add(v.a[w], rows_bytes(v.tokens[w], pitch, features, es), !store);
+    m.add(v.b[w], checkpoint_size(v.tokens[w], features), store);
   }
   if (int rc = m.check()) return rc;
   if (int rc = need_device(p)) return rc;
@@ -1295,8 +1299,8 @@ int checkpoint_call(caramel_plan* p, bool store, const uint64_t* tokens, uint64_
   a.bf16 = dtype == CARAMEL_BF16;
   if (tracing())
     std::fprintf(stderr, "caramel: checkpoint %s stream %p, %u workers, up to %u tokens, %u features\n", store ? "store" : "load",
-                 (void*)stream, a.world, a.max_tokens, a.features);
-  HIP_TRY(store ? launch_checkpoint_store(a, stream) : launch_checkpoint_load(a, stream));
+                 (void*)stream, a.all, a.max_tokens, a.features);
+  HIP_TRY(store ? launch_checkpoint_store(a, v, stream) : launch_checkpoint_load(a, v, stream));
   return CARAMEL_OK;
 }
 
@@ -1319,6 +1323,7 @@ int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t fe
   const uint64_t es = p->host.elem_size();
   uint64_t outputs = 0;
   WeightGradientArgs a{};
+  AllWorkers v{};
   if (int rc = check_matrix(p, "weight", weight, features, &outputs)) return rc;
   if (int rc = check_columns("features", features)) return rc;
   if (int rc = check_columns("outputs", outputs)) return rc;
@@ -1328,26 +1333,26 @@ int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t fe
       return fail(CARAMEL_EINVAL, "tensor %u is no bias of %llu outputs", bias, (unsigned long long)outputs);
   }
   if (int rc = check_dtype("dy_dtype", dy_dtype)) return rc;
-  if (int rc = take_tokens(p, tokens, a.w.tokens, &a.max_tokens)) return rc;
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
   if (int rc = check_rows("dy_pitch", dy_pitch, outputs, a.max_tokens)) return rc;
   if (uint64_t(a.max_tokens) * features > kMaxValues) return fail(CARAMEL_EINVAL, "more than 2^38 values at one worker");
-  if (int rc = take_pointers(p, "checkpoint", checkpoint, a.w.tokens, 16, a.w.a)) return rc;
-  if (int rc = take_pointers(p, "dy", dy, a.w.tokens, size_of(dy_dtype), a.w.b)) return rc;
-  a.world = p->host.cfg.world;
-  const uint64_t need = weight_gradient_workspace(a.world, uint32_t(features), uint32_t(outputs), a.max_tokens);
+  if (int rc = take_pointers(p, "checkpoint", checkpoint, v.tokens, 16, v.a)) return rc;
+  if (int rc = take_pointers(p, "dy", dy, v.tokens, size_of(dy_dtype), v.b)) return rc;
+  a.all = p->host.cfg.world;
+  const uint64_t need = weight_gradient_workspace(a.all, uint32_t(features), uint32_t(outputs), a.max_tokens);
   if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
   if (int rc = need_bound(p, false)) return rc;
-  Memory m;
+  Memory m(a.all);
   m.add(reinterpret_cast<uint64_t>(ws), need, true);
-  for (uint32_t w = 0; w < a.world; ++w) {
-    a.w.c[w] = p->bind.rows[weight * a.world + w];
-    m.add(a.w.c[w], features * outputs * es, true);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    v.c[w] = p->bind.rows[weight * a.all + w];
+    m.add(v.c[w], features * outputs * es, true);
     if (a.has_bias) {
-      a.bias[w] = p->bind.rows[bias * a.world + w];
-      m.add(a.bias[w], outputs * es, true);
+      v.d[w] = p->bind.rows[bias * a.all + w];
+      m.add(v.d[w], outputs * es, true);
     }
-    m.add(a.w.a[w], checkpoint_size(a.w.tokens[w], features), false);
-    m.add(a.w.b[w], rows_bytes(a.w.tokens[w], dy_pitch, outputs, size_of(dy_dtype)), false);
+    m.add(v.a[w], checkpoint_size(v.tokens[w], features), false);
+    m.add(v.b[w], rows_bytes(v.tokens[w], dy_pitch, outputs, size_of(dy_dtype)), false);
   }
   if (int rc = m.check()) return rc;
   a.features = uint32_t(features);
@@ -1359,8 +1364,8 @@ int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t fe
   a.ws = static_cast<unsigned char*>(ws);
   if (tracing())
     std::fprintf(stderr, "caramel: weight gradient stream %p, tensor %u, %u workers, up to %u tokens, %u x %u\n", (void*)stream,
-                 weight, a.world, a.max_tokens, a.features, a.outputs);
-  HIP_TRY(launch_weight_gradient(a, stream));
+                 weight, a.all, a.max_tokens, a.features, a.outputs);
+  HIP_TRY(launch_weight_gradient(a, v, stream));
   return CARAMEL_OK;
 }
 

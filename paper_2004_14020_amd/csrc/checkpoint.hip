@@ -229,23 +229,27 @@ dim3 grid_of(const CheckpointArgs& a, uint32_t features) {  // of a lane
 
 }  // namespace
 
-hipError_t launch_checkpoint_store(const CheckpointArgs& a, hipStream_t s) {
-  if (a.max_tokens == 0) return hipSuccess;
-  bool odd = a.pitch % 2 || a.features % 2;
-  for (uint32_t w = 0; w < a.world; ++w) odd = odd || a.w.a[w] % 4;
-  const dim3 block(64 * kWaves);
-  if (!a.bf16) hipLaunchKernelGGL((k_checkpoint_store<false, false>), grid_of(a, 2), block, 0, s, a);
-  else if (odd) hipLaunchKernelGGL((k_checkpoint_store<true, true>), grid_of(a, 4), block, 0, s, a);
-  else hipLaunchKernelGGL((k_checkpoint_store<true, false>), grid_of(a, 4), block, 0, s, a);
-  return hipGetLastError();
+hipError_t launch_checkpoint_store(const CheckpointArgs& args, const AllWorkers& v, hipStream_t s) {
+  if (args.max_tokens == 0) return hipSuccess;
+  bool odd = args.pitch % 2 || args.features % 2;
+  for (uint32_t w = 0; w < args.all; ++w) odd = odd || v.a[w] % 4;
+  return in_groups(args, v, [&](const CheckpointArgs& a, uint32_t) {
+    const dim3 block(64 * kWaves);
+    if (!a.bf16) hipLaunchKernelGGL((k_checkpoint_store<false, false>), grid_of(a, 2), block, 0, s, a);
+    else if (odd) hipLaunchKernelGGL((k_checkpoint_store<true, true>), grid_of(a, 4), block, 0, s, a);
+    else hipLaunchKernelGGL((k_checkpoint_store<true, false>), grid_of(a, 4), block, 0, s, a);
+    return hipGetLastError();
+  });
 }
 
-hipError_t launch_checkpoint_load(const CheckpointArgs& a, hipStream_t s) {
-  if (a.max_tokens == 0) return hipSuccess;
-  const dim3 block(64 * kWaves);
-  if (a.bf16) hipLaunchKernelGGL((k_checkpoint_load<true>), grid_of(a, 4), block, 0, s, a);
-  else hipLaunchKernelGGL((k_checkpoint_load<false>), grid_of(a, 4), block, 0, s, a);
-  return hipGetLastError();
+hipError_t launch_checkpoint_load(const CheckpointArgs& args, const AllWorkers& v, hipStream_t s) {
+  if (args.max_tokens == 0) return hipSuccess;
+  return in_groups(args, v, [&](const CheckpointArgs& a, uint32_t) {
+    const dim3 block(64 * kWaves);
+    if (a.bf16) hipLaunchKernelGGL((k_checkpoint_load<true>), grid_of(a, 4), block, 0, s, a);
+    else hipLaunchKernelGGL((k_checkpoint_load<false>), grid_of(a, 4), block, 0, s, a);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace caramel

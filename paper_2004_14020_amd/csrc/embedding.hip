@@ -528,73 +528,39 @@ uint32_t lanes_for(uint32_t width, uint32_t per_lane, uint32_t most) {
   return lanes;
 }
 
-}  // namespace
-
-hipError_t launch_embedding_lookup(const LookupArgs& a, hipStream_t s) {
-  if (a.max_tokens == 0) return hipSuccess;
-  const uint32_t lanes = lanes_for(a.width, a.bf16 ? 8 : 4, 256);
-  const uint32_t rows = 256 / lanes * kLookupRows;
-  const dim3 grid((a.max_tokens + rows - 1) / rows, a.world);
-  uint64_t bytes = 0;
-  for (uint32_t w = 0; w < a.world; ++w) bytes += uint64_t(a.w.tokens[w]) * a.width * (a.bf16 ? 2 : 4);
-  const bool stream = bytes > (uint64_t(32) << 20);
-#define CARAMEL_LOOKUP(BF16, IDS64)                                                                                    \
-  if (stream) hipLaunchKernelGGL((k_embedding_lookup<BF16, IDS64, true>), grid, dim3(256), 0, s, a, lanes);            \
-  else hipLaunchKernelGGL((k_embedding_lookup<BF16, IDS64, false>), grid, dim3(256), 0, s, a, lanes)
-  if (a.bf16) {
-    if (a.ids64) {
-      CARAMEL_LOOKUP(true, true);
+// `h` has the shape of clearing a row.
+hipError_t launch_few(const EmbeddingGradientArgs& a, SumShape h, hipStream_t s) {
+  const uint32_t per_lane = a.dy_bf16 ? 8 : 4;
+  const uint32_t slices = (a.width + 64 * per_lane - 1) / (64 * per_lane);
+  // few rows: one to a wavefront, as long as that gives no more than eight wavefronts per SIMD
+  const uint64_t even = (uint64_t(a.vocab) * a.all * slices + 8191) / 8192;
+  h.clear_rows = uint32_t(std::min<uint64_t>(h.clear_rows, even));
+  const uint32_t rows = h.clear_rows * (kSumBlock / 64);  // of a workgroup
+  const dim3 grid((a.vocab + rows - 1) / rows, a.world, slices);
+#define CARAMEL_FEW(IDS64, DY, OUT) hipLaunchKernelGGL((k_embedding_few<IDS64, DY, OUT>), grid, dim3(kSumBlock), 0, s, a, h)
+  if (a.ids64) {
+    if (a.dy_bf16) {
+      if (a.out_bf16) CARAMEL_FEW(true, true, true);
+      else CARAMEL_FEW(true, true, false);
     } else {
-      CARAMEL_LOOKUP(true, false);
+      if (a.out_bf16) CARAMEL_FEW(true, false, true);
+      else CARAMEL_FEW(true, false, false);
     }
-  } else if (a.ids64) {
-    CARAMEL_LOOKUP(false, true);
+  } else if (a.dy_bf16) {
+    if (a.out_bf16) CARAMEL_FEW(false, true, true);
+    else CARAMEL_FEW(false, true, false);
   } else {
-    CARAMEL_LOOKUP(false, false);
+    if (a.out_bf16) CARAMEL_FEW(false, false, true);
+    else CARAMEL_FEW(false, false, false);
   }
-#undef CARAMEL_LOOKUP
+#undef CARAMEL_FEW
   return hipGetLastError();
 }
 
-uint64_t embedding_gradient_workspace(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_tokens) {
-  return layout(world, vocab, width, max_tokens).stride * world;
-}
-
-hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& a, hipStream_t s) {
-  if (a.max_tokens == 0 && a.accumulate) return hipSuccess;
+hipError_t launch_sorted(const EmbeddingGradientArgs& a, const Layout& l, SumShape h, hipStream_t s) {
   const uint32_t per_lane = a.dy_bf16 ? 8 : 4;
-  SumShape h{};
-  h.clear_lanes = lanes_for(a.width, a.out_bf16 ? 8 : 4, 64);
-  h.clear_rows = std::min(64u, 1024 / h.clear_lanes);
-  if (a.max_tokens <= kFew) {
-    const uint32_t slices = (a.width + 64 * per_lane - 1) / (64 * per_lane);
-    // few rows: one to a wavefront, as long as that gives no more than eight wavefronts per SIMD
-    const uint64_t even = (uint64_t(a.vocab) * a.world * slices + 8191) / 8192;
-    h.clear_rows = uint32_t(std::min<uint64_t>(h.clear_rows, even));
-    const uint32_t rows = h.clear_rows * (kSumBlock / 64);  // of a workgroup
-    const dim3 grid((a.vocab + rows - 1) / rows, a.world, slices);
-#define CARAMEL_FEW(IDS64, DY, OUT) hipLaunchKernelGGL((k_embedding_few<IDS64, DY, OUT>), grid, dim3(kSumBlock), 0, s, a, h)
-    if (a.ids64) {
-      if (a.dy_bf16) {
-        if (a.out_bf16) CARAMEL_FEW(true, true, true);
-        else CARAMEL_FEW(true, true, false);
-      } else {
-        if (a.out_bf16) CARAMEL_FEW(true, false, true);
-        else CARAMEL_FEW(true, false, false);
-      }
-    } else if (a.dy_bf16) {
-      if (a.out_bf16) CARAMEL_FEW(false, true, true);
-      else CARAMEL_FEW(false, true, false);
-    } else {
-      if (a.out_bf16) CARAMEL_FEW(false, false, true);
-      else CARAMEL_FEW(false, false, false);
-    }
-#undef CARAMEL_FEW
-    return hipGetLastError();
-  }
-  const Layout l = layout(a.world, a.vocab, a.width, a.max_tokens);
   // enough workgroups to fill the chip, each with as few ids as that allows
-  const uint64_t even = (uint64_t(a.vocab) * a.world + 255) / 256;
+  const uint64_t even = (uint64_t(a.vocab) * a.all + 255) / 256;
   const uint32_t range = uint32_t(std::min<uint64_t>({kSortRange, std::max<uint64_t>(64, even), a.vocab}));
   uint32_t bits = 0;
   while ((1u << bits) < range) ++bits;
@@ -633,6 +599,54 @@ hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& a, hipStream_t
   if (a.out_bf16) hipLaunchKernelGGL((k_embedding_join<true>), join_grid, dim3(64 * kJoinWaves), 0, s, a, l);
   else hipLaunchKernelGGL((k_embedding_join<false>), join_grid, dim3(64 * kJoinWaves), 0, s, a, l);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_embedding_lookup(const LookupArgs& args, const AllWorkers& v, hipStream_t s) {
+  if (args.max_tokens == 0) return hipSuccess;
+  const uint32_t lanes = lanes_for(args.width, args.bf16 ? 8 : 4, 256);
+  const uint32_t rows = 256 / lanes * kLookupRows;
+  uint64_t bytes = 0;
+  for (uint32_t w = 0; w < args.all; ++w) bytes += uint64_t(v.tokens[w]) * args.width * (args.bf16 ? 2 : 4);
+  const bool stream = bytes > (uint64_t(32) << 20);
+  return in_groups(args, v, [&](const LookupArgs& a, uint32_t) {
+    const dim3 grid((a.max_tokens + rows - 1) / rows, a.world);
+#define CARAMEL_LOOKUP(BF16, IDS64)                                                                                    \
+  if (stream) hipLaunchKernelGGL((k_embedding_lookup<BF16, IDS64, true>), grid, dim3(256), 0, s, a, lanes);            \
+  else hipLaunchKernelGGL((k_embedding_lookup<BF16, IDS64, false>), grid, dim3(256), 0, s, a, lanes)
+    if (a.bf16) {
+      if (a.ids64) {
+        CARAMEL_LOOKUP(true, true);
+      } else {
+        CARAMEL_LOOKUP(true, false);
+      }
+    } else if (a.ids64) {
+      CARAMEL_LOOKUP(false, true);
+    } else {
+      CARAMEL_LOOKUP(false, false);
+    }
+#undef CARAMEL_LOOKUP
+    return hipGetLastError();
+  });
+}
+
+uint64_t embedding_gradient_workspace(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_tokens) {
+  return layout(world, vocab, width, max_tokens).stride * world;
+}
+
+hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& args, const AllWorkers& v, hipStream_t s) {
+  if (args.max_tokens == 0 && args.accumulate) return hipSuccess;
+  SumShape h{};
+  h.clear_lanes = lanes_for(args.width, args.out_bf16 ? 8 : 4, 64);
+  h.clear_rows = std::min(64u, 1024 / h.clear_lanes);
+  if (args.max_tokens <= kFew)
+    return in_groups(args, v, [&](const EmbeddingGradientArgs& a, uint32_t) { return launch_few(a, h, s); });
+  const Layout l = layout(args.all, args.vocab, args.width, args.max_tokens);
+  return in_groups(args, v, [&](EmbeddingGradientArgs a, uint32_t first) {
+    a.ws += first * l.stride;
+    return launch_sorted(a, l, h, s);
+  });
 }
 
 }  // namespace caramel

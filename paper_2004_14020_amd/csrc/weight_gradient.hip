@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
 
   if (sums_dy) {  // the same for all lanes of the workgroup
     __syncthreads();
-    write_bias<OUT_BF16, TN, OCTETS>(a, reinterpret_cast<float*>(lds), tid, n0, a.bias[w] + split * t.bias_stride, dy.octet, dy.pair,
+    write_bias<OUT_BF16, TN, OCTETS>(a, reinterpret_cast<float*>(lds), tid, n0, a.w.d[w] + split * t.bias_stride, dy.octet, dy.pair,
                                      dy.bias);
   }
 }
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradient
 
   if (sums_dy) {
     __syncthreads();
-    write_bias<OUT_BF16, TN, 4>(a, reinterpret_cast<float*>(lds), tid, n0, a.bias[w], dy.octet, dy.pair, dy.bias);
+    write_bias<OUT_BF16, TN, 4>(a, reinterpret_cast<float*>(lds), tid, n0, a.w.d[w], dy.octet, dy.pair, dy.bias);
   }
 }
 
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(256) k_weight_join(WeightGradientArgs a, Tilin
     if (!a.has_bias || i >= a.outputs) return;
     from = bias_parts + w * t.splits * t.bias_stride;
     stride = t.bias_stride;
-    to = a.bias[w];
+    to = a.w.d[w];
     end = a.outputs;
   }
   if (i + 4 <= end) {
@@ -645,35 +645,39 @@ uint64_t weight_gradient_workspace(uint32_t world, uint32_t features, uint32_t o
   return uint64_t(world) * c.splits * (up256(uint64_t(features) * outputs * 4) + up256(uint64_t(outputs) * 4));
 }
 
-hipError_t launch_weight_gradient(const WeightGradientArgs& a, hipStream_t s) {
-  if (a.max_tokens == 0 && a.accumulate) return hipSuccess;
-  const Shape c = choose(a.world, a.features, a.outputs, a.max_tokens, a.dy_bf16);
-  if (c.kernel == kShort) return launch_short(a, s);
+hipError_t launch_weight_gradient(const WeightGradientArgs& args, const AllWorkers& v, hipStream_t s) {
+  if (args.max_tokens == 0 && args.accumulate) return hipSuccess;
+  const Shape c = choose(args.all, args.features, args.outputs, args.max_tokens, args.dy_bf16);
+  if (c.kernel == kShort) return in_groups(args, v, [&](const WeightGradientArgs& a, uint32_t) { return launch_short(a, s); });
   const bool large = c.kernel == kLargeTile;
   const uint32_t side = large ? 256 : 128;
   Tiling t{};
-  t.nk = (a.features + side - 1) / side;
-  t.nn = (a.outputs + side - 1) / side;
+  t.nk = (args.features + side - 1) / side;
+  t.nn = (args.outputs + side - 1) / side;
   t.splits = c.splits;
-  t.total = t.nk * t.nn * t.splits * a.world;
-  if (c.splits == 1) return large ? launch<8, 1, 1, 4, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2, 1, 2>(a, t, a.out_bf16, s);
-
-  t.split_stride = up256(uint64_t(a.features) * a.outputs * 4);
-  t.bias_stride = up256(uint64_t(a.outputs) * 4);
-  const uint64_t parts = reinterpret_cast<uint64_t>(a.ws), bias_parts = parts + a.world * t.splits * t.split_stride;
-  WeightGradientArgs p = a;
-  p.accumulate = false;
-  for (uint32_t w = 0; w < a.world; ++w) {
-    p.w.c[w] = parts + w * t.splits * t.split_stride;
-    p.bias[w] = bias_parts + w * t.splits * t.bias_stride;
+  if (c.splits > 1) {
+    t.split_stride = up256(uint64_t(args.features) * args.outputs * 4);
+    t.bias_stride = up256(uint64_t(args.outputs) * 4);
   }
-  const hipError_t e = large ? launch<8, 1, 1, 4, 2>(p, t, false, s) : launch<2, 2, 2, 1, 2>(p, t, false, s);
-  if (e != hipSuccess) return e;
-  const uint64_t vecs = (uint64_t(a.features) * a.outputs + 3) / 4 + (a.has_bias ? (a.outputs + 3) / 4 : 0);
-  const dim3 grid(uint32_t((vecs + 255) / 256), a.world);
-  if (a.out_bf16) hipLaunchKernelGGL((k_weight_join<true>), grid, dim3(256), 0, s, a, t, parts, bias_parts);
-  else hipLaunchKernelGGL((k_weight_join<false>), grid, dim3(256), 0, s, a, t, parts, bias_parts);
-  return hipGetLastError();
+  return in_groups(args, v, [&](const WeightGradientArgs& a, uint32_t first) {
+    t.total = t.nk * t.nn * t.splits * a.world;
+    if (c.splits == 1) return large ? launch<8, 1, 1, 4, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2, 1, 2>(a, t, a.out_bf16, s);
+    const uint64_t parts = reinterpret_cast<uint64_t>(a.ws) + first * t.splits * (t.split_stride + t.bias_stride);
+    const uint64_t bias_parts = parts + a.world * t.splits * t.split_stride;
+    WeightGradientArgs p = a;
+    p.accumulate = false;
+    for (uint32_t w = 0; w < a.world; ++w) {
+      p.w.c[w] = parts + w * t.splits * t.split_stride;
+      p.w.d[w] = bias_parts + w * t.splits * t.bias_stride;
+    }
+    const hipError_t e = large ? launch<8, 1, 1, 4, 2>(p, t, false, s) : launch<2, 2, 2, 1, 2>(p, t, false, s);
+    if (e != hipSuccess) return e;
+    const uint64_t vecs = (uint64_t(a.features) * a.outputs + 3) / 4 + (a.has_bias ? (a.outputs + 3) / 4 : 0);
+    const dim3 grid(uint32_t((vecs + 255) / 256), a.world);
+    if (a.out_bf16) hipLaunchKernelGGL((k_weight_join<true>), grid, dim3(256), 0, s, a, t, parts, bias_parts);
+    else hipLaunchKernelGGL((k_weight_join<false>), grid, dim3(256), 0, s, a, t, parts, bias_parts);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace caramel

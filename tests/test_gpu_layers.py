@@ -97,7 +97,7 @@ EGRAD = [  # world, tokens, vocab, width, gap, ids
     (1, 1, 1, 1, 0, "one"), (2, 9, 5, 3, 2, "uniform"), (3, 64, 64, 8, 0, "positions"), (8, 65, 100, 17, 1, "skewed"),
     (2, 300, 512, 1000, 0, "padded"), (3, 1025, 2, 1001, 7, "uniform"), (1, 5000, 3000, 64, 0, "skewed"),
     (2, 2000, 7, 260, 4, "one"), (1, 777, 1500, 2500, 0, "uniform"), (64, 40, 30, 24, 0, "uniform"), (2, 100, 50, 16, 0, "padding"),
-    (4, 6000, 1025, 36, 0, "positions")]
+    (4, 6000, 1025, 36, 0, "positions"), (20, 100, 50, 40, 0, "uniform"), (37, 130, 9, 300, 1, "skewed")]
 
 
 @pytest.mark.parametrize("accumulate", [False, True], ids=["write", "add"])
@@ -232,7 +232,8 @@ WGRAD = [  # world, tokens, features, outputs, gap
     (1, 1, 1, 1, 0), (2, 5, 3, 10, 0), (3, 33, 33, 2, 4), (8, 64, 32, 64, 0), (2, 100, 130, 129, 1), (1, 300, 257, 200, 0),
     (2, 31, 784, 256, 0), (1, 1500, 40, 70, 2), (1, 2100, 300, 131, 3), (64, 20, 17, 12, 0), (8, 260, 1100, 1060, 0),
     (8, 289, 1030, 1301, 0), (12, 2050, 500, 510, 0), (12, 2050, 500, 511, 1), (2, 190, 70, 1, 0), (2, 230, 70, 1, 3),
-    (1, 64, 1000, 130, 0), (3, 192, 40, 300, 2)]
+    (1, 64, 1000, 130, 0), (3, 192, 40, 300, 2),
+    (20, 600, 40, 70, 0), (33, 225, 130, 50, 1)]
 TYPES = [(cm.F32, cm.F32), (cm.BF16, cm.BF16), (cm.BF16, cm.F32), (cm.F32, cm.BF16)]
 
 
