@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
 // fp32 (134 MB): 8 + 22 + 5.
 
 constexpr int kSortWaves = 16;
-constexpr int kSortAhead = 4;          // ids per lane that are fetched at once
+constexpr int kSortAhead = 4;          // ids per lane that are fetched at once; up to 4096 tokens they stay in registers
 constexpr uint32_t kSortRange = 1024;  // most ids of a workgroup: one per lane in the scan, 64 KiB of counters
 
 struct Layout {
@@ -287,30 +287,45 @@ __device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64
 constexpr int kSumBlock = 256;
 constexpr int kAhead = 8;  // tokens whose rows are fetched at once
 
-// Clears the rows that no token names: a wavefront looks at `rows` of them, and `lanes` lanes write one.  Streaming stores: with
-// plain ones, the zeros of the pass before are still being written back (8 x 30522 x 1024 bf16, 4096 tokens each: 123 us, 90).
+// Clears those of the rows [first, first + rows) whose bit in `empty` is set; one wavefront, at most 64 rows.  The rows are taken as
+// the one stretch of memory that they are, so that stores are whole and next to each other however wide a row is.  Streaming
+// stores: with plain ones, the zeros of the pass before are still being written back (8 x 30522 x 1024 bf16, 4096 tokens
+// each: 123 us, 90).
 template <bool OUT_BF16>
-__device__ __forceinline__ void clear_rows(const EmbeddingGradientArgs& a, const uint32_t* start, uint64_t out, uint32_t first,
-                                           uint32_t rows, uint32_t lanes) {
+__device__ __forceinline__ void clear_rows(uint64_t out, uint32_t width, uint32_t first, uint32_t rows, uint64_t empty) {
   constexpr int OS = OUT_BF16 ? 2 : 4, N = 16 / OS;
-  if (first >= a.vocab) return;
-  const uint32_t lane = threadIdx.x % 64, r = min(first + lane, a.vocab - 1);
-  const uint64_t empty = __ballot(lane < rows && first + lane < a.vocab && start[r] == start[r + 1]);
+  if (!empty) return;
+  const uint64_t base = out + uint64_t(first) * width * OS;
+  const uint32_t total = rows * width, down = 64 * N / width, right = 64 * N % width;
   const float zero[N] = {};
-  for (uint32_t k = lane / lanes; k < rows; k += 64 / lanes) {
-    if (!(empty >> k & 1)) continue;
-    const uint64_t at = out + uint64_t(first + k) * a.width * OS;
-    if (a.width >= N) {
-      for (uint32_t c = lane % lanes * N; c < a.width; c += lanes * N) store_elems<OUT_BF16, N, true>(at + min(c, a.width - N) * OS, zero);
-    } else {
-      for (uint32_t c = lane % lanes; c < a.width; c += lanes) store_elems<OUT_BF16, 1>(at + c * OS, zero);
+  uint32_t e = threadIdx.x % 64 * N, r = e / width, c = e - r * width;
+  for (; e < total; e += 64 * N) {
+    // up to two rows, unless a row is narrower than a store
+    const bool one = empty >> r & 1, other = c + N <= width ? one : empty >> r >> 1 & 1;
+    if (one && other && width >= N && e + N <= total) {
+      store_elems<OUT_BF16, N, true>(base + uint64_t(e) * OS, zero);
+    } else if (one || other || width < N) {
+      uint32_t row = r, col = c;
+      for (uint32_t j = 0; j < N && e + j < total; ++j) {
+        if (empty >> row & 1) store_elems<OUT_BF16, 1>(base + uint64_t(e + j) * OS, zero);
+        if (++col == width) {
+          col = 0;
+          ++row;
+        }
+      }
+    }
+    r += down;
+    c += right;
+    if (c >= width) {
+      c -= width;
+      ++r;
     }
   }
 }
 
 struct SumShape {
-  uint32_t lanes, sum_blocks;       // lanes of a chunk
-  uint32_t clear_lanes, clear_rows;
+  uint32_t lanes, sum_blocks;  // lanes of a chunk
+  uint32_t clear_rows;         // rows that a wavefront looks at, to clear them
 };
 
 // FULL: 64 lanes per chunk, so that the walk along the list is the wavefront's own: its tokens are fetched by one load
@@ -324,7 +339,10 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientAr
   const uint64_t out = a.w.c[w];
   if (blockIdx.x >= h.sum_blocks) {
     const uint32_t wave = ((blockIdx.x - h.sum_blocks) * gridDim.z + blockIdx.z) * (kSumBlock / 64) + threadIdx.x / 64;
-    clear_rows<OUT_BF16>(a, start, out, wave * h.clear_rows, h.clear_rows, h.clear_lanes);
+    const uint32_t first = wave * h.clear_rows;
+    if (first >= a.vocab) return;
+    const uint32_t rows = min(h.clear_rows, a.vocab - first), r = first + min(threadIdx.x % 64, rows - 1);
+    clear_rows<OUT_BF16>(out, a.width, first, rows, __ballot(start[r] == start[r + 1]));
     return;
   }
   const uint32_t at_col = (blockIdx.z * lanes + threadIdx.x % lanes) * N;
@@ -341,6 +359,7 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientAr
   const bool idle = at_col >= a.width;
   const uint64_t dy = a.w.b[w] + uint64_t(c.col) * ES;
   uint32_t list_id = 0, list_token = 0;
+  u32x4 ids = 0, tokens = 0;
   if constexpr (FULL) {  // a chunk is at most 64 tokens
     const uint32_t e = min(c0 + threadIdx.x % 64, c1 - 1);
     list_id = sorted[e];
@@ -348,16 +367,9 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientAr
   } else if (idle) {
     return;
   }
-  auto id_of = [&](uint32_t e) -> uint32_t {
-    if constexpr (FULL) return __builtin_amdgcn_readlane(list_id, e - c0);
-    else return sorted[e];
-  };
-  auto token_of = [&](uint32_t e) -> uint32_t {
-    if constexpr (FULL) return __builtin_amdgcn_readlane(list_token, e - c0);
-    else return order[e];
-  };
+  const uint32_t first_token = FULL ? 0 : order[c0];
   float sum[N] = {};
-  uint32_t row = id_of(c0);
+  uint32_t row = FULL ? __builtin_amdgcn_readlane(list_id, 0) : sorted[c0];
   auto leave = [&](bool cut_end) {
     const bool cut_begin = start[row] < c0;
     if (idle) return;
@@ -374,10 +386,21 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_sum(EmbeddingGradientAr
       uint32_t id[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        // behind the end: the last token again, which is not added
+        // behind the end: a token again, which is not added
         const uint32_t at = min(e + j, c1 - 1);
-        id[j] = id_of(at);
-        fetch(dy + uint64_t(token_of(at)) * a.dy_pitch * ES, x[j]);
+        uint32_t token;
+        if constexpr (FULL) {
+          id[j] = __builtin_amdgcn_readlane(list_id, at - c0);
+          token = __builtin_amdgcn_readlane(list_token, at - c0);
+        } else {
+          if (j % 4 == 0) {  // four of the list at once; the lists' memory goes on to the next 256 bytes
+            ids = *reinterpret_cast<const u32x4*>(sorted + e + j);
+            tokens = *reinterpret_cast<const u32x4*>(order + e + j);
+          }
+          id[j] = ids[j % 4];
+          token = e + j < c1 ? tokens[j % 4] : first_token;
+        }
+        fetch(dy + uint64_t(token) * a.dy_pitch * ES, x[j]);
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -413,7 +436,7 @@ constexpr uint32_t kFew = 64;
 
 template <bool IDS64, bool DY_BF16, bool OUT_BF16>
 __global__ void __launch_bounds__(kSumBlock) k_embedding_few(EmbeddingGradientArgs a, SumShape h) {
-  constexpr int N = DY_BF16 ? 8 : 4, ES = DY_BF16 ? 2 : 4, OS = OUT_BF16 ? 2 : 4, Z = 16 / OS;
+  constexpr int N = DY_BF16 ? 8 : 4, ES = DY_BF16 ? 2 : 4;
   const uint32_t w = blockIdx.y, n = a.w.tokens[w], lane = threadIdx.x % 64;
   const uint32_t row0 = uniform((blockIdx.x * (kSumBlock / 64) + threadIdx.x / 64) * h.clear_rows);
   if (row0 >= a.vocab) return;
@@ -425,18 +448,8 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_few(EmbeddingGradientAr
   uint64_t named = 0;
   for (uint64_t left = mine; left; left &= left - 1) named |= uint64_t(1) << (__builtin_amdgcn_readlane(id, __ffsll((unsigned long long)left) - 1) - row0);
   if (!a.accumulate) {
-    const float zero[Z] = {};
-    const uint32_t share = (rows + gridDim.z - 1) / gridDim.z, last = min((blockIdx.z + 1) * share, rows);
-    for (uint32_t k = blockIdx.z * share + lane / h.clear_lanes; k < last; k += 64 / h.clear_lanes) {
-      if (named >> k & 1) continue;
-      const uint64_t at = out + uint64_t(row0 + k) * a.width * OS;
-      if (a.width >= Z) {
-        for (uint32_t c = lane % h.clear_lanes * Z; c < a.width; c += h.clear_lanes * Z)
-          store_elems<OUT_BF16, Z, true>(at + min(c, a.width - Z) * OS, zero);
-      } else {
-        for (uint32_t c = lane % h.clear_lanes; c < a.width; c += h.clear_lanes) store_elems<OUT_BF16, 1>(at + c * OS, zero);
-      }
-    }
+    const uint32_t share = (rows + gridDim.z - 1) / gridDim.z, from = min(blockIdx.z * share, rows);
+    if (from < rows) clear_rows<OUT_BF16>(out, a.width, row0 + from, min(share, rows - from), ~named >> from);
   }
   const uint32_t at_col = (blockIdx.z * 64 + lane) * N;
   if (!mine || (blockIdx.z * 64) * N >= a.width) return;
@@ -481,7 +494,9 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_few(EmbeddingGradientAr
   }
 }
 
-constexpr int kJoinWaves = 8;
+// Most chunks have nothing to join, so workgroups are small: 8 x 4096 tokens of 30522 words four wavefronts 4.8 us, eight 6.3; all
+// on two rows 5.5 and 5.8, two wavefronts 7.0.
+constexpr int kJoinWaves = 4;
 
 // One workgroup per chunk and 256 columns; it works if a row begins in the chunk and runs past its end.  The
 // wavefronts take equal stretches of that row's partial sums.
@@ -503,7 +518,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_join(EmbeddingGra
   const uint32_t p0 = min(wave * share, pieces), p1 = min(p0 + share, pieces);
   const uint64_t partial = reinterpret_cast<uint64_t>(ws + l.partial) + uint64_t(c.col) * 4;
   float sum[4] = {};
-#pragma unroll 4
+#pragma unroll 8
   for (uint32_t p = p0; p < p1; ++p) {
     // the first piece lies in the second place of its chunk, the others in the first
     const uint64_t at = partial + (uint64_t(chunk + p) * 2 + (p == 0 ? 1 : 0)) * a.width * 4;
@@ -638,8 +653,7 @@ uint64_t embedding_gradient_workspace(uint32_t world, uint32_t vocab, uint32_t w
 hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& args, const AllWorkers& v, hipStream_t s) {
   if (args.max_tokens == 0 && args.accumulate) return hipSuccess;
   SumShape h{};
-  h.clear_lanes = lanes_for(args.width, args.out_bf16 ? 8 : 4, 64);
-  h.clear_rows = std::min(64u, 1024 / h.clear_lanes);
+  h.clear_rows = std::min(64u, std::max(1u, (32u << 10) / (args.width * (args.out_bf16 ? 2 : 4))));  // 32 KiB
   if (args.max_tokens <= kFew)
     return in_groups(args, v, [&](const EmbeddingGradientArgs& a, uint32_t) { return launch_few(a, h, s); });
   const Layout l = layout(args.all, args.vocab, args.width, args.max_tokens);

@@ -160,65 +160,53 @@ __device__ __forceinline__ uint32_t widen_two(uint32_t codes, int upper, float s
 }
 
 // 32 features of this lane's outputs n (y0) and n + 1 (y1): a lane of the first half holds features 8 (r / 4) + r % 4, one of the
-// second half those 4 further on.  off: of the first of them; left: outputs from n on; even: every row starts on a pair.
-// AUX: cache policy of the stores (2: streaming).
+// second half those 4 further on.  off: of the first of them; left: outputs from n on; ends_odd: the tile holds the last
+// output of an odd number of them, which is stored by itself.  (Pairs may lie on any element.)  AUX: cache policy of the stores (2:
+// streaming).
 template <bool OUT_BF16, int AUX>
-__device__ __forceinline__ void write_strip(__amdgpu_buffer_rsrc_t ro, uint32_t off, uint32_t left, uint32_t out_row, bool even,
+__device__ __forceinline__ void write_strip(__amdgpu_buffer_rsrc_t ro, uint32_t off, uint32_t left, uint32_t out_row, bool ends_odd,
                                             bool accumulate, f32x16 y0, f32x16 y1) {
-  constexpr int OS = OUT_BF16 ? 2 : 4;
-  // lanes behind the last output get an offset that the range check drops
-  const uint32_t at0 = left > 0 ? off : kNowhere, at1 = left > 1 ? off + OS : kNowhere;
+  // lanes that have nothing to store get an offset that the range check drops
+  const uint32_t pair = left > 1 ? off : kNowhere, single = left == 1 ? off : kNowhere;
   auto row = [&](int r) { return (8 * (r / 4) + r % 4) * out_row; };
-  if (even) {
-    if constexpr (OUT_BF16) {
-      if (accumulate) {
-        uint32_t old[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b32(ro, int(at0 + row(r)), 0, 0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          y0[r] += bf16_low(old[r]);
-          y1[r] += bf16_high(old[r]);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) __builtin_amdgcn_raw_buffer_store_b32(bf16_pair(y0[r], y1[r]), ro, int(at0 + row(r)), 0, AUX);
-    } else {
-      if (accumulate) {
-        u32x2 old[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) old[r] = __builtin_amdgcn_raw_buffer_load_b64(ro, int(at0 + row(r)), 0, 0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          y0[r] += as_float(old[r][0]);
-          y1[r] += as_float(old[r][1]);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        __builtin_amdgcn_raw_buffer_store_b64(u32x2{as_bits(y0[r]), as_bits(y1[r])}, ro, int(at0 + row(r)), 0, AUX);
-    }
-  } else {
-    // rows start on any element: one by one
+  if (accumulate) {
+    u32x2 old[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int p0 = int(at0 + row(r)), p1 = int(at1 + row(r));
       if constexpr (OUT_BF16) {
-        if (accumulate) {
-          y0[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p0, 0, 0)));
-          y1[r] += bf16_low(uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, p1, 0, 0)));
-        }
-        const uint32_t v = bf16_pair(y0[r], y1[r]);
-        __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v), ro, p0, 0, AUX);
-        __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v >> 16), ro, p1, 0, AUX);
+        const uint32_t v = __builtin_amdgcn_raw_buffer_load_b32(ro, int(pair + row(r)), 0, 0);
+        old[r] = u32x2{v << 16, v & 0xFFFF0000u};
       } else {
-        if (accumulate) {
-          y0[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p0, 0, 0));
-          y1[r] += as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, p1, 0, 0));
-        }
-        __builtin_amdgcn_raw_buffer_store_b32(as_bits(y0[r]), ro, p0, 0, AUX);
-        __builtin_amdgcn_raw_buffer_store_b32(as_bits(y1[r]), ro, p1, 0, AUX);
+        old[r] = __builtin_amdgcn_raw_buffer_load_b64(ro, int(pair + row(r)), 0, 0);
       }
+    }
+    if (ends_odd) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (OUT_BF16) old[r][0] |= uint32_t(__builtin_amdgcn_raw_buffer_load_b16(ro, int(single + row(r)), 0, 0)) << 16;
+        else old[r][0] |= __builtin_amdgcn_raw_buffer_load_b32(ro, int(single + row(r)), 0, 0);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      y0[r] += as_float(old[r][0]);
+      y1[r] += as_float(old[r][1]);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if constexpr (OUT_BF16)
+      __builtin_amdgcn_raw_buffer_store_b32(bf16_pair(y0[r], y1[r]), ro, int(pair + row(r)), 0, AUX);
+    else
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2{as_bits(y0[r]), as_bits(y1[r])}, ro, int(pair + row(r)), 0, AUX);
+  }
+  if (ends_odd) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (OUT_BF16)
+        __builtin_amdgcn_raw_buffer_store_b16(uint16_t(bf16_pair(y0[r], y0[r])), ro, int(single + row(r)), 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b32(as_bits(y0[r]), ro, int(single + row(r)), 0, 0);
     }
   }
 }
@@ -417,7 +405,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
     for (int c = 0; c < TB; ++c) {
       const uint32_t col = ((wn * TB + c) * 32 + l32) * 2;
       const uint32_t left = n0 + col < N ? N - n0 - col : 0;
-      write_strip<OUT_BF16, 0>(ro, ((wk * FK + f) * 32 + 4 * half) * out_row + col * OS, left, out_row, N % 2 == 0, a.accumulate,
+      write_strip<OUT_BF16, 0>(ro, ((wk * FK + f) * 32 + 4 * half) * out_row + col * OS, left, out_row, N % 2 && n0 + TN >= N, a.accumulate,
                             acc[f][2 * c], acc[f][2 * c + 1]);
     }
 
@@ -431,12 +419,14 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
 // Few tokens: what is written outweighs the product.  A workgroup keeps dy of all tokens in LDS, 128 outputs of it, and goes
 // along the features, each wavefront by itself, 32 features at a time: codes come in and sums go out without a barrier.
 // Bound: HBM writes.  2 x (64 tokens, 25088 x 4096) fp32, 822 MB: 149 us, and 256 in the tiles of the other kernel; with plain stores
-// 172, with three workgroups per compute unit 187, with workgroups for three rounds 158.
+// 172, with three workgroups per compute unit 187, with workgroups for three rounds 158.  STREAM: streaming stores, where rows are
+// whole cache lines and all tensors together are more than the last-level cache holds; 4 x (14 tokens, 2845 x 3365) bf16, 77 MB in rows
+// that are not: 29 us, with streaming stores 62.
 struct ShortTiling {
   uint32_t nn, share;  // tiles along the outputs; steps of 32 features per workgroup
 };
 
-template <int BLOCKS, bool DY_BF16, bool OUT_BF16, Load LOAD>
+template <int BLOCKS, bool DY_BF16, bool OUT_BF16, Load LOAD, bool STREAM>
 __global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradientArgs a, ShortTiling t) {
   constexpr int TN = 128, TB = 2, P = DY_BF16 ? 1 : 3, OS = OUT_BF16 ? 2 : 4;
   __shared__ u32x4 lds[BLOCKS][P][4][TN];
@@ -505,7 +495,7 @@ __global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradient
 #pragma unroll
     for (int c = 0; c < TB; ++c) {
       const uint32_t col = (c * 32 + l32) * 2, left = n0 + col < N ? N - n0 - col : 0;
-      write_strip<OUT_BF16, 2>(ro, 4 * half * out_row + col * OS, left, out_row, N % 2 == 0, a.accumulate, acc[2 * c], acc[2 * c + 1]);
+      write_strip<OUT_BF16, STREAM ? 2 : 0>(ro, 4 * half * out_row + col * OS, left, out_row, N % 2 && n0 + TN >= N, a.accumulate, acc[2 * c], acc[2 * c + 1]);
     }
   }
 
@@ -618,19 +608,37 @@ hipError_t launch_short(const WeightGradientArgs& a, hipStream_t s) {
   t.share = (steps + parts - 1) / parts;
   t.share = (t.share + 3) / 4 * 4;
   const dim3 grid(t.nn * ((steps + t.share - 1) / t.share), a.world), block(256);
-#define CARAMEL_WG(BLOCKS, DY, OUT, LOAD) hipLaunchKernelGGL((k_weight_gradient_short<BLOCKS, DY, OUT, LOAD>), grid, block, 0, s, a, t)
+  const uint64_t row = uint64_t(a.outputs) * (a.out_bf16 ? 2 : 4);
+  const bool stream = row % 128 == 0 && row * a.features * a.all > (uint64_t(256) << 20);
+#define CARAMEL_WG(BLOCKS, DY, OUT, LOAD)                                                                                            \
+  if constexpr (LOAD == kPairs) { /* the others' rows are no whole lines */                                                          \
+    if (stream) hipLaunchKernelGGL((k_weight_gradient_short<BLOCKS, DY, OUT, LOAD, true>), grid, block, 0, s, a, t);                 \
+    else hipLaunchKernelGGL((k_weight_gradient_short<BLOCKS, DY, OUT, LOAD, false>), grid, block, 0, s, a, t);                       \
+  } else {                                                                                                                           \
+    hipLaunchKernelGGL((k_weight_gradient_short<BLOCKS, DY, OUT, LOAD, false>), grid, block, 0, s, a, t);                            \
+  }
   if (!a.dy_bf16) {
-    if (a.out_bf16) CARAMEL_WG(2, false, true, kPairs);
-    else CARAMEL_WG(2, false, false, kPairs);
+    if (a.out_bf16) {
+      CARAMEL_WG(2, false, true, kPairs)
+    } else {
+      CARAMEL_WG(2, false, false, kPairs)
+    }
   } else if (a.outputs % 2 == 0) {
-    if (a.out_bf16) CARAMEL_WG(6, true, true, kPairs);
-    else CARAMEL_WG(6, true, false, kPairs);
+    if (a.out_bf16) {
+      CARAMEL_WG(6, true, true, kPairs)
+    } else {
+      CARAMEL_WG(6, true, false, kPairs)
+    }
   } else if (a.outputs > 1) {
-    if (a.out_bf16) CARAMEL_WG(6, true, true, kShift);
-    else CARAMEL_WG(6, true, false, kShift);
+    if (a.out_bf16) {
+      CARAMEL_WG(6, true, true, kShift)
+    } else {
+      CARAMEL_WG(6, true, false, kShift)
+    }
+  } else if (a.out_bf16) {
+    CARAMEL_WG(6, true, true, kSingle)
   } else {
-    if (a.out_bf16) CARAMEL_WG(6, true, true, kSingle);
-    else CARAMEL_WG(6, true, false, kSingle);
+    CARAMEL_WG(6, true, false, kSingle)
   }
 #undef CARAMEL_WG
   return hipGetLastError();

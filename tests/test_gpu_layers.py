@@ -455,6 +455,20 @@ def test_a_captured_training_step_replays(dtype):
     other.plan.close()
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+def test_weight_gradient_of_few_tokens_and_large_tensors(dtype):
+    """More than the last-level cache holds: streaming stores."""
+    rng = np.random.default_rng(12)
+    n, k, outputs = 40, 9000, 8192 if dtype == cm.F32 else 16384
+    plan, grads = bound_plan(1, [k * outputs], dtype)
+    x, d = whole(rng, n, k), torch.tensor(rng.integers(-8, 9, (n, outputs)).astype(np.float32)).to(TORCH[dtype])
+    saved, dy = saved_checkpoints([x]), d.to(DEV)
+    plan.weight_gradient(0, None, addresses(saved), [n], k, [dy.data_ptr()], None, 0, stream=stream())
+    want = (torch.tensor(x.T, dtype=torch.float32, device=DEV) @ d.float().to(DEV)).to(TORCH[dtype])       # integers: exact
+    assert torch.equal(grads[0][0].view(k, outputs), want)
+    plan.close()
+
+
 def test_overlap_with_the_bound_tensors_is_refused():
     plan, grads = bound_plan(1, [64 * 32], cm.F32)
     ids = torch.zeros(4, dtype=torch.int64, device=DEV)
