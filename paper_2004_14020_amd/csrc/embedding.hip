@@ -91,12 +91,13 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
 //                      Rows cut by a chunk's border leave partial sums.  Other workgroups clear the rows that
 //                      no token names.
 //   k_embedding_join   adds the partial sums of the rows that were cut, in the chunks' order.
-// Bound: HBM, most of all the zeros.  8 x 4096 tokens, 30522 x 1024 bf16 (567 MB): 12 + 91 + 6 us; all tokens on two rows of 1024
-// fp32 (134 MB): 8 + 22 + 5.
+// Bound: HBM, most of all the zeros.  8 x 4096 tokens, 30522 x 1024 bf16 (567 MB): 11 + 86 + 6 us; all tokens on two rows of 1024
+// fp32 (134 MB): 7 + 22 + 6.
 
 constexpr int kSortWaves = 16;
 constexpr int kSortAhead = 4;          // ids per lane that are fetched at once; up to 4096 tokens they stay in registers
-constexpr uint32_t kSortRange = 1024;  // most ids of a workgroup: one per lane in the scan, 64 KiB of counters
+constexpr uint32_t kSortRange = 1008;  // most ids of a workgroup: one per lane in the scan; two workgroups' LDS to a compute unit
+constexpr uint32_t kSortHeld = 128;    // tokens that a wavefront gathers before it ranks 64 of them
 
 struct Layout {
   uint64_t start, order, sorted, partial, stride;  // bytes; stride from worker to worker
@@ -107,8 +108,11 @@ struct Layout {
 Layout layout(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_tokens) {
   auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
   Layout l{};
-  // sums and joining, 8 x 4096 tokens of 1024 bf16: 32 to a chunk 91 + 6 us, 16 87 + 10; 4 x 2050 of 1001: 8 8.0 + 5.8, 16 9.9 + 3.9
-  l.chunk = uint64_t(world) * max_tokens >= 16384 ? 32 : 8;
+  // Short chunks give more wavefronts to the sums, long ones cut fewer rows.  Sums and joining, chunks of 8, 16 and 32: 4 x 2050 tokens
+  // of 1001 bf16 and fp32 8.3 + 4.4, 9.8 + 3.8 us, -; 8 x 4096 tokens of 1024, bf16, 30522 rows 83 + 10, 86 + 6.4, 91 + 4.9; on two
+  // rows (every chunk is cut), fp32 23 + 14, 23 + 9, 22 + 6; 16 x 7400 tokens of 105, bf16, 2759 rows 16 + 12, 15 + 7.7, 22 + 5.4.
+  const bool many = uint64_t(world) * max_tokens >= 16384;
+  l.chunk = !many ? 8 : max_tokens / 32 < vocab ? 16 : 32;
   l.chunks = (max_tokens + l.chunk - 1) / l.chunk;
   l.start = 0;
   l.order = up((uint64_t(vocab) + 1) * 4);
@@ -129,32 +133,40 @@ __device__ __forceinline__ uint32_t read_id(uint64_t ids, uint32_t i, uint32_t v
   }
 }
 
-// Bound: latency (a few thousand ids from the caches).  8 x 4096 tokens of 30522 words 12.0 us; with eight wavefronts 15, and with
-// one round per different id among 64 tokens in place of the comparison by bits, and one id in flight per lane, 46.8.
+// Bound: latency (a few thousand ids from the caches), with more tokens the instructions of the workgroup whose ids are the most
+// frequent.  8 x 4096 tokens of 30522 words 11.0 us; with eight wavefronts 15, and with one round per different id among 64 tokens in
+// place of the comparison by bits, and one id in flight per lane, 46.8.  2 x 60000 of 1000 skewed ids 31 us; at least 64 ids to a
+// workgroup in place of 16 43; all tokens ranked as they come, in both passes, 80.
 template <bool IDS64>
 __global__ void __launch_bounds__(64 * kSortWaves) k_embedding_sort(EmbeddingGradientArgs a, Layout l, uint32_t range, uint32_t bits) {
   constexpr uint32_t kLanes = 64 * kSortWaves, kNone = 0xFFFFFFFFu;
   __shared__ uint32_t count[kSortWaves * kSortRange];  // [wave][id - lo]
+  __shared__ uint32_t held[kSortWaves][2][kSortHeld];  // ids' places in the range, tokens
   __shared__ uint32_t sums[2][kSortWaves];
   const uint32_t w = blockIdx.y, n = a.w.tokens[w];
-  const uint32_t lo = blockIdx.x * range, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const uint32_t lo = blockIdx.x * range, lane = threadIdx.x % 64;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint64_t ids = a.w.a[w];
   unsigned char* const ws = a.ws + w * l.stride;
   // each wave has a stretch of the tokens
   const uint32_t part = (n + kLanes - 1) / kLanes * 64;
   const uint32_t begin = min(wave * part, n), end = min(begin + part, n);
-  uint32_t id[kSortAhead];
-  auto fetch = [&](uint32_t i0) {
+  // Between lanes of one wavefront, whose accesses to LDS are done in order.  A volatile access through an ordinary pointer
+  // would wait for global memory too.
+  using Shared = volatile __attribute__((address_space(3))) uint32_t;
+  struct Ids {
+    uint32_t v[kSortAhead];
+  };
+  auto fetch = [&](uint32_t i0) {  // begin < end; past the end the last id, so that no branch parts the loads
+    Ids r;
 #pragma unroll
-    for (int j = 0; j < kSortAhead; ++j) {
-      const uint32_t i = i0 + j * 64 + lane;
-      id[j] = i < end ? read_id<IDS64>(ids, i, a.vocab) : kNone;
-    }
+    for (int j = 0; j < kSortAhead; ++j) r.v[j] = read_id<IDS64>(ids, min(i0 + j * 64 + lane, end - 1), a.vocab);
+    return r;
   };
   // One step of a wavefront's walk: every lane's place among the tokens of its id, in order; the counters move on.
-  volatile uint32_t* const next = count + wave * range;  // one lane moves it on for the others of its wavefront
-  auto rank = [&](uint32_t v) -> uint32_t {
-    const uint32_t key = v - lo;  // kNone - lo is more than any range
+  Shared* const next = (Shared*)(count + wave * range);  // one lane moves it on for the others of its wavefront
+  const uint64_t lower = (uint64_t(1) << lane) - 1;
+  auto rank = [&](uint32_t key) -> uint32_t {
     const bool in = key < range;
     uint64_t same = __ballot(in);
     if (!same) return 0;
@@ -165,22 +177,48 @@ __global__ void __launch_bounds__(64 * kSortWaves) k_embedding_sort(EmbeddingGra
     }
     uint32_t at = 0;
     if (in) {
-      at = next[key] + __popcll(same & ((uint64_t(1) << lane) - 1));
+      at = next[key] + __popcll(same & lower);
       if ((same >> lane) == 1) next[key] = at + 1;  // the last of them
     }
     return at;
   };
-  fetch(begin);
+  // A long stretch: the next ids are fetched before these are used.
+  auto walk = [&](auto visit) {
+    if (begin == end) return;
+    Ids id = fetch(begin);
+    for (uint32_t i0 = begin; i0 < end; i0 += 64 * kSortAhead) {
+      const Ids following = fetch(min(i0 + 64 * kSortAhead, end - 1));
+#pragma unroll
+      for (int j = 0; j < kSortAhead; ++j) {
+        const uint32_t i = i0 + j * 64 + lane;
+        visit(i < end ? id.v[j] : kNone, i);
+      }
+      id = following;
+    }
+  };
+  uint32_t below = 0, place[kSortAhead];
+  const bool kept = part <= 64 * kSortAhead;  // ids and places stay in registers
+  Ids id;
+#pragma unroll
+  for (int j = 0; j < kSortAhead; ++j) id.v[j] = kNone;
+  if (kept && begin < end) {
+    id = fetch(begin);
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) id.v[j] = begin + j * 64 + lane < end ? id.v[j] : kNone;
+  }
   for (uint32_t i = threadIdx.x; i < kSortWaves * range; i += kLanes) count[i] = 0;
   __syncthreads();
-  uint32_t below = 0, place[kSortAhead];
-  for (uint32_t i0 = begin; i0 < end; i0 += 64 * kSortAhead) {
-    if (i0 != begin) fetch(i0);
+  if (kept) {
 #pragma unroll
     for (int j = 0; j < kSortAhead; ++j) {
-      place[j] = rank(id[j]);
-      below += id[j] < lo;
+      place[j] = rank(id.v[j] - lo);
+      below += id.v[j] < lo;
     }
+  } else {
+    walk([&](uint32_t v, uint32_t) {
+      below += v < lo;
+      if (v - lo < range) atomicAdd(count + wave * range + (v - lo), 1u);  // kNone - lo is more than any range
+    });
   }
   for (int d = 32; d; d /= 2) below += __shfl_xor(below, d);
   if (lane == 0) sums[0][wave] = below;
@@ -218,20 +256,42 @@ __global__ void __launch_bounds__(64 * kSortWaves) k_embedding_sort(EmbeddingGra
   // each wave deals out its stretch, in order
   uint32_t* const order = reinterpret_cast<uint32_t*>(ws + l.order);
   uint32_t* const sorted = reinterpret_cast<uint32_t*>(ws + l.sorted);
-  const bool kept = end - begin <= 64 * kSortAhead;  // ids and places are still in registers
-  for (uint32_t i0 = begin; i0 < end; i0 += 64 * kSortAhead) {
-    if (!kept) fetch(i0);
+  if (kept) {
 #pragma unroll
     for (int j = 0; j < kSortAhead; ++j) {
-      const uint32_t key = id[j] - lo;
-      uint32_t to;
-      if (kept) to = key < range ? next[key] + place[j] : 0;
-      else to = rank(id[j]);
+      const uint32_t key = id.v[j] - lo;
       if (key < range) {
-        order[to] = i0 + j * 64 + lane;
-        sorted[to] = id[j];
+        const uint32_t to = next[key] + place[j];
+        order[to] = begin + j * 64 + lane;
+        sorted[to] = id.v[j];
       }
     }
+  } else {
+    // the tokens in the range are gathered first, so that 64 of them are ranked at once
+    Shared* const keys = (Shared*)held[wave][0];
+    Shared* const tokens = (Shared*)held[wave][1];
+    uint32_t total = 0, done = 0;
+    auto deal = [&] {
+      const uint32_t from = (done + lane) % kSortHeld, key = done + lane < total ? keys[from] : kNone, to = rank(key);
+      if (key < range) {
+        order[to] = tokens[from];
+        sorted[to] = lo + key;
+      }
+      done += 64;
+    };
+    walk([&](uint32_t v, uint32_t i) {
+      const uint32_t key = v - lo;
+      const uint64_t in = __ballot(key < range);
+      if (!in) return;
+      if (key < range) {
+        const uint32_t at = (total + __popcll(in & lower)) % kSortHeld;
+        keys[at] = key;
+        tokens[at] = i;
+      }
+      total += __popcll(in);
+      if (total - done >= 64) deal();
+    });
+    if (done < total) deal();
   }
 }
 
@@ -494,8 +554,8 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_few(EmbeddingGradientAr
   }
 }
 
-// Most chunks have nothing to join, so workgroups are small: 8 x 4096 tokens of 30522 words four wavefronts 4.8 us, eight 6.3; all
-// on two rows 5.5 and 5.8, two wavefronts 7.0.
+// Most chunks have nothing to join, so workgroups are small: 8 x 4096 tokens of 30522 words, 32 to a chunk, four wavefronts 4.8 us,
+// eight 6.3; all on two rows 5.5 and 5.8, two wavefronts 7.0.
 constexpr int kJoinWaves = 4;
 
 // One workgroup per chunk and 256 columns; it works if a row begins in the chunk and runs past its end.  The
@@ -576,7 +636,7 @@ hipError_t launch_sorted(const EmbeddingGradientArgs& a, const Layout& l, SumSha
   const uint32_t per_lane = a.dy_bf16 ? 8 : 4;
   // enough workgroups to fill the chip, each with as few ids as that allows
   const uint64_t even = (uint64_t(a.vocab) * a.all + 255) / 256;
-  const uint32_t range = uint32_t(std::min<uint64_t>({kSortRange, std::max<uint64_t>(64, even), a.vocab}));
+  const uint32_t range = uint32_t(std::min<uint64_t>({kSortRange, std::max<uint64_t>(16, even), a.vocab}));
   uint32_t bits = 0;
   while ((1u << bits) < range) ++bits;
   const dim3 sort_grid((a.vocab + range - 1) / range, a.world);

@@ -151,6 +151,14 @@ def test_embedding_gradient(world, n, vocab, width, gap, kind, dy_dtype, dtype, 
     plan.close()
 
 
+@pytest.mark.parametrize("world,n,vocab,width,kind", [(2, 4097, 1, 3, "one"), (1, 12289, 40, 8, "skewed"), (2, 20001, 3, 5, "padded"),
+                                                      (1, 33000, 2100, 9, "skewed"), (3, 8191, 17, 16, "positions"),
+                                                      (1, 70000, 1030, 4, "padded"), (1, 16500, 5000, 70, "skewed")])
+def test_embedding_gradient_of_long_lists(world, n, vocab, width, kind):
+    """More tokens than the sort keeps in registers: they are counted and dealt out in steps."""
+    test_embedding_gradient(world, n, vocab, width, 0, kind, cm.F32, cm.F32, False)
+
+
 def test_embedding_gradient_agrees_with_differences():
     """<gradient, direction> = <dy, what the lookup gives for the direction>: the lookup is linear in the table."""
     rng = np.random.default_rng(5)
