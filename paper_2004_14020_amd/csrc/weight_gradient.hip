@@ -505,7 +505,10 @@ __global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradient
   }
 }
 
-// Adds the parts of the tokens, in order.
+// Adds the parts of the tokens, in order; kJoinAhead of them are fetched at once.  23 parts of 102 x 885: 9.3 us, four at once
+// 11.0; 10 parts of 8 x 2142 x 247 9.9 (four), 9.9 and, sixteen at once, 12.5.
+constexpr int kJoinAhead = 8;
+
 template <bool OUT_BF16>
 __global__ void __launch_bounds__(256) k_weight_join(WeightGradientArgs a, Tiling t, uint64_t parts, uint64_t bias_parts) {
   constexpr int OS = OUT_BF16 ? 2 : 4;
@@ -523,11 +526,14 @@ __global__ void __launch_bounds__(256) k_weight_join(WeightGradientArgs a, Tilin
   }
   if (i + 4 <= end) {
     float sum[4] = {};
-#pragma unroll 4
-    for (uint32_t p = 0; p < t.splits; ++p) {
-      float x[4];
-      load_elems<false, 4>(from + p * stride + i * 4, x);
-      for (int j = 0; j < 4; ++j) sum[j] += x[j];
+    for (uint32_t p = 0; p < t.splits; p += kJoinAhead) {
+      float x[kJoinAhead][4];
+#pragma unroll
+      for (int q = 0; q < kJoinAhead; ++q) load_elems<false, 4>(from + min(p + q, t.splits - 1) * stride + i * 4, x[q]);
+#pragma unroll
+      for (int q = 0; q < kJoinAhead; ++q)
+        if (p + q < t.splits)
+          for (int j = 0; j < 4; ++j) sum[j] += x[q][j];
     }
     if (a.accumulate) {
       float old[4];
@@ -554,7 +560,7 @@ __global__ void __launch_bounds__(256) k_weight_join(WeightGradientArgs a, Tilin
 }
 
 // Which kernel, and in how many parts the tokens are summed.
-enum Kernel { kShort, kSmallTile, kLargeTile };
+enum Kernel { kShort, kNarrowTile, kSmallTile, kLargeTile };
 struct Shape {
   Kernel kernel;
   uint32_t splits;
@@ -564,6 +570,8 @@ struct Shape {
 // little is left for a workgroup to do; else small ones in parts for two rounds of two workgroups per compute unit.  Fewer
 // tiles than compute units: 16384 x 1024 x 1024 fp32, large in 16 parts 94.8 + 11.6 us (joining), small in 8 parts 111.3 + 7.0, in
 // 4 133 + 5, in 16 114 + 12.  More: 8 x (4096 x 1024 x 4096) bf16, large 252 us, small 355.
+// Tiles of 64 outputs in place of 128 where these would be empty in at least a sixth: 16 x (376 x 4610 x 34) fp32 24 us, small 38;
+// 4 x (1580 x 1024 x 320) fp32 34 and 41, of 192 30 and 29; with fewer empty places, 4 x (256 x 1024 x 960), 18 and 16.
 Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_tokens, bool dy_bf16) {
   auto tiles = [&](uint32_t side) { return uint64_t(world) * ((features + side - 1) / side) * ((outputs + side - 1) / side); };
   const uint64_t small = tiles(128), large = tiles(256);
@@ -573,6 +581,9 @@ Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_t
     const uint64_t splits = std::max<uint64_t>(1, std::min(256 / large, blocks / 16));
     if (large * splits >= 192 && blocks >= 8 * splits) return {kLargeTile, uint32_t(splits)};
   }
+  const uint32_t strips = (outputs + 63) / 64;
+  const uint64_t narrow = uint64_t(world) * ((features + 127) / 128) * strips;
+  if (strips % 2 && strips <= 5) return {kNarrowTile, uint32_t(std::max<uint64_t>(1, std::min((1024 + narrow - 1) / narrow, blocks / 8)))};
   return {kSmallTile, uint32_t(std::max<uint64_t>(1, std::min((512 + small - 1) / small, blocks / 8)))};
 }
 
@@ -591,7 +602,7 @@ hipError_t launch(const WeightGradientArgs& a, const Tiling& t, bool out_bf16, h
   } else if (a.outputs > 1) {
     if (out_bf16) CARAMEL_WG(true, true, kShift);
     else CARAMEL_WG(true, false, kShift);
-  } else if constexpr (WK == 2) {  // one output is never worth the large tile
+  } else if constexpr (WK == 2 && WN == 1) {  // one output always goes to narrow tiles
     if (out_bf16) CARAMEL_WG(true, true, kSingle);
     else CARAMEL_WG(true, false, kSingle);
   }
@@ -657,11 +668,10 @@ hipError_t launch_weight_gradient(const WeightGradientArgs& args, const AllWorke
   if (args.max_tokens == 0 && args.accumulate) return hipSuccess;
   const Shape c = choose(args.all, args.features, args.outputs, args.max_tokens, args.dy_bf16);
   if (c.kernel == kShort) return in_groups(args, v, [&](const WeightGradientArgs& a, uint32_t) { return launch_short(a, s); });
-  const bool large = c.kernel == kLargeTile;
-  const uint32_t side = large ? 256 : 128;
+  const uint32_t tk = c.kernel == kLargeTile ? 256 : 128, tn = c.kernel == kNarrowTile ? 64 : tk;
   Tiling t{};
-  t.nk = (args.features + side - 1) / side;
-  t.nn = (args.outputs + side - 1) / side;
+  t.nk = (args.features + tk - 1) / tk;
+  t.nn = (args.outputs + tn - 1) / tn;
   t.splits = c.splits;
   if (c.splits > 1) {
     t.split_stride = up256(uint64_t(args.features) * args.outputs * 4);
@@ -669,7 +679,12 @@ hipError_t launch_weight_gradient(const WeightGradientArgs& args, const AllWorke
   }
   return in_groups(args, v, [&](const WeightGradientArgs& a, uint32_t first) {
     t.total = t.nk * t.nn * t.splits * a.world;
-    if (c.splits == 1) return large ? launch<8, 1, 1, 4, 2>(a, t, a.out_bf16, s) : launch<2, 2, 2, 1, 2>(a, t, a.out_bf16, s);
+    auto tiles = [&](const WeightGradientArgs& to, bool out_bf16) {
+      if (c.kernel == kLargeTile) return launch<8, 1, 1, 4, 2>(to, t, out_bf16, s);
+      if (c.kernel == kSmallTile) return launch<2, 2, 2, 1, 2>(to, t, out_bf16, s);
+      return launch<2, 1, 2, 1, 2>(to, t, out_bf16, s);
+    };
+    if (c.splits == 1) return tiles(a, a.out_bf16);
     const uint64_t parts = reinterpret_cast<uint64_t>(a.ws) + first * t.splits * (t.split_stride + t.bias_stride);
     const uint64_t bias_parts = parts + a.world * t.splits * t.split_stride;
     WeightGradientArgs p = a;
@@ -678,7 +693,7 @@ hipError_t launch_weight_gradient(const WeightGradientArgs& args, const AllWorke
       p.w.c[w] = parts + w * t.splits * t.split_stride;
       p.w.d[w] = bias_parts + w * t.splits * t.bias_stride;
     }
-    const hipError_t e = large ? launch<8, 1, 1, 4, 2>(p, t, false, s) : launch<2, 2, 2, 1, 2>(p, t, false, s);
+    const hipError_t e = tiles(p, false);
     if (e != hipSuccess) return e;
     const uint64_t vecs = (uint64_t(a.features) * a.outputs + 3) / 4 + (a.has_bias ? (a.outputs + 3) / 4 : 0);
     const dim3 grid(uint32_t((vecs + 255) / 256), a.world);
