@@ -21,6 +21,7 @@
 // of the operand.  The tokens are dealt to the operand's places in the same permuted order on both sides.
 // Outputs are dealt to lanes in pairs, so that a lane ends with two neighbours to store.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "layers.hpp"
@@ -567,7 +568,7 @@ struct Shape {
 };
 
 // Large tiles, in as many parts of the tokens as fill the chip once, unless their ragged ends waste a quarter of the work or too
-// little is left for a workgroup to do; else small ones in parts for two rounds of two workgroups per compute unit.  Fewer
+// little is left for a workgroup to do; else small ones in parts for at most one round of two workgroups per compute unit.  Fewer
 // tiles than compute units: 16384 x 1024 x 1024 fp32, large in 16 parts 94.8 + 11.6 us (joining), small in 8 parts 111.3 + 7.0, in
 // 4 133 + 5, in 16 114 + 12.  More: 8 x (4096 x 1024 x 4096) bf16, large 252 us, small 355.
 // Tiles of 64 outputs in place of 128 where these would be empty in at least a sixth: 16 x (376 x 4610 x 34) fp32 24 us, small 38;
@@ -581,10 +582,18 @@ Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_t
     const uint64_t splits = std::max<uint64_t>(1, std::min(256 / large, blocks / 16));
     if (large * splits >= 192 && blocks >= 8 * splits) return {kLargeTile, uint32_t(splits)};
   }
+  // A part more takes time off the walk along the tokens (half a microsecond a block) and adds its sums' way to memory and back (at 4
+  // TB/s); their total is least at the root.  3 x (1430 x 426 x 848) bf16 22 us, with all parts of at least eight blocks 25; 11964 x
+  // 102 x 885 22 and 26; 4 x (1024 x 1024 x 1000) fp32 41 and 49; 8 x (512 x 784 x 10) 11 and 14.  More than 64 parts are joined too
+  // slowly: 16384 x 64 x 64 fp32 18 us, with 128 20.
+  auto parts = [&](uint64_t fill) {
+    const uint64_t best = std::llround(std::sqrt(0.25e6 * double(blocks) / (double(world) * features * outputs)));
+    return uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({fill, blocks / 4, best, 64})));
+  };
   const uint32_t strips = (outputs + 63) / 64;
   const uint64_t narrow = uint64_t(world) * ((features + 127) / 128) * strips;
-  if (strips % 2 && strips <= 5) return {kNarrowTile, uint32_t(std::max<uint64_t>(1, std::min((1024 + narrow - 1) / narrow, blocks / 8)))};
-  return {kSmallTile, uint32_t(std::max<uint64_t>(1, std::min((512 + small - 1) / small, blocks / 8)))};
+  if (strips % 2 && strips <= 5) return {kNarrowTile, parts((1024 + narrow - 1) / narrow)};
+  return {kSmallTile, parts((512 + small - 1) / small)};
 }
 
 uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
