@@ -2,8 +2,8 @@
 //
 // A block is 32 consecutive tokens of one feature.  With a = its largest magnitude and e the smallest
 // exponent >= -126 for which a <= 127 * 2^e, a value x is kept as q = round(x / 2^e), ties to even, |q| <= 127,
-// and read back as q * 2^e.  (e stops at 121, so that 127 * 2^e is still a number: what lies above is kept as 127.)  The scale is a power of two, so that every value that is read back is a bf16
-// number: the weight gradient feeds the matrix cores with it without another rounding.  A block that holds
+// and read back as q * 2^e.  (e stops at 121, so that 127 * 2^e is still a number: what lies above is
+// kept as 127.)  The scale is a power of two, so that every value that is read back is a bf16 number: the weight gradient feeds the matrix cores with it without another rounding.  A block that holds
 // an infinity or a NaN is marked and reads back as NaN throughout.  One scale per feature (not per token)
 // keeps the few features that are much larger than the rest from taking the others' bits.
 //
