@@ -582,13 +582,13 @@ Shape choose(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_t
     const uint64_t splits = std::max<uint64_t>(1, std::min(256 / large, blocks / 16));
     if (large * splits >= 192 && blocks >= 8 * splits) return {kLargeTile, uint32_t(splits)};
   }
-  // A part more takes time off the walk along the tokens (half a microsecond a block) and adds its sums' way to memory and back (at 4
-  // TB/s); their total is least at the root.  3 x (1430 x 426 x 848) bf16 22 us, with all parts of at least eight blocks 25; 11964 x
-  // 102 x 885 22 and 26; 4 x (1024 x 1024 x 1000) fp32 41 and 49; 8 x (512 x 784 x 10) 11 and 14.  More than 64 parts are joined too
-  // slowly: 16384 x 64 x 64 fp32 18 us, with 128 20.
+  // A part more takes time off the walk along the tokens (0.56 us a block) and adds its sums' way to memory and back (at 4 TB/s) and a
+  // step of the join (0.06 us); their total is least at the root.  3 x (1430 x 426 x 848) bf16 22 us, with as many parts as have eight
+  // blocks 25; 11964 x 102 x 885 22 and 26; 4 x (1024 x 1024 x 1000) fp32 41 and 49; 8 x (512 x 784 x 10) 11 and 14; 2^20 x 64 x 64
+  // fp32 127, with 64 parts 466.
   auto parts = [&](uint64_t fill) {
-    const uint64_t best = std::llround(std::sqrt(0.25e6 * double(blocks) / (double(world) * features * outputs)));
-    return uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({fill, blocks / 4, best, 64})));
+    const uint64_t best = std::llround(std::sqrt(0.28e6 * double(blocks) / (double(world) * features * outputs + 3e4)));
+    return uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({fill, blocks / 4, best})));
   };
   const uint32_t strips = (outputs + 63) / 64;
   const uint64_t narrow = uint64_t(world) * ((features + 127) / 128) * strips;

@@ -296,9 +296,9 @@ def test_weight_gradient(world, n, k, outputs, gap, dy_dtype, dtype, accumulate)
 
 @pytest.mark.parametrize("dy_dtype,dtype", TYPES, ids=["f32", "bf16", "bf16-f32", "f32-bf16"])
 @pytest.mark.parametrize("world,n,k,outputs,gap", [(2, 700, 150, 63, 1), (1, 3000, 129, 319, 0), (3, 520, 64, 33, 5), (17, 390, 515, 64, 0),
-                                                  (1, 6000, 31, 1, 0), (2, 1400, 260, 192, 2), (1, 5900, 100, 200, 0)])
+                                                  (1, 6000, 31, 1, 0), (1, 40000, 20, 9, 1), (2, 1400, 260, 192, 2), (1, 5900, 100, 200, 0)])
 def test_weight_gradient_of_few_outputs(world, n, k, outputs, gap, dy_dtype, dtype):
-    """Outputs that fill no tile of 128, in one part of the tokens and in up to 23."""
+    """Outputs that fill no tile of 128, in one part of the tokens and in many."""
     test_weight_gradient(world, n, k, outputs, gap, dy_dtype, dtype, True)
 
 
