@@ -1,12 +1,13 @@
-"""The kernel variants that large calls of the gradient-filling operators take: all tilings of the weight gradient."""
+"""The kernel variants that large calls of the gradient-filling operators take: all tilings of the weight gradient, the embedding
+gradient of wide rows and long lists, the lookup with streaming stores."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2004_14020_amd as cm
 
-from layer_util import DEV, TORCH, addresses, bound_plan, saved_sparse, stream, untouched, workspace
-from test_gpu_layers import DTYPES, NAMES, counts, dtype_id
+from layer_util import DEV, HALF_STEP, TORCH, addresses, bound_plan, f64, rows, saved_sparse, stream, untouched, workspace
+from test_gpu_layers import DTYPES, NAMES, TYPES, close, counts, dtype_id, make_ids
 
 pytestmark = pytest.mark.gpu
 
@@ -92,4 +93,86 @@ def test_tiles_pass_on_infinities_and_nan(world, n, k, outputs, parts, dy_dtype)
             want[5], want[k - 1] = float("nan"), float("nan")
         for got, ref in ((grads[w][0].view(k, outputs), want), (grads[w][1], bias)):
             assert torch.equal(torch.nan_to_num(got.cpu(), nan=-5.0), torch.nan_to_num(ref, nan=-5.0)), f"worker {w}"
+    plan.close()
+
+
+# ---- embedding gradient: wide rows, chunks of 16 and 32 ----------------------------------------
+@pytest.mark.parametrize("accumulate", [False, True], ids=["write", "add"])
+@pytest.mark.parametrize("dy_dtype,dtype", TYPES, ids=["f32", "bf16", "bf16-f32", "f32-bf16"])
+@pytest.mark.parametrize("world,n,vocab,width,gap,kind", [
+    (4, 4100, 3000, 300, 0, "skewed"), (4, 4111, 2, 300, 3, "uniform"), (4, 4100, 3000, 1001, 0, "padded"), (5, 4099, 2, 1001, 1, "padded"),
+    (1, 17001, 700, 520, 0, "skewed"), (1, 17001, 500, 264, 4, "skewed"), (17, 1000, 29, 1024, 0, "skewed"), (2, 9000, 40, 96, 0, "skewed")])
+def test_embedding_gradient_of_wide_rows_and_many_tokens(world, n, vocab, width, gap, kind, dy_dtype, dtype, accumulate):
+    """From 16384 tokens over all workers on, chunks of 16 tokens (more than tokens / 32 rows) and of 32; rows that many chunks cut."""
+    print(f"case: egrad world={world} n={n} vocab={vocab} width={width} {kind} {NAMES[dy_dtype]}->{NAMES[dtype]}", flush=True)
+    rng = np.random.default_rng(n + width)
+    ns, id_bytes, scale = counts(world, n), 8 if width % 2 else 4, -1.7
+    plan, grads = bound_plan(world, [5, vocab * width, 3], dtype, fill=0.75)
+    ids = [make_ids(kind, rng, m, vocab) for m in ns]
+    di = [torch.tensor(i, dtype=torch.int64 if id_bytes == 8 else torch.int32, device=DEV) for i in ids]
+    need = plan.embedding_workspace(1, width, ns)
+    ws = workspace(need)
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    for exact in (True, False):
+        dy, old = [], 0.75 if accumulate else 0.0
+        for m, i in zip(ns, di):
+            v = (torch.randint(-8, 9, (m, width), device=DEV, generator=gen).float() if exact
+                 else torch.randn(m, width, device=DEV, generator=gen))
+            v[(i < 0) | (i >= vocab)] = float("nan")                                  # padding must not reach any row
+            dy.append(rows(m, width, width + gap, dy_dtype, v))
+        s, first = 2.0 if exact else scale, None
+        for again in range(2):                               # the second time over other leftovers: the same bits
+            ws[:max(need, 16)] = 0x5A if again else 0xFF
+            for row in grads:
+                row[1].fill_(0.75)
+            plan.embedding_gradient(1, width, addresses(di), ns, addresses([d[0] for d in dy]), ws.data_ptr(), need, scale=s,
+                                    id_bytes=id_bytes, dy_dtype=dy_dtype, dy_pitch=width + gap, accumulate=accumulate, stream=stream())
+            torch.cuda.synchronize()
+            assert untouched(ws, need)
+            now = [row[1].clone() for row in grads]
+            assert first is None or all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(first, now))
+            first = now
+        for w in range(world):
+            known = ((di[w] >= 0) & (di[w] < vocab)).nonzero().flatten()
+            at, d = di[w][known].long(), dy[w][1][known].double()
+            zero = torch.zeros(vocab, width, dtype=torch.float64, device=DEV)
+            want = float(np.float32(s)) * zero.index_add(0, at, d) + old
+            got = grads[w][1].view(vocab, width)
+            if exact:                                        # integers below 2^24: exact in fp32 in any order
+                assert torch.equal(got, want.float().to(TORCH[dtype])), f"worker {w}"
+            else:
+                mag = abs(float(np.float32(s))) * zero.index_add(0, at, d.abs())
+                terms = torch.bincount(at, minlength=vocab).double()[:, None]
+                bound = (terms + 2) * 2.0 ** -24 * (mag + old) * (1 + 2.0 ** -10)
+                if dtype == cm.BF16:
+                    bound = bound + HALF_STEP[cm.BF16] * (want.abs() + bound)
+                close(f64(got), f64(want), f64(bound), f"worker {w}")
+            assert bool((grads[w][0] == 0.75).all()) and bool((grads[w][2] == 0.75).all()), "other tensors stay"
+    plan.close()
+
+
+# ---- lookup: more than 32 MiB of output --------------------------------------------------------
+@pytest.mark.parametrize("id_bytes", [4, 8])
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+@pytest.mark.parametrize("world,n,vocab,width,gap", [(3, 9000, 500, 1001, 0), (2, 12001, 70, 1024, 8), (2, 400_000, 1000, 35, 1)])
+def test_lookup_with_streaming_stores(world, n, vocab, width, gap, dtype, id_bytes):
+    print(f"case: lookup world={world} n={n} vocab={vocab} width={width} gap={gap} dtype={NAMES[dtype]}", flush=True)
+    ns, scale = [n] * (world - 1) + [n // 2 + 9], 2.7
+    assert sum(ns) * width * 2 > 32 << 20
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    plan = cm.Plan(world, [1], dtype=dtype)
+    table = [torch.randn(vocab, width, device=DEV, generator=gen).to(TORCH[dtype]) for _ in range(world)]
+    ids = [torch.randint(-2, vocab + 2, (m,), device=DEV, generator=gen).to(torch.int64 if id_bytes == 8 else torch.int32) for m in ns]
+    out = [rows(m, width, width + gap, dtype, fill=7.0) for m in ns]
+    plan.embedding_lookup(addresses(table), vocab, width, addresses(ids), ns, addresses([o[0] for o in out]), scale=scale,
+                          id_bytes=id_bytes, out_pitch=width + gap, stream=stream())
+    torch.cuda.synchronize()
+    for w in range(world):
+        mem, view = out[w]
+        known = (ids[w] >= 0) & (ids[w] < vocab)
+        want = table[w].float()[ids[w].long().clamp(0, vocab - 1)] * torch.tensor(scale, dtype=torch.float32, device=DEV)
+        want = torch.where(known[:, None], want, torch.zeros((), device=DEV)).to(TORCH[dtype])       # one product, one rounding: exact
+        assert torch.equal(view, want), f"worker {w}"
+        view.fill_(7.0)
+        assert bool((mem == 7.0).all()), "the gaps between the rows and what lies behind the last one stay"
     plan.close()
