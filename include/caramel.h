@@ -354,8 +354,9 @@ int caramel_checkpoint_load(caramel_plan* plan, const uint64_t* tokens, uint64_t
 /* Gradients of a dense layer y = x W + b from the checkpoint of its input x and the gradient dy of its output:
  *   grads[w][weight] = x^T dy      features x outputs, where outputs = elements of the tensor / features
  *   grads[w][bias]   = sum of the rows of dy      (bias == CARAMEL_NO_TENSOR: not computed)
- * dy_dtype may differ from the plan's dtype.  The products are exact in both types (an fp32 dy goes through the matrix cores
- * as the sum of three bf16 numbers). */
+ * dy_dtype may differ from the plan's dtype.  A bf16 dy enters the products as it is.  An fp32 dy goes through the matrix cores as the
+ * sum of three bf16 numbers: exactly where it is 0 or at least 2^-110 in magnitude; of smaller values the bits below 2^-133, the smallest
+ * bf16 number, are cut off, so that a product x dy is off by less than 2^-133 |x|.  (The bias takes dy as it is.) */
 #define CARAMEL_NO_TENSOR 0xFFFFFFFFu
 int caramel_weight_gradient_workspace(const caramel_plan* plan, uint32_t weight, uint64_t features, const uint64_t* tokens,
                                       uint64_t* bytes);

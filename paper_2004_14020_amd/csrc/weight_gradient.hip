@@ -3,11 +3,12 @@
 //   dW[k, n] = round([dW[k, n] +] sum over the tokens m of x[m, k] * dy[m, n])
 //   db[n]    = round([db[n] +]    sum over the tokens m of dy[m, n])
 //
-// for all workers of a plan in one launch.  The product runs on the matrix cores in bf16 with fp32 sums, and
-// loses nothing on the way in: a value read back from a checkpoint is a bf16 number (checkpoint.hip), and an
-// fp32 gradient is the sum of three bf16 numbers (24 significant bits, eight each), which go through the
-// matrix cores one after the other.  That is three products instead of one, at 16 times the rate of
-// the fp32 matrix instructions.
+// for all workers of a plan in one launch.  The product runs on the matrix cores in bf16 with fp32 sums.  Nothing is rounded on the
+// way in: a value read back from a checkpoint is a bf16 number (checkpoint.hip), and an fp32 gradient is the sum of three bf16
+// numbers (24 significant bits, eight each), which go through the matrix cores one after the other.  That is three products
+// instead of one, at 16 times the rate of the fp32 matrix instructions.  Below 2^-110 the third number would be smaller than bf16
+// goes: bits under 2^-133 are cut off.  (The matrix cores take subnormal numbers as they are.)  A common power of two cannot help, as
+// both x and dy may lie anywhere in fp32's range, and finding one for each tile would be another pass over dy.
 //
 // Bound: the matrix cores.  8 x (4096 tokens, 1024 x 4096) bf16 251 us = 1094 TFLOP/s, against 1265 of a library product of 8192^3
 // and 676 of one of this shape; 16384 tokens, 1024 x 1024 fp32 95 us + 12 for joining its 16 parts (three products: 1085
@@ -129,7 +130,7 @@ struct Dy {
 #pragma unroll
         for (int j = 0; j < 8; ++j) bias[odd] += odd ? bf16_high(in[j]) : bf16_low(in[j]);
     } else {
-      // v = hi + mid + lo: the upper half of a float is a bf16 number, and the rest is exact
+      // v = hi + mid + lo: the upper half of a float is a bf16 number, and the rest is exact; lo's lower half is 0 from 2^-110 on
       const int d = n % 4;
       uint32_t part[3][2];
 #pragma unroll

@@ -61,6 +61,24 @@ def test_tiles_lose_no_bit_of_fp32_gradients(world, n, k, outputs, parts, dtype)
         assert torch.equal(grads[w].view(k, outputs).cpu(), want.to(TORCH[dtype])), f"worker {w}"
 
 
+@pytest.mark.parametrize("world,n,k,outputs", [(1, 50, 150, 64)] + [t[:4] for t in TILES.values()], ids=["few-tokens", *TILES])
+def test_tiny_fp32_gradients_lose_only_what_lies_below_bf16(world, n, k, outputs):
+    """From 2^-110 on a product is exact; below, dy's bits under 2^-133 are cut off.  x >= 1, so that no product is subnormal for x's
+    sake alone."""
+    print(f"case: tiny dy, world={world} n={n} k={k} outputs={outputs}", flush=True)
+    rng = np.random.default_rng(n + k)
+    dv = [(rng.choice([-1, 1], (m, outputs)) * 2.0 ** rng.uniform(-149, -100, (m, outputs))).astype(np.float32) for m in counts(world, n)]
+    grads, placed, _ = sparse_gradient(rng, world, n, k, outputs, cm.F32, dv, (0, 100))
+    for w, v in enumerate(dv):
+        if len(v) == 0:
+            assert not bool(grads[w].any())
+            continue
+        at, x = placed[w]
+        v, x, got = v[at].astype(np.float64), x[:, None], f64(grads[w]).reshape(k, outputs)
+        assert np.array_equal(got[np.abs(v) >= 2.0 ** -110], (v * x)[np.abs(v) >= 2.0 ** -110])
+        assert (np.abs(got - v * x) < 2.0 ** -133 * x).all()
+
+
 @pytest.mark.parametrize("dy_dtype", DTYPES, ids=dtype_id)
 @tiles()
 def test_tiles_pass_on_infinities_and_nan(world, n, k, outputs, parts, dy_dtype):
