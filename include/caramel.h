@@ -308,9 +308,10 @@ int caramel_allreduce_static(caramel_plan* plan, void* const* grads, void* strea
  * All calls are asynchronous on `stream`, allocate nothing, upload nothing and issue only kernel
  * launches, so they can be captured.  Rows are `pitch` elements apart and may start on any element.  Buffers
  * that a call writes must not overlap any other buffer of the call (EINVAL).  Sums are fp32 in an order that
- * depends on the sizes alone, so results are reproducible bit for bit; each result is rounded once.
+ * depends on the sizes alone, so results are reproducible bit for bit; what is done with a sum (scaling, adding) is one fp32
+ * operation, whose result is rounded to bf16 where the tensor is.
  * Gradients are written; with `accumulate` they are added to what the tensor holds (micro-batches, tied
- * weights), in one rounding.  The two gradient calls need a workspace: its size depends on the sizes given, its contents
+ * weights).  The two gradient calls need a workspace: its size depends on the sizes given, its contents
  * need not be kept from call to call, and calls that may run at the same time need one each.
  * EINVAL: NULL or misaligned pointers (to the element, unless stated), more than 2^25 tokens, 2^20 columns, a
  * pitch below the columns or above 2^23, 2^38 values at a worker, a workspace that is too small.  ESTATE: the plan is

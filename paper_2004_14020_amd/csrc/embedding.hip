@@ -325,7 +325,7 @@ __device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64
     float y[N];
     if (a.accumulate) {
       load_elems<OUT_BF16, N>(at, y);
-      for (int j = 0; j < N; ++j) y[j] += a.scale * sum[j];
+      for (int j = 0; j < N; ++j) y[j] = __builtin_fmaf(a.scale, sum[j], y[j]);  // one rounding
     } else {
       for (int j = 0; j < N; ++j) y[j] = a.scale * sum[j];
     }
@@ -334,10 +334,11 @@ __device__ __forceinline__ void write_row(const EmbeddingGradientArgs& a, uint64
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if (uint32_t(j) < c.twice || uint32_t(j) >= c.count) continue;
-      float y = a.scale * sum[j], old = 0.0f;
+      float y = a.scale * sum[j];
       if (a.accumulate) {
+        float old;
         load_elems<OUT_BF16, 1>(at + j * ES, &old);
-        y += old;
+        y = __builtin_fmaf(a.scale, sum[j], old);
       }
       store_elems<OUT_BF16, 1>(at + j * ES, &y);
     }

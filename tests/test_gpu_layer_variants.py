@@ -169,6 +169,29 @@ def test_embedding_gradient_of_wide_rows_and_many_tokens(world, n, vocab, width,
     plan.close()
 
 
+@pytest.mark.parametrize("n,vocab,width", [(50, 30, 20), (50, 30, 3), (300, 200, 300), (300, 200, 33), (3000, 3, 301), (3000, 3, 2)])
+@pytest.mark.parametrize("dy_dtype,dtype", TYPES, ids=["f32", "bf16", "bf16-f32", "f32-bf16"])
+def test_accumulating_rounds_once(n, vocab, width, dy_dtype, dtype):
+    """old + scale * sum in one rounding to fp32, for rows of few tokens, of a sorted list, and cut by chunks.  Sums of integers, a
+    scale and old values of 24 bits in [1, 2): in 64 bits all of it is exact."""
+    print(f"case: accumulate once, n={n} vocab={vocab} width={width} {NAMES[dy_dtype]}->{NAMES[dtype]}", flush=True)
+    rng = np.random.default_rng(n + width)
+    plan, grads = bound_plan(1, [vocab * width], dtype)
+    ids = torch.tensor(rng.integers(0, vocab, n), device=DEV)
+    dy = torch.tensor(rng.integers(-8, 9, (n, width)).astype(np.float32), device=DEV).to(TORCH[dy_dtype])
+    old = torch.tensor((1 + rng.random(vocab * width)).astype(np.float32), device=DEV).to(TORCH[dtype])
+    grads[0][0].copy_(old)
+    scale = float(np.float32(1.7))
+    need = plan.embedding_workspace(0, width, [n])
+    ws = workspace(need)
+    plan.embedding_gradient(0, width, [ids.data_ptr()], [n], [dy.data_ptr()], ws.data_ptr(), need, scale=scale, dy_dtype=dy_dtype,
+                            accumulate=True, stream=stream())
+    total = torch.zeros(vocab, width, dtype=torch.float64, device=DEV).index_add(0, ids, dy.double())
+    want = (old.double().view(vocab, width) + scale * total).float().to(TORCH[dtype])
+    assert torch.equal(grads[0][0].view(vocab, width), want)
+    plan.close()
+
+
 # ---- lookup: more than 32 MiB of output --------------------------------------------------------
 @pytest.mark.parametrize("id_bytes", [4, 8])
 @pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
