@@ -305,7 +305,7 @@ int caramel_allreduce_static(caramel_plan* plan, void* const* grads, void* strea
  * differ and may be 0 (such a worker's pointers are not looked at).  The plan may be used for the aggregation,
  * in any order on one stream, between such calls.
  *
- * All calls are asynchronous on `stream`, allocate nothing, upload nothing and issue only kernel
+ * All calls are asynchronous on `stream`, allocate nothing (no device memory, no host memory of their own), upload nothing and issue only kernel
  * launches, so they can be captured.  Rows are `pitch` elements apart and may start on any element.  Buffers
  * that a call writes must not overlap any other buffer of the call (EINVAL).  Sums are fp32 in an order that
  * depends on the sizes alone, so results are reproducible bit for bit; what is done with a sum (scaling, adding) is one fp32

@@ -1088,16 +1088,17 @@ struct Memory {
     uint64_t lo, hi;
     bool written;
   };
-  std::vector<Span> spans;
+  Span spans[4 * CARAMEL_MAX_WORLD + 1];  // four buffers of every worker, and a workspace
+  uint32_t n = 0;
 
-  explicit Memory(uint32_t world) { spans.reserve(4 * world + 1); }
   void add(uint64_t at, uint64_t bytes, bool written) {
-    if (bytes) spans.push_back({at, at + bytes, written});
+    if (bytes) spans[n++] = {at, at + bytes, written};
   }
   int check() {
-    std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.lo < y.lo; });
+    std::sort(spans, spans + n, [](const Span& x, const Span& y) { return x.lo < y.lo; });
     uint64_t any = 0, written = 0;  // how far what came before reaches
-    for (const Span& s : spans) {
+    for (uint32_t i = 0; i < n; ++i) {
+      const Span& s = spans[i];
       if (s.lo < written || (s.written && s.lo < any)) return fail(CARAMEL_EINVAL, "buffers overlap with one that is written");
       any = std::max(any, s.hi);
       if (s.written) written = std::max(written, s.hi);
@@ -1196,7 +1197,7 @@ int embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, 
   if (int rc = take_pointers(p, "ids", ids, v.tokens, id_bytes, v.b)) return rc;
   if (int rc = take_pointers(p, "out", out, v.tokens, es, v.c)) return rc;
   a.all = p->host.cfg.world;
-  Memory m(a.all);
+  Memory m;
   for (uint32_t w = 0; w < a.all; ++w) {
     if (!v.tokens[w]) continue;
     m.add(v.a[w], vocab * width * es, false);
@@ -1249,7 +1250,7 @@ int embedding_gradient(caramel_plan* p, uint32_t tensor, uint64_t width, float s
   const uint64_t need = embedding_gradient_workspace(a.all, uint32_t(vocab), uint32_t(width), a.max_tokens);
   if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
   if (int rc = need_bound(p, false)) return rc;
-  Memory m(a.all);
+  Memory m;
   m.add(reinterpret_cast<uint64_t>(ws), need, true);
   for (uint32_t w = 0; w < a.all; ++w) {
     v.c[w] = p->bind.rows[tensor * a.all + w];
@@ -1287,7 +1288,7 @@ int checkpoint_call(caramel_plan* p, bool store, const uint64_t* tokens, uint64_
   if (int rc = take_pointers(p, "x", x, v.tokens, es, v.a)) return rc;
   if (int rc = take_pointers(p, "checkpoint", checkpoint, v.tokens, 16, v.b)) return rc;
   a.all = p->host.cfg.world;
-  Memory m(a.all);
+  Memory m;
   for (uint32_t w = 0; w < a.all; ++w) {
     m.add(v.a[w], rows_bytes(v.tokens[w], pitch, features, es), !store);
     m.add(v.b[w], checkpoint_size(v.tokens[w], features), store);
@@ -1342,7 +1343,7 @@ int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t fe
   const uint64_t need = weight_gradient_workspace(a.all, uint32_t(features), uint32_t(outputs), a.max_tokens);
   if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
   if (int rc = need_bound(p, false)) return rc;
-  Memory m(a.all);
+  Memory m;
   m.add(reinterpret_cast<uint64_t>(ws), need, true);
   for (uint32_t w = 0; w < a.all; ++w) {
     v.c[w] = p->bind.rows[weight * a.all + w];
