@@ -307,7 +307,8 @@ int caramel_allreduce_static(caramel_plan* plan, void* const* grads, void* strea
  *
  * All calls are asynchronous on `stream`, allocate nothing (no device memory, no host memory of their own), upload nothing and issue only kernel
  * launches, so they can be captured.  Rows are `pitch` elements apart and may start on any element.  Buffers
- * that a call writes must not overlap any other buffer of the call (EINVAL).  Sums are fp32 in an order that
+ * that a call writes must not overlap any other buffer of the call (EINVAL); what lies between the rows is not the buffer's and is
+ * not written, so the workers' rows may interleave in one array.  Sums are fp32 in an order that
  * depends on the sizes alone, so results are reproducible bit for bit; what is done with a sum (scaling, adding) is one fp32
  * operation, whose result is rounded to bf16 where the tensor is.
  * Gradients are written; with `accumulate` they are added to what the tensor holds (micro-batches, tied

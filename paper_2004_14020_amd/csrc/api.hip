@@ -17,6 +17,7 @@
 #include "caramel.h"
 #include "kernels.hpp"
 #include "layers.hpp"
+#include "memory.hpp"
 #include "plan.hpp"
 #include "schedule.hpp"
 #include "slices.hpp"
@@ -1082,30 +1083,9 @@ int need_device(const caramel_plan* p) {
   return CARAMEL_OK;
 }
 
-// Memory a call reads and writes.  Nothing it writes may overlap anything else of the call.
-struct Memory {
-  struct Span {
-    uint64_t lo, hi;
-    bool written;
-  };
-  Span spans[4 * CARAMEL_MAX_WORLD + 1];  // four buffers of every worker, and a workspace
-  uint32_t n = 0;
-
-  void add(uint64_t at, uint64_t bytes, bool written) {
-    if (bytes) spans[n++] = {at, at + bytes, written};
-  }
-  int check() {
-    std::sort(spans, spans + n, [](const Span& x, const Span& y) { return x.lo < y.lo; });
-    uint64_t any = 0, written = 0;  // how far what came before reaches
-    for (uint32_t i = 0; i < n; ++i) {
-      const Span& s = spans[i];
-      if (s.lo < written || (s.written && s.lo < any)) return fail(CARAMEL_EINVAL, "buffers overlap with one that is written");
-      any = std::max(any, s.hi);
-      if (s.written) written = std::max(written, s.hi);
-    }
-    return CARAMEL_OK;
-  }
-};
+int check_memory(Memory& m) {
+  return m.overlap() ? fail(CARAMEL_EINVAL, "buffers overlap with one that is written") : CARAMEL_OK;
+}
 
 int take_tokens(const caramel_plan* p, const uint64_t* tokens, uint32_t* out, uint32_t* most) {
   if (!tokens) return fail(CARAMEL_EINVAL, "tokens is NULL");
@@ -1157,11 +1137,6 @@ int check_workspace(const void* ws, uint64_t have, uint64_t need) {
   return CARAMEL_OK;
 }
 
-// bytes of `tokens` rows, the last one without what lies behind it
-uint64_t rows_bytes(uint64_t tokens, uint64_t pitch, uint64_t columns, uint64_t es) {
-  return tokens ? ((tokens - 1) * pitch + columns) * es : 0;
-}
-
 uint64_t checkpoint_size(uint64_t tokens, uint64_t features) {
   return (checkpoint_blocks(tokens) * features * (kCheckpointBlock + 1) + 15) / 16 * 16;
 }
@@ -1202,9 +1177,9 @@ int embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, 
     if (!v.tokens[w]) continue;
     m.add(v.a[w], vocab * width * es, false);
     m.add(v.b[w], uint64_t(v.tokens[w]) * id_bytes, false);
-    m.add(v.c[w], rows_bytes(v.tokens[w], out_pitch, width, es), true);
+    m.add_rows(v.c[w], v.tokens[w], out_pitch, width, es, true);
   }
-  if (int rc = m.check()) return rc;
+  if (int rc = check_memory(m)) return rc;
   if (int rc = need_device(p)) return rc;
   a.vocab = uint32_t(vocab);
   a.width = uint32_t(width);
@@ -1256,9 +1231,9 @@ int embedding_gradient(caramel_plan* p, uint32_t tensor, uint64_t width, float s
     v.c[w] = p->bind.rows[tensor * a.all + w];
     m.add(v.c[w], vocab * width * es, true);
     m.add(v.a[w], uint64_t(v.tokens[w]) * id_bytes, false);
-    m.add(v.b[w], rows_bytes(v.tokens[w], dy_pitch, width, size_of(dy_dtype)), false);
+    m.add_rows(v.b[w], v.tokens[w], dy_pitch, width, size_of(dy_dtype), false);
   }
-  if (int rc = m.check()) return rc;
+  if (int rc = check_memory(m)) return rc;
   a.vocab = uint32_t(vocab);
   a.width = uint32_t(width);
   a.dy_pitch = dy_pitch;
@@ -1290,10 +1265,10 @@ int checkpoint_call(caramel_plan* p, bool store, const uint64_t* tokens, uint64_
   a.all = p->host.cfg.world;
   Memory m;
   for (uint32_t w = 0; w < a.all; ++w) {
-    m.add(v.a[w], rows_bytes(v.tokens[w], pitch, features, es), !store);
+    m.add_rows(v.a[w], v.tokens[w], pitch, features, es, !store);
     m.add(v.b[w], checkpoint_size(v.tokens[w], features), store);
   }
-  if (int rc = m.check()) return rc;
+  if (int rc = check_memory(m)) return rc;
   if (int rc = need_device(p)) return rc;
   a.features = uint32_t(features);
   a.pitch = pitch;
@@ -1353,9 +1328,9 @@ int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t fe
       m.add(v.d[w], outputs * es, true);
     }
     m.add(v.a[w], checkpoint_size(v.tokens[w], features), false);
-    m.add(v.b[w], rows_bytes(v.tokens[w], dy_pitch, outputs, size_of(dy_dtype)), false);
+    m.add_rows(v.b[w], v.tokens[w], dy_pitch, outputs, size_of(dy_dtype), false);
   }
-  if (int rc = m.check()) return rc;
+  if (int rc = check_memory(m)) return rc;
   a.features = uint32_t(features);
   a.outputs = uint32_t(outputs);
   a.dy_pitch = dy_pitch;

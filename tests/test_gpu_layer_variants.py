@@ -6,8 +6,9 @@ import torch
 
 import paper_2004_14020_amd as cm
 
-from layer_util import DEV, HALF_STEP, TORCH, addresses, bound_plan, f64, rows, saved_sparse, stream, untouched, workspace
-from test_gpu_layers import DTYPES, NAMES, TYPES, close, counts, dtype_id, make_ids
+from layer_util import (DEV, HALF_STEP, TORCH, addresses, bound_plan, embedding_gradient, f64, rows, saved_sparse, stream, untouched,
+                        workspace)
+from test_gpu_layers import DTYPES, NAMES, TYPES, close, counts, dtype_id, make_ids, saved_checkpoints
 
 pytestmark = pytest.mark.gpu
 
@@ -216,4 +217,47 @@ def test_lookup_with_streaming_stores(world, n, vocab, width, gap, dtype, id_byt
         assert torch.equal(view, want), f"worker {w}"
         view.fill_(7.0)
         assert bool((mem == 7.0).all()), "the gaps between the rows and what lies behind the last one stay"
+    plan.close()
+
+
+# ---- the workers' rows side by side in one array -------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+@pytest.mark.parametrize("world,n,width", [(2, 70, 33), (3, 5, 1), (8, 40, 260), (64, 33, 7)])
+def test_rows_of_all_workers_interleave(world, n, width, dtype):
+    """[token][worker][column]: lookup, store and load, and both gradients, one column free behind the last worker's."""
+    print(f"case: interleaved rows world={world} n={n} width={width} dtype={NAMES[dtype]}", flush=True)
+    rng = np.random.default_rng(n + width)
+    vocab, k, pitch, es = 40, 24, world * width + 1, 2 if dtype == cm.BF16 else 4
+    plan, grads = bound_plan(world, [vocab * width, k * width], dtype)
+    side_by_side = lambda fill: torch.full((n, pitch), fill, dtype=TORCH[dtype], device=DEV)                # noqa: E731
+    at = lambda t: [t.data_ptr() + w * width * es for w in range(world)]                                 # noqa: E731
+    of = lambda t, w: t[:, w * width:(w + 1) * width]                                                    # noqa: E731
+    table = torch.tensor(rng.integers(-8, 9, (vocab, width)).astype(np.float32)).to(TORCH[dtype])
+    ids = [torch.tensor(rng.integers(-1, vocab, n)) for _ in range(world)]
+    dt, di, ns = table.to(DEV), [i.to(DEV) for i in ids], [n] * world
+    x, back = side_by_side(7.0), side_by_side(7.0)
+    plan.embedding_lookup([dt.data_ptr()] * world, vocab, width, addresses(di), ns, at(x), out_pitch=pitch, stream=stream())
+    saved = [torch.empty(cm.checkpoint_bytes(n, width), dtype=torch.uint8, device=DEV) for _ in range(world)]
+    plan.checkpoint_store(at(x), ns, width, addresses(saved), dtype=dtype, pitch=pitch, stream=stream())
+    plan.checkpoint_load(addresses(saved), ns, width, at(back), dtype=dtype, pitch=pitch, stream=stream())
+    torch.cuda.synchronize()
+    for w in range(world):
+        want = torch.where((ids[w] >= 0)[:, None], table[ids[w].clamp(min=0)], torch.zeros((), dtype=TORCH[dtype]))
+        assert torch.equal(of(x, w).cpu(), want) and torch.equal(of(back, w).cpu(), want)                 # integers: kept as they are
+    assert bool((x[:, -1] == 7.0).all()) and bool((back[:, -1] == 7.0).all())
+    dy = side_by_side(float("nan"))
+    for w in range(world):
+        of(dy, w).copy_(torch.tensor(rng.integers(-8, 9, (n, width)).astype(np.float32)))
+    need = [plan.embedding_workspace(0, width, ns), plan.weight_gradient_workspace(1, k, ns)]
+    ws = [workspace(b) for b in need]
+    kept = [rng.integers(-8, 9, (n, k)).astype(np.float64) for _ in range(world)]
+    codes = saved_checkpoints(kept)
+    plan.embedding_gradient(0, width, addresses(di), ns, at(dy), ws[0].data_ptr(), need[0], dy_pitch=pitch, stream=stream())
+    plan.weight_gradient(1, None, addresses(codes), ns, k, at(dy), ws[1].data_ptr(), need[1], dy_pitch=pitch, stream=stream())
+    torch.cuda.synchronize()
+    for w in range(world):
+        d = f64(of(dy, w))
+        for got, want in ((grads[w][0].view(vocab, width), embedding_gradient(vocab, ids[w].tolist(), d, 1.0)[0]),
+                          (grads[w][1].view(k, width), kept[w].T @ d)):
+            assert torch.equal(got.cpu(), torch.tensor(want, dtype=torch.float32).to(TORCH[dtype])), f"worker {w}"
     plan.close()
