@@ -312,8 +312,8 @@ int caramel_allreduce_static(caramel_plan* plan, void* const* grads, void* strea
  * depends on the sizes alone, so results are reproducible bit for bit; what is done with a sum (scaling, adding) is one fp32
  * operation, whose result is rounded to bf16 where the tensor is.
  * Gradients are written; with `accumulate` they are added to what the tensor holds (micro-batches, tied
- * weights).  The two gradient calls need a workspace: its size depends on the sizes given, its contents
- * need not be kept from call to call, and calls that may run at the same time need one each.
+ * weights).  The two gradient calls need a workspace: its size depends on the sizes given, and what is enough for some tokens is
+ * enough for fewer; its contents need not be kept from call to call, and calls that may run at the same time need one each.
  * EINVAL: NULL or misaligned pointers (to the element, unless stated), more than 2^25 tokens, 2^20 columns, a
  * pitch below the columns or above 2^23, 2^38 values at a worker, a workspace that is too small.  ESTATE: the plan is
  * bound on another device than the current one; for the gradients also: not bound.  Pointers and stream must belong to

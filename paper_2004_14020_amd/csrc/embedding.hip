@@ -104,6 +104,8 @@ struct Layout {
   uint32_t chunk, chunks;                          // tokens per chunk; chunks of the longest worker
 };
 
+constexpr uint32_t kManyTokens = 16384;  // of all workers: longer chunks
+
 // Bytes are laid out for the longest worker, so that offsets are the same for all.
 Layout layout(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_tokens) {
   auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
@@ -111,7 +113,7 @@ Layout layout(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_token
   // Short chunks give more wavefronts to the sums, long ones cut fewer rows.  Sums and joining, chunks of 8, 16 and 32: 4 x 2050 tokens
   // of 1001 bf16 and fp32 8.3 + 4.4, 9.8 + 3.8 us, -; 8 x 4096 tokens of 1024, bf16, 30522 rows 83 + 10, 86 + 6.4, 91 + 4.9; on two
   // rows (every chunk is cut), fp32 23 + 14, 23 + 9, 22 + 6; 16 x 7400 tokens of 105, bf16, 2759 rows 16 + 12, 15 + 7.7, 22 + 5.4.
-  const bool many = uint64_t(world) * max_tokens >= 16384;
+  const bool many = uint64_t(world) * max_tokens >= kManyTokens;
   l.chunk = !many ? 8 : max_tokens / 32 < vocab ? 16 : 32;
   l.chunks = (max_tokens + l.chunk - 1) / l.chunk;
   l.start = 0;
@@ -707,8 +709,13 @@ hipError_t launch_embedding_lookup(const LookupArgs& args, const AllWorkers& v, 
   });
 }
 
+// Enough for fewer tokens too: those just below a step to longer chunks have the most of them.
 uint64_t embedding_gradient_workspace(uint32_t world, uint32_t vocab, uint32_t width, uint32_t max_tokens) {
-  return layout(world, vocab, width, max_tokens).stride * world;
+  const uint64_t few = (kManyTokens - 1) / world, wide = uint64_t(vocab) * 32 - 1;  // the most tokens with chunks of 8, of 16
+  uint64_t most = 0;
+  for (uint64_t n : {uint64_t(max_tokens), few, wide})
+    if (n <= max_tokens) most = std::max(most, layout(world, vocab, width, uint32_t(n)).stride);
+  return most * world;
 }
 
 hipError_t launch_embedding_gradient(const EmbeddingGradientArgs& args, const AllWorkers& v, hipStream_t s) {

@@ -1,6 +1,7 @@
 """How the calls that fill gradient tensors check their arguments: what that costs, and which memory may lie where.  No GPU call is
 made."""
 import os
+import random
 import shutil
 import subprocess
 
@@ -46,3 +47,18 @@ def test_rows_that_interleave_by_less_than_their_length_are_refused():
                 call()
             assert e.value.status == binding.EINVAL and "overlap" in str(e.value)
     plan.close()
+
+
+def test_a_workspace_serves_fewer_tokens():
+    """Also at the steps from short chunks of the sorted tokens to longer ones, and between the weight gradient's kernels."""
+    rng = random.Random(3)
+    for _ in range(300):
+        world, k, outputs = rng.choice([1, 2, 3, 8, 16, 64]), int(2 ** rng.uniform(0, 11)), int(2 ** rng.uniform(0, 11))
+        plan = cm.Plan(world, [k * outputs])
+        steps = [16384 // world + d for d in (-9, -1, 0, 1, 9)] + [32 * k + d for d in (-17, -1, 0, 1)]
+        tokens = sorted(max(0, t) for t in steps + [int(2 ** rng.uniform(0, 18)) for _ in range(20)])
+        for size in (lambda n: plan.embedding_workspace(0, outputs, [n] * world),
+                     lambda n: plan.weight_gradient_workspace(0, k, [n] * world)):
+            sizes = [size(n) for n in tokens]
+            assert sizes == sorted(sizes), (world, k, outputs, tokens, sizes)
+        plan.close()
