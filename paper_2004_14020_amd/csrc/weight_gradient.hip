@@ -62,16 +62,13 @@ __device__ __forceinline__ float signed_byte(uint32_t word, int n) {
 // start on any element.)
 enum Load { kPairs, kShift, kSingle };
 
-// The rows of dy of one workgroup: TN outputs, brought in by its lanes 32 tokens at a time.  A task is eight tokens of two
-// outputs; a lane has TASKS of them.
-template <bool BF16, Load LOAD, int TN, int TASKS>
+// The rows of dy of one workgroup: TN outputs, brought in by its 2 TN lanes 32 tokens at a time; a lane has eight tokens of two
+// outputs.
+template <bool BF16, Load LOAD, int TN>
 struct Dy {
-  static constexpr int ES = BF16 ? 2 : 4, P = BF16 ? 1 : 3, kOctets = 4 / TASKS;
-  static constexpr int kPacks = 2 * TASKS * (BF16 ? 1 : 4);
-  typedef uint32_t task __attribute__((ext_vector_type(BF16 ? 8 : 16)));
-  struct raw {
-    task v[TASKS];
-  };
+  static constexpr int ES = BF16 ? 2 : 4, P = BF16 ? 1 : 3;
+  static constexpr int kPacks = 2 * (BF16 ? 1 : 4);
+  typedef uint32_t raw __attribute__((ext_vector_type(BF16 ? 8 : 16)));
   uint64_t base;
   uint32_t row_bytes, behind, end_token, off, octet, pair;
   bool last_pair;
@@ -95,31 +92,30 @@ struct Dy {
     const uint32_t rows = min(end_token - min(b * kCheckpointBlock, end_token), kCheckpointBlock);
     return buffer(base + uint64_t(b) * kCheckpointBlock * row_bytes, max(int(rows * row_bytes - behind), 0));
   }
-  __device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t r, raw& v, int n) const {  // n: 0 to 8 * TASKS - 1
-    const int i = n / 8, j = n % 8, at = int(off + (i * kOctets * 8 + j) * row_bytes);
+  __device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t r, raw& v, int j) const {  // j: 0 to 7
+    const int at = int(off + j * row_bytes);
     if constexpr (!BF16) {
       const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
-      v.v[i][2 * j] = x[0];
-      v.v[i][2 * j + 1] = x[1];
+      v[2 * j] = x[0];
+      v[2 * j + 1] = x[1];
     } else if constexpr (LOAD == kSingle) {
-      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+      v[j] = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
     } else {
-      v.v[i][j] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+      v[j] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
     }
   }
   __device__ __forceinline__ raw load(uint32_t b) const {
     raw v;
     const __amdgpu_buffer_rsrc_t r = block(b);
 #pragma unroll
-    for (int n = 0; n < 8 * TASKS; ++n) load_row(r, v, n);
+    for (int j = 0; j < 8; ++j) load_row(r, v, j);
     return v;
   }
   // To LDS as operands, eight tokens of an output to a piece, and into the sums where the bias is due; in kPacks steps.
   template <typename BIAS>
-  __device__ __forceinline__ void pack(raw& v, u32x4 (*lds)[4][TN], int n, BIAS) {
-    const int i = BF16 ? n : n / 4, odd = i % 2;
-    task& in = v.v[i / 2];
-    u32x4* const to = &lds[0][octet + i / 2 * kOctets][odd * (TN / 2) + pair];
+  __device__ __forceinline__ void pack(raw& in, u32x4 (*lds)[4][TN], int n, BIAS) {
+    const int odd = BF16 ? n : n / 4;
+    u32x4* const to = &lds[0][octet][odd * (TN / 2) + pair];
     if constexpr (BF16) {
       if constexpr (LOAD == kShift)
         if (!odd) in >>= last_pair ? 16u : 0u;
@@ -214,7 +210,7 @@ __device__ __forceinline__ void write_strip(__amdgpu_buffer_rsrc_t ro, uint32_t 
 }
 
 // The bias of a workgroup's outputs from its lanes' sums; LDS has to be free.
-template <bool OUT_BF16, int TN, int OCTETS>
+template <bool OUT_BF16, int TN>
 __device__ __forceinline__ void write_bias(const WeightGradientArgs& a, float* part, uint32_t tid, uint32_t n0, uint64_t to,
                                            uint32_t octet, uint32_t pair, const float* sums) {
   constexpr int OS = OUT_BF16 ? 2 : 4;
@@ -224,7 +220,7 @@ __device__ __forceinline__ void write_bias(const WeightGradientArgs& a, float* p
   if (tid >= TN || n0 + tid >= a.outputs) return;
   float y = part[tid];
 #pragma unroll
-  for (int o = 1; o < OCTETS; ++o) y += part[o * TN + tid];
+  for (int o = 1; o < 4; ++o) y += part[o * TN + tid];
   const uint64_t at = to + uint64_t(n0 + tid) * OS;
   if (a.accumulate) {
     float old;
@@ -238,9 +234,7 @@ __device__ __forceinline__ void write_bias(const WeightGradientArgs& a, float* p
 template <int WK, int WN, int FK, int TB, int OCCUPANCY, bool DY_BF16, bool OUT_BF16, Load LOAD>
 __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(WeightGradientArgs a, Tiling t) {
   constexpr int TK = WK * FK * 32, TN = WN * TB * 64, THREADS = WK * WN * 64;
-  // a task is eight tokens of two outputs of dy; a lane has TASKS of them per block
-  constexpr int TASKS = 2 * TN / THREADS, OCTETS = 4 / TASKS;
-  static_assert(TASKS * THREADS == 2 * TN && OCTETS * TASKS == 4, "the lanes share a block of dy evenly");
+  static_assert(THREADS == 2 * TN, "the lanes share a block of dy evenly");
   constexpr int P = DY_BF16 ? 1 : 3, OS = OUT_BF16 ? 2 : 4;
   __shared__ u32x4 lds[3][P][4][TN];
 
@@ -268,7 +262,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
   const uint32_t wk = wave / WN, wn = wave % WN, l32 = lane % 32, half = lane / 32;
 
   const uint64_t codes = a.w.a[w], scales = codes + uint64_t(blocks) * K * kCheckpointBlock;
-  typedef Dy<DY_BF16, LOAD, TN, TASKS> Rows;
+  typedef Dy<DY_BF16, LOAD, TN> Rows;
   typedef typename Rows::raw raw;
   constexpr int kPacks = Rows::kPacks;
   Rows dy(a, w, n0, min(M, b1 * kCheckpointBlock), tid);
@@ -355,7 +349,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
     // Block b is multiplied while x of block b + 1 is widened, dy of block b + 2 goes to LDS, and x of block b + 1 + kSets and dy
     // of block b + 2 + kSets are fetched.  The order of the instructions is laid down: a few others after every product, which run in its shadow.
     // A wavefront issues in order, so a row of loads, or of conversions, would hold up the products behind it.
-    constexpr int kLoads = 8 * TASKS, kPieces = kPacks + kLoads + kWidens + FK;
+    constexpr int kLoads = 8, kPieces = kPacks + kLoads + kWidens + FK;
     auto turn = [&](uint32_t b, Widened& now, Widened& then, Codes& x_in, raw& dy_in, auto with_bias) {
       const __amdgpu_buffer_rsrc_t r = dy.block(b + 2 + kSets);
       auto piece = [&](int n) {
@@ -413,7 +407,7 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
 
   if (sums_dy) {  // the same for all lanes of the workgroup
     __syncthreads();
-    write_bias<OUT_BF16, TN, OCTETS>(a, reinterpret_cast<float*>(lds), tid, n0, a.w.d[w] + split * t.bias_stride, dy.octet, dy.pair,
+    write_bias<OUT_BF16, TN>(a, reinterpret_cast<float*>(lds), tid, n0, a.w.d[w] + split * t.bias_stride, dy.octet, dy.pair,
                                      dy.bias);
   }
 }
@@ -455,7 +449,7 @@ __global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradient
   uint32_t step = part * t.share + wave;
   Codes next = load_codes(step, 0);
 
-  typedef Dy<DY_BF16, LOAD, TN, 1> Rows;
+  typedef Dy<DY_BF16, LOAD, TN> Rows;
   Rows dy(a, w, n0, M, tid);
   const bool sums_dy = a.has_bias && part == 0;
   typename Rows::raw v[BLOCKS];
@@ -503,7 +497,7 @@ __global__ void __launch_bounds__(256, 2) k_weight_gradient_short(WeightGradient
 
   if (sums_dy) {
     __syncthreads();
-    write_bias<OUT_BF16, TN, 4>(a, reinterpret_cast<float*>(lds), tid, n0, a.w.d[w], dy.octet, dy.pair, dy.bias);
+    write_bias<OUT_BF16, TN>(a, reinterpret_cast<float*>(lds), tid, n0, a.w.d[w], dy.octet, dy.pair, dy.bias);
   }
 }
 
