@@ -17,8 +17,8 @@ namespace {
 // ---- lookup ---------------------------------------------------------------------------------
 
 // Bound: HBM (rows named once, read and written).  `lanes` lanes (a power of two) take one row, four rows
-// each, so that four independent loads are in flight per lane.  8 x 4096 tokens of 1024 bf16: 18.6 us, 101 MB at 5.4 TB/s (two rows
-// each 20.1, eight 21.0).
+// each, so that four independent loads are in flight per lane.  8 x 4096 tokens of 1024 bf16: 18.9 us back to back, 101 MB at 5.3 TB/s
+// (two rows each 20.1, eight 21.0), and 24 with 640 MB of other data read in between (49 MB read, 67 written); fp32 35 us.
 constexpr int kLookupRows = 4;
 
 // STREAM: streaming stores, where the output is more than the L2s hold (8 x 4096 tokens of 1024 bf16: 20.3 us with plain
@@ -91,8 +91,9 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(LookupArgs a, uint32_t
 //                      Rows cut by a chunk's border leave partial sums.  Other workgroups clear the rows that
 //                      no token names.
 //   k_embedding_join   adds the partial sums of the rows that were cut, in the chunks' order.
-// Bound: HBM, most of all the zeros.  8 x 4096 tokens, 30522 x 1024 bf16 (567 MB): 11 + 86 + 6 us; all tokens on two rows of 1024
-// fp32 (134 MB): 7 + 22 + 6.
+// Bound: HBM, most of all the zeros, and the latency of three dependent launches.  8 x 4096 tokens, 30522 x 1024 bf16 (567 MB; by counters
+// 506 written and 71 read): 11 + 84 + 6 us back to back, 12 + 107 + 6 with 640 MB of other data read in between; accumulating, without
+// the zeros, 44 a call.  All tokens on two rows of 1024 fp32 (134 MB): 6 + 22 + 6 and 7 + 31 + 6.
 
 constexpr int kSortWaves = 16;
 constexpr int kSortAhead = 4;          // ids per lane that are fetched at once; up to 4096 tokens they stay in registers
@@ -352,8 +353,7 @@ constexpr int kAhead = 8;  // tokens whose rows are fetched at once
 
 // Clears those of the rows [first, first + rows) whose bit in `empty` is set; one wavefront, at most 64 rows.  The rows are taken as
 // the one stretch of memory that they are, so that stores are whole and next to each other however wide a row is.  Streaming
-// stores: with plain ones, the zeros of the pass before are still being written back (8 x 30522 x 1024 bf16, 4096 tokens
-// each: 123 us, 90).
+// stores: 8 x 30522 x 1024 bf16, 4096 tokens each 90 us, with plain ones 123.
 template <bool OUT_BF16>
 __device__ __forceinline__ void clear_rows(uint64_t out, uint32_t width, uint32_t first, uint32_t rows, uint64_t empty) {
   constexpr int OS = OUT_BF16 ? 2 : 4, N = 16 / OS;
@@ -562,7 +562,8 @@ __global__ void __launch_bounds__(kSumBlock) k_embedding_few(EmbeddingGradientAr
 constexpr int kJoinWaves = 4;
 
 // One workgroup per chunk and 256 columns; it works if a row begins in the chunk and runs past its end.  The
-// wavefronts take equal stretches of that row's partial sums.
+// wavefronts take equal stretches of that row's partial sums: however long the row is, one workgroup for 256 of its columns.  2^18 tokens on
+// two rows of 128 fp32: sorting 250 us (one workgroup has both ids), sums 22, joining 91; 2^20: 980, 104, 440.
 template <bool OUT_BF16>
 __global__ void __launch_bounds__(64 * kJoinWaves) k_embedding_join(EmbeddingGradientArgs a, Layout l) {
   __shared__ float part[kJoinWaves][256];

@@ -10,10 +10,12 @@
 // goes: bits under 2^-133 are cut off.  (The matrix cores take subnormal numbers as they are.)  A common power of two cannot help, as
 // both x and dy may lie anywhere in fp32's range, and finding one for each tile would be another pass over dy.
 //
-// Bound: the matrix cores.  8 x (4096 tokens, 1024 x 4096) bf16 251 us = 1094 TFLOP/s, against 1265 of a library product of 8192^3
-// and 676 of one of this shape; 16384 tokens, 1024 x 1024 fp32 95 us + 12 for joining its 16 parts (three products: 1085
-// TFLOP/s; an fp32 library product 153).  What the loop's instructions cost there: without widening x 230 us, without fetching dy
-// 225, without either and without LDS writes 200 (at 1.86 GHz: what power leaves of 2.4).  Few tokens: HBM, see below.
+// Bound: no unit by itself.  8 x (4096 tokens, 1024 x 4096) bf16 takes 261 us a call = 1053 TFLOP/s (the kernel's least 252; back to
+// back 277 to 316, as the clock falls), against 1262 of a library product of 8192^3 and 675 of one of this shape.  Of the cycles, at
+// the 1.9 GHz that power leaves of 2.4, the matrix cores are busy in 53 %, other vector instructions take 32 % of the SIMDs', and
+// LDS, which gives every product its 128-bit operand at 256 bytes a clock, is busy in 33 %.  What the loop's instructions cost, of 251 us:
+// without widening x 230, without fetching dy 225, without either and without LDS writes 200.  16384 tokens, 1024 x 1024 fp32 95 us + 12
+// for joining its 16 parts (three products: 1085 TFLOP/s; an fp32 library product 153).  Few tokens: HBM, see below.
 //
 // Tiling.  A workgroup owns TK features x TN outputs and walks the tokens 32 at a time (one block of the
 // checkpoint).  dy is brought to LDS once per workgroup, transposed on the way through registers so that
@@ -414,8 +416,9 @@ __global__ void __launch_bounds__(WK * WN * 64, OCCUPANCY) k_weight_gradient(Wei
 
 // Few tokens: what is written outweighs the product.  A workgroup keeps dy of all tokens in LDS, 128 outputs of it, and goes
 // along the features, each wavefront by itself, 32 features at a time: codes come in and sums go out without a barrier.
-// Bound: HBM writes.  2 x (64 tokens, 25088 x 4096) fp32, 822 MB: 149 us, and 256 in the tiles of the other kernel; with plain stores
-// 172, with three workgroups per compute unit 187, with workgroups for three rounds 158.  STREAM: streaming stores, where rows are
+// Bound: HBM writes.  2 x (64 tokens, 25088 x 4096) fp32: 162 us a call, 828 MB written at 5.1 TB/s (the kernel's least 151, back to back
+// 165).  Least values of one session: 149, in the tiles of the other kernel 256, with plain stores 172, with three workgroups per compute
+// unit 187, with workgroups for three rounds 158.  STREAM: streaming stores, where rows are
 // whole cache lines and all tensors together are more than the last-level cache holds; 4 x (14 tokens, 2845 x 3365) bf16, 77 MB in rows
 // that are not: 29 us, with streaming stores 62.
 struct ShortTiling {
