@@ -366,6 +366,35 @@ int caramel_weight_gradient(caramel_plan* plan, uint32_t weight, uint32_t bias, 
                             const void* const* checkpoint, const uint64_t* tokens, const void* const* dy, uint32_t dy_dtype,
                             uint64_t dy_pitch, int accumulate, void* ws, uint64_t ws_bytes, void* stream);
 
+/* ---- a training step around them --------------------------------------------------------- */
+
+/* What a language model's step does between the calls above.  The same rules hold: all W workers in one call, arrays of W DEVICE
+ * pointers, host counts that may be 0, no allocation, no upload, kernel launches only, buffers that a call writes overlap no other
+ * buffer of the call.  An optional array of pointers may be NULL.  Matrices have one row per token; those that share a `pitch` in the
+ * argument list share it in memory, and rows of different pitch must not interleave. */
+
+/* The norm in front of a layer, with the residual stream's addition:
+ *   sum[w][i, :]  = x[w][i, :] + residual[w][i, :], rounded to dtype                          (both or neither; neither: sum is x)
+ *   rstd[w][i]    = 1 / sqrt(mean of the squares of sum[w][i, :] + eps)                       (fp32, kept for the gradient)
+ *   y[w][i, j]    = (sum[w][i, j] * rstd[w][i]) * gain[w][j]    two fp32 products, rounded to dtype
+ *   checkpoint[w] = what caramel_checkpoint_store makes of y[w]                               (optional)
+ * gain is `width` elements of the plan's dtype, dtype that of all rows.  The mean is taken in 64 bits, so that rstd, y and the codes do not hang on
+ * the order of a sum.  Infinities and NaN go by these formulas.  EINVAL besides the above: width above 32768, eps not a positive number. */
+int caramel_residual_norm(caramel_plan* plan, const void* const* gain, uint64_t width, float eps, const uint64_t* tokens,
+                          const void* const* x, const void* const* residual, uint32_t dtype, uint64_t pitch, void* const* sum,
+                          void* const* y, float* const* rstd, void* const* checkpoint, void* stream);
+
+/* Its gradient, from x (the sum, if there was a residual), rstd and gain as they were, and dy, the gradient of y:
+ *   with u = dy * gain and n = x * rstd,  dx[w][i, :] = rstd * (u - n * mean(u n)) + dsum[w][i, :], rounded to dtype
+ *   grads[w][gain_tensor] = sum over the tokens of dy * n
+ * dsum (optional) is the gradient of the sum that comes along the residual stream; dx is that of both x and residual.  The width
+ * is the tensor's number of elements.  Bound plan, workspace and `accumulate` as for the gradients above. */
+int caramel_residual_norm_workspace(const caramel_plan* plan, uint32_t gain_tensor, const uint64_t* tokens, uint64_t* bytes);
+int caramel_residual_norm_gradient(caramel_plan* plan, uint32_t gain_tensor, const void* const* gain, const uint64_t* tokens,
+                                   const void* const* x, const float* const* rstd, const void* const* dy, const void* const* dsum,
+                                   uint32_t dtype, uint64_t pitch, void* const* dx, int accumulate, void* ws, uint64_t ws_bytes,
+                                   void* stream);
+
 /* ---- launch tuning and timing (do not change results) ------------------------------------ */
 
 /* How the work is cut up for the GPU.  A "run" is a maximal piece of one tensor (or of the fused

@@ -133,6 +133,18 @@ def caramel_weight_gradient(plan: Plan, weight, bias, checkpoint, tokens, featur
     plan.weight_gradient(weight, bias, checkpoint, tokens, features, dy, ws, ws_bytes, **kw)
 
 
+def caramel_residual_norm(plan: Plan, gain, width, tokens, x, y, rstd, **kw) -> None:
+    plan.residual_norm(gain, width, tokens, x, y, rstd, **kw)
+
+
+def caramel_residual_norm_workspace(plan: Plan, gain_tensor, tokens) -> int:
+    return plan.residual_norm_workspace(gain_tensor, tokens)
+
+
+def caramel_residual_norm_gradient(plan: Plan, gain_tensor, gain, tokens, x, rstd, dy, dx, ws, ws_bytes, **kw) -> None:
+    plan.residual_norm_gradient(gain_tensor, gain, tokens, x, rstd, dy, dx, ws, ws_bytes, **kw)
+
+
 def caramel_profile(plan: Plan, level: int) -> None:
     plan.profile(level)
 

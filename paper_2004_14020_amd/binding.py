@@ -37,6 +37,7 @@ EXPORTS = (
     "caramel_version", "caramel_stream_probe", "caramel_allreduce_loop",
     "caramel_embedding_lookup", "caramel_embedding_workspace", "caramel_embedding_gradient", "caramel_checkpoint_bytes",
     "caramel_checkpoint_store", "caramel_checkpoint_load", "caramel_weight_gradient_workspace", "caramel_weight_gradient",
+    "caramel_residual_norm", "caramel_residual_norm_workspace", "caramel_residual_norm_gradient",
 )
 
 
@@ -134,6 +135,9 @@ def lib() -> C.CDLL:
     L.caramel_checkpoint_load.argtypes = [P, PU64, U64, PP, PP, U32, U64, P]
     L.caramel_weight_gradient_workspace.argtypes = [P, U32, U64, PU64, PU64]
     L.caramel_weight_gradient.argtypes = [P, U32, U32, U64, PP, PU64, PP, U32, U64, C.c_int, P, U64, P]
+    L.caramel_residual_norm.argtypes = [P, PP, U64, C.c_float, PU64, PP, PP, U32, U64, PP, PP, PP, PP, P]
+    L.caramel_residual_norm_workspace.argtypes = [P, U32, PU64, PU64]
+    L.caramel_residual_norm_gradient.argtypes = [P, U32, PP, PU64, PP, PP, PP, PP, U32, U64, PP, C.c_int, P, U64, P]
     _lib = L
     return L
 
@@ -343,6 +347,40 @@ class Plan:
             self._h, weight, NO_TENSOR if bias is None else bias, features, per(C.c_void_p, checkpoint, "checkpoint"),
             per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype,
             self._outputs(weight, features) if dy_pitch is None else dy_pitch, int(accumulate), ws, ws_bytes, stream))
+
+    # -- a training step around them
+    def _optional(self, values, name):
+        return None if values is None else self._per_worker(C.c_void_p, values, name)
+
+    def residual_norm(self, gain: Sequence[int], width: int, tokens: Sequence[int], x: Sequence[int], y: Sequence[int],
+                      rstd: Sequence[int], eps: float = 1e-5, residual: Optional[Sequence[int]] = None,
+                      sum: Optional[Sequence[int]] = None, checkpoint: Optional[Sequence[int]] = None,
+                      dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
+        """dtype None: the plan's; pitch None: rows without gaps."""
+        per, opt = self._per_worker, self._optional
+        _check(lib().caramel_residual_norm(
+            self._h, per(C.c_void_p, gain, "gain"), width, eps, per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, x, "x"),
+            opt(residual, "residual"), self.cfg.dtype if dtype is None else dtype, width if pitch is None else pitch,
+            opt(sum, "sum"), per(C.c_void_p, y, "y"), per(C.c_void_p, rstd, "rstd"), opt(checkpoint, "checkpoint"), stream))
+
+    def residual_norm_workspace(self, gain_tensor: int, tokens: Sequence[int]) -> int:
+        """Bytes of workspace that residual_norm_gradient needs for these sizes."""
+        n = C.c_uint64()
+        _check(lib().caramel_residual_norm_workspace(self._h, gain_tensor, self._per_worker(C.c_uint64, tokens, "tokens"),
+                                                     C.byref(n)))
+        return n.value
+
+    def residual_norm_gradient(self, gain_tensor: int, gain: Sequence[int], tokens: Sequence[int], x: Sequence[int],
+                               rstd: Sequence[int], dy: Sequence[int], dx: Sequence[int], ws: int, ws_bytes: int,
+                               dsum: Optional[Sequence[int]] = None, dtype: Optional[int] = None, pitch: Optional[int] = None,
+                               accumulate: bool = False, stream: int = 0) -> None:
+        """dtype None: the plan's; pitch None: rows without gaps."""
+        per = self._per_worker
+        _check(lib().caramel_residual_norm_gradient(
+            self._h, gain_tensor, per(C.c_void_p, gain, "gain"), per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, x, "x"),
+            per(C.c_void_p, rstd, "rstd"), per(C.c_void_p, dy, "dy"), self._optional(dsum, "dsum"),
+            self.cfg.dtype if dtype is None else dtype, self._outputs(gain_tensor, 1) if pitch is None else pitch,
+            per(C.c_void_p, dx, "dx"), int(accumulate), ws, ws_bytes, stream))
 
     def profile(self, level: int) -> None:
         _check(lib().caramel_profile(self._h, int(level)))

@@ -1345,6 +1345,140 @@ int weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uint64_t fe
   return CARAMEL_OK;
 }
 
+// ---- before and between them ----------------------------------------------------------------
+
+// As take_pointers; a call may go without them: addresses 0.
+int take_optional(const caramel_plan* p, const char* name, const void* const* from, const uint32_t* tokens, uint64_t align,
+                  uint64_t* out) {
+  return from ? take_pointers(p, name, from, tokens, align, out) : int(CARAMEL_OK);
+}
+
+int check_norm_width(uint64_t width) {
+  if (width == 0 || width > kNormWidth)
+    return fail(CARAMEL_EINVAL, "width must be 1 to %u, is %llu", kNormWidth, (unsigned long long)width);
+  return CARAMEL_OK;
+}
+
+int residual_norm(caramel_plan* p, const void* const* gain, uint64_t width, float eps, const uint64_t* tokens, const void* const* x,
+                  const void* const* residual, uint32_t dtype, uint64_t pitch, void* const* sum, void* const* y, float* const* rstd,
+                  void* const* checkpoint, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  const uint64_t gs = p->host.elem_size();
+  NormArgs a{};
+  AllBuffers<kNormBuffers> v{};
+  if (int rc = check_norm_width(width)) return rc;
+  if (int rc = check_dtype("dtype", dtype)) return rc;
+  if (!(eps > 0.0f) || !std::isfinite(eps)) return fail(CARAMEL_EINVAL, "eps must be a positive number, is %g", double(eps));
+  if ((residual != nullptr) != (sum != nullptr)) return fail(CARAMEL_EINVAL, "residual and sum go together");
+  const uint64_t es = size_of(dtype);
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("pitch", pitch, width, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "gain", gain, v.tokens, gs, v.at[kNormGain])) return rc;
+  if (int rc = take_pointers(p, "x", x, v.tokens, es, v.at[kNormX])) return rc;
+  if (int rc = take_optional(p, "residual", residual, v.tokens, es, v.at[kNormResidual])) return rc;
+  if (int rc = take_optional(p, "sum", sum, v.tokens, es, v.at[kNormSum])) return rc;
+  if (int rc = take_pointers(p, "y", y, v.tokens, es, v.at[kNormY])) return rc;
+  if (int rc = take_pointers(p, "rstd", reinterpret_cast<const void* const*>(rstd), v.tokens, 4, v.at[kNormRstd])) return rc;
+  if (int rc = take_optional(p, "checkpoint", checkpoint, v.tokens, 16, v.at[kNormCheckpoint])) return rc;
+  a.all = p->host.cfg.world;
+  Memory m;
+  for (uint32_t w = 0; w < a.all; ++w) {
+    const uint64_t n = v.tokens[w];
+    if (!n) continue;
+    m.add(v.at[kNormGain][w], width * gs, false);
+    m.add_rows(v.at[kNormX][w], n, pitch, width, es, false);
+    m.add_rows(v.at[kNormY][w], n, pitch, width, es, true);
+    m.add(v.at[kNormRstd][w], n * 4, true);
+    if (residual) m.add_rows(v.at[kNormResidual][w], n, pitch, width, es, false);
+    if (sum) m.add_rows(v.at[kNormSum][w], n, pitch, width, es, true);
+    if (checkpoint) m.add(v.at[kNormCheckpoint][w], checkpoint_size(n, width), true);
+  }
+  if (int rc = check_memory(m)) return rc;
+  if (int rc = need_device(p)) return rc;
+  a.width = uint32_t(width);
+  a.pitch = pitch;
+  a.eps = eps;
+  a.bf16 = dtype == CARAMEL_BF16;
+  a.gain_bf16 = p->host.cfg.dtype == CARAMEL_BF16;
+  a.residual = residual != nullptr;
+  a.checkpoint = checkpoint != nullptr;
+  if (tracing())
+    std::fprintf(stderr, "caramel: residual norm stream %p, %u workers, up to %u tokens, %u columns\n", (void*)stream, a.all,
+                 a.max_tokens, a.width);
+  HIP_TRY(launch_norm(a, v, stream));
+  return CARAMEL_OK;
+}
+
+int check_gain(const caramel_plan* p, uint32_t gain_tensor, uint64_t* width) {
+  uint64_t rows = 0;
+  if (int rc = check_matrix(p, "gain", gain_tensor, 1, &rows)) return rc;
+  *width = rows;
+  return check_norm_width(rows);
+}
+
+int residual_norm_workspace(const caramel_plan* p, uint32_t gain_tensor, const uint64_t* tokens, uint64_t* bytes) {
+  if (!p || !bytes) return fail(CARAMEL_EINVAL, "NULL argument");
+  uint64_t width = 0;
+  uint32_t n[CARAMEL_MAX_WORLD], most = 0;
+  if (int rc = check_gain(p, gain_tensor, &width)) return rc;
+  if (int rc = take_tokens(p, tokens, n, &most)) return rc;
+  *bytes = norm_gradient_workspace(p->host.cfg.world, uint32_t(width), most);
+  return CARAMEL_OK;
+}
+
+int residual_norm_gradient(caramel_plan* p, uint32_t gain_tensor, const void* const* gain, const uint64_t* tokens,
+                           const void* const* x, const float* const* rstd, const void* const* dy, const void* const* dsum,
+                           uint32_t dtype, uint64_t pitch, void* const* dx, int accumulate, void* ws, uint64_t ws_bytes,
+                           hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  const uint64_t gs = p->host.elem_size();
+  uint64_t width = 0;
+  NormGradientArgs a{};
+  AllBuffers<kNormGradBuffers> v{};
+  if (int rc = check_gain(p, gain_tensor, &width)) return rc;
+  if (int rc = check_dtype("dtype", dtype)) return rc;
+  const uint64_t es = size_of(dtype);
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("pitch", pitch, width, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "gain", gain, v.tokens, gs, v.at[kNormGradGain])) return rc;
+  if (int rc = take_pointers(p, "x", x, v.tokens, es, v.at[kNormGradX])) return rc;
+  if (int rc = take_pointers(p, "rstd", reinterpret_cast<const void* const*>(rstd), v.tokens, 4, v.at[kNormGradRstd])) return rc;
+  if (int rc = take_pointers(p, "dy", dy, v.tokens, es, v.at[kNormGradDy])) return rc;
+  if (int rc = take_optional(p, "dsum", dsum, v.tokens, es, v.at[kNormGradDsum])) return rc;
+  if (int rc = take_pointers(p, "dx", dx, v.tokens, es, v.at[kNormGradDx])) return rc;
+  a.all = p->host.cfg.world;
+  const uint64_t need = norm_gradient_workspace(a.all, uint32_t(width), a.max_tokens);
+  if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
+  if (int rc = need_bound(p, false)) return rc;
+  Memory m;
+  m.add(reinterpret_cast<uint64_t>(ws), need, true);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    const uint64_t n = v.tokens[w];
+    v.at[kNormGradOut][w] = p->bind.rows[gain_tensor * a.all + w];
+    m.add(v.at[kNormGradOut][w], width * gs, true);
+    if (!n) continue;
+    m.add(v.at[kNormGradGain][w], width * gs, false);
+    m.add(v.at[kNormGradRstd][w], n * 4, false);
+    m.add_rows(v.at[kNormGradX][w], n, pitch, width, es, false);
+    m.add_rows(v.at[kNormGradDy][w], n, pitch, width, es, false);
+    m.add_rows(v.at[kNormGradDx][w], n, pitch, width, es, true);
+    if (dsum) m.add_rows(v.at[kNormGradDsum][w], n, pitch, width, es, false);
+  }
+  if (int rc = check_memory(m)) return rc;
+  a.width = uint32_t(width);
+  a.pitch = pitch;
+  a.bf16 = dtype == CARAMEL_BF16;
+  a.gain_bf16 = p->host.cfg.dtype == CARAMEL_BF16;
+  a.dsum = dsum != nullptr;
+  a.accumulate = accumulate != 0;
+  a.ws = static_cast<unsigned char*>(ws);
+  if (tracing())
+    std::fprintf(stderr, "caramel: residual norm gradient stream %p, tensor %u, %u workers, up to %u tokens, %u columns\n",
+                 (void*)stream, gain_tensor, a.all, a.max_tokens, a.width);
+  HIP_TRY(launch_norm_gradient(a, v, stream));
+  return CARAMEL_OK;
+}
+
 }  // namespace
 
 int caramel_embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, uint64_t width, float scale,
@@ -1399,6 +1533,28 @@ int caramel_weight_gradient(caramel_plan* p, uint32_t weight, uint32_t bias, uin
   return guarded([&] {
     return weight_gradient(p, weight, bias, features, checkpoint, tokens, dy, dy_dtype, dy_pitch, accumulate, ws, ws_bytes,
                            hipStream_t(stream));
+  });
+}
+
+int caramel_residual_norm(caramel_plan* p, const void* const* gain, uint64_t width, float eps, const uint64_t* tokens,
+                          const void* const* x, const void* const* residual, uint32_t dtype, uint64_t pitch, void* const* sum,
+                          void* const* y, float* const* rstd, void* const* checkpoint, void* stream) {
+  return guarded([&] {
+    return residual_norm(p, gain, width, eps, tokens, x, residual, dtype, pitch, sum, y, rstd, checkpoint, hipStream_t(stream));
+  });
+}
+
+int caramel_residual_norm_workspace(const caramel_plan* p, uint32_t gain_tensor, const uint64_t* tokens, uint64_t* bytes) {
+  return guarded([&] { return residual_norm_workspace(p, gain_tensor, tokens, bytes); });
+}
+
+int caramel_residual_norm_gradient(caramel_plan* p, uint32_t gain_tensor, const void* const* gain, const uint64_t* tokens,
+                                   const void* const* x, const float* const* rstd, const void* const* dy, const void* const* dsum,
+                                   uint32_t dtype, uint64_t pitch, void* const* dx, int accumulate, void* ws, uint64_t ws_bytes,
+                                   void* stream) {
+  return guarded([&] {
+    return residual_norm_gradient(p, gain_tensor, gain, tokens, x, rstd, dy, dsum, dtype, pitch, dx, accumulate, ws, ws_bytes,
+                                  hipStream_t(stream));
   });
 }
 

@@ -1,6 +1,6 @@
-// Kernels that fill a plan's gradient tensors: the embedding lookup and its gradient, activation
-// checkpoints in 8 bits, and the weight and bias gradients that read them.  Launch wrappers; the
-// arguments have been checked by the entry points.
+// Kernels that fill a plan's gradient tensors, and those of a training step before and between them: the
+// embedding lookup and its gradient, activation checkpoints in 8 bits, the weight and bias gradients that
+// read them, the residual norm and its gradient.  Launch wrappers; the arguments have been checked by the entry points.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -42,6 +42,35 @@ hipError_t in_groups(ARGS a, const AllWorkers& v, LAUNCH&& launch) {
       a.w.c[w] = v.c[g + w];
       a.w.d[w] = v.d[g + w];
       a.w.tokens[w] = v.tokens[g + w];
+    }
+    const hipError_t e = launch(a, g);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// The same for calls with more buffers, or with another count per worker.  A buffer that a call goes without has address 0.
+template <int N>
+struct AllBuffers {
+  uint64_t at[N][CARAMEL_MAX_WORLD];
+  uint32_t tokens[CARAMEL_MAX_WORLD];
+  uint32_t more[CARAMEL_MAX_WORLD];
+};
+template <int N>
+struct Buffers {
+  uint64_t at[N][kGroup];
+  uint32_t tokens[kGroup];
+  uint32_t more[kGroup];
+};
+
+template <typename ARGS, int N, typename LAUNCH>
+hipError_t in_groups(ARGS a, const AllBuffers<N>& v, LAUNCH&& launch) {
+  for (uint32_t g = 0; g < a.all; g += kGroup) {
+    a.world = a.all - g < kGroup ? a.all - g : kGroup;
+    for (uint32_t w = 0; w < a.world; ++w) {
+      for (int i = 0; i < N; ++i) a.w.at[i][w] = v.at[i][g + w];
+      a.w.tokens[w] = v.tokens[g + w];
+      a.w.more[w] = v.more[g + w];
     }
     const hipError_t e = launch(a, g);
     if (e != hipSuccess) return e;
@@ -99,5 +128,32 @@ struct WeightGradientArgs {
 };
 uint64_t weight_gradient_workspace(uint32_t world, uint32_t features, uint32_t outputs, uint32_t max_tokens);
 hipError_t launch_weight_gradient(const WeightGradientArgs& args, const AllWorkers& v, hipStream_t s);
+
+constexpr uint32_t kNormWidth = 32768;  // most columns: a row stays in the registers of one workgroup
+
+enum { kNormX, kNormResidual, kNormSum, kNormY, kNormRstd, kNormGain, kNormCheckpoint, kNormBuffers };
+struct NormArgs {
+  Buffers<kNormBuffers> w;
+  uint32_t world, all;  // workers of the launch, of the call
+  uint32_t max_tokens;  // of all workers
+  uint32_t width;
+  uint64_t pitch;  // of all rows, elements
+  float eps;
+  bool bf16, gain_bf16, residual, checkpoint;
+};
+hipError_t launch_norm(const NormArgs& args, const AllBuffers<kNormBuffers>& v, hipStream_t s);
+
+enum { kNormGradX, kNormGradRstd, kNormGradDy, kNormGradDsum, kNormGradDx, kNormGradGain, kNormGradOut, kNormGradBuffers };
+struct NormGradientArgs {
+  Buffers<kNormGradBuffers> w;
+  uint32_t world, all;  // workers of the launch, of the call
+  uint32_t max_tokens;  // of all workers
+  uint32_t width;
+  uint64_t pitch;
+  bool bf16, gain_bf16, dsum, accumulate;  // gain_bf16: the plan's dtype, of gain and its gradient
+  unsigned char* ws;
+};
+uint64_t norm_gradient_workspace(uint32_t world, uint32_t width, uint32_t max_tokens);
+hipError_t launch_norm_gradient(const NormGradientArgs& args, const AllBuffers<kNormGradBuffers>& v, hipStream_t s);
 
 }  // namespace caramel

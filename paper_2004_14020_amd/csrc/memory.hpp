@@ -9,14 +9,14 @@
 namespace caramel {
 
 // Buffers are rows of equal length, `pitch` bytes apart; those in one piece are a single row.  What lies between the rows is not the
-// buffer's, so that workers' rows may interleave in one array.  Buffers of several rows all have the same pitch within a call
-// (a call has one kind of them).
+// buffer's, so that workers' rows may interleave in one array.  Rows of different pitch may not: such buffers overlap where the
+// stretches from their first to their last byte do.
 struct Memory {
   struct Span {
     uint64_t lo, hi, row, pitch;
     bool written;
   };
-  Span spans[4 * CARAMEL_MAX_WORLD + 1];  // four buffers of every worker, and a workspace
+  Span spans[12 * CARAMEL_MAX_WORLD + 1];  // twelve buffers of every worker, and a workspace
   uint32_t n = 0;
 
   void add(uint64_t at, uint64_t bytes, bool written) {
@@ -28,6 +28,7 @@ struct Memory {
   }
   // x begins first, and y before x ends.
   static bool share(const Span& x, const Span& y) {
+    if (x.pitch != y.pitch && x.hi - x.lo > x.row && y.hi - y.lo > y.row) return true;
     const uint64_t down = (y.lo - x.lo) / x.pitch, right = (y.lo - x.lo) % x.pitch;
     const bool next = (down + 1) * x.pitch < x.hi - x.lo;  // x has a row after the one that y begins beside
     return right < x.row || (next && right + y.row > x.pitch);

@@ -1,0 +1,81 @@
+"""The calls of a training step around the gradients: sizes and refusals.  No GPU call is made."""
+import ctypes as C
+import math
+import random
+
+import pytest
+
+import paper_2004_14020_amd as cm
+
+from test_layers_host import A, T, refused
+
+E = cm.binding.EINVAL
+
+
+@pytest.fixture
+def plan():
+    p = cm.Plan(2, [8 * 16, 16, 24, 1 << 20])
+    yield p
+    p.close()
+
+
+NORM = dict(gain=[A, A], width=16, tokens=[3, 3], x=[2 * A, 3 * A], y=[4 * A, 5 * A], rstd=[6 * A, 7 * A])
+MORE = dict(residual=[8 * A, 9 * A], sum=[10 * A, 11 * A], checkpoint=[12 * A, 13 * A])
+
+
+@pytest.mark.parametrize("change", [
+    dict(width=0), dict(width=32769, pitch=32769), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.inf), dict(eps=math.nan), dict(dtype=2),
+    dict(tokens=[T, 1]), dict(pitch=15), dict(pitch=(1 << 23) + 1), dict(tokens=[1 << 25, 1], pitch=1 << 23),
+    dict(gain=[A, None]), dict(gain=[A, A + 2]), dict(x=[None, A]), dict(x=[2 * A, 3 * A + 1]), dict(y=[4 * A, None]),
+    dict(y=[4 * A + 2, 5 * A]), dict(rstd=[None, 7 * A]), dict(rstd=[6 * A + 2, 7 * A]), dict(residual=None), dict(sum=None),
+    dict(residual=[8 * A, None]), dict(sum=[None, 11 * A]), dict(checkpoint=[12 * A, None]), dict(checkpoint=[12 * A + 8, 13 * A]),
+    # what is written overlaps: the other worker's, an input, the gain
+    dict(y=[4 * A, 4 * A]), dict(y=[2 * A, 5 * A]), dict(y=[A + 32, 5 * A]), dict(sum=[8 * A, 11 * A]), dict(sum=[2 * A, 11 * A]),
+    dict(sum=[4 * A + 64, 11 * A]), dict(rstd=[2 * A, 7 * A]), dict(rstd=[6 * A, 6 * A + 8]), dict(checkpoint=[12 * A, 12 * A]),
+    dict(checkpoint=[4 * A, 13 * A]),
+], ids=str)
+def test_norm_refusals(plan, change):
+    refused(E, plan.residual_norm, **{**NORM, **MORE, **change})
+
+
+NGRAD = dict(gain_tensor=1, gain=[A, A], tokens=[3, 3], x=[2 * A, 3 * A], rstd=[6 * A, 7 * A], dy=[8 * A, 9 * A], dx=[4 * A, 5 * A],
+             ws=10 * A, ws_bytes=1 << 16)
+
+
+@pytest.mark.parametrize("change", [
+    dict(gain_tensor=4, pitch=16), dict(gain_tensor=3), dict(dtype=2), dict(tokens=[1, T]), dict(pitch=15), dict(pitch=(1 << 23) + 1),
+    dict(gain=[None, A]), dict(gain=[A, A + 2]), dict(x=[2 * A, None]), dict(rstd=[6 * A, None]), dict(rstd=[6 * A, 7 * A + 2]),
+    dict(dy=[None, 9 * A]), dict(dsum=[None, 9 * A]), dict(dsum=[A, A + 2]), dict(dx=[4 * A, None]), dict(ws=None), dict(ws=10 * A + 8),
+    dict(ws_bytes=16), dict(tokens=[1 << 25, 1], pitch=1 << 23),
+], ids=str)
+def test_norm_gradient_refusals(plan, change):
+    refused(E, plan.residual_norm_gradient, **{**NGRAD, **change})
+
+
+def test_norm_gradient_needs_a_bound_plan(plan):
+    refused(cm.binding.ESTATE, plan.residual_norm_gradient, **NGRAD)
+    with pytest.raises(ValueError):
+        plan.residual_norm_gradient(**{**NGRAD, "gain_tensor": -1})
+    for bad in ((4, [1, 1]), (3, [1, 1]), (1, [T, 1])):
+        refused(E, plan.residual_norm_workspace, *bad)
+
+
+def test_norm_null_arguments(plan):
+    L, two, n, b = cm.lib(), (C.c_void_p * 2)(A, 2 * A), (C.c_uint64 * 2)(0, 0), C.c_uint64()
+    forward = [plan._h, two, 16, 1e-5, n, two, None, 0, 16, None, two, two, None, None]
+    backward = [plan._h, 1, two, n, two, two, two, None, 0, 16, two, 0, A, 1 << 20, None]
+    for call, args, needed in ((L.caramel_residual_norm, forward, (0, 1, 4, 5, 10, 11)),
+                               (L.caramel_residual_norm_gradient, backward, (0, 2, 3, 4, 5, 6, 10)),
+                               (L.caramel_residual_norm_workspace, [plan._h, 1, n, C.byref(b)], (0, 2, 3))):
+        for i in needed:
+            assert call(*[None if k == i else v for k, v in enumerate(args)]) == E, (call, i)
+
+
+def test_norm_workspaces_serve_fewer_tokens():
+    rng = random.Random(4)
+    for _ in range(200):
+        plan = cm.Plan(rng.choice([1, 2, 3, 8, 16, 17, 64]), [rng.randint(1, 4096)])
+        tokens = sorted(int(2 ** rng.uniform(0, 25)) for _ in range(30))
+        sizes = [plan.residual_norm_workspace(0, [n] * plan.cfg.world) for n in tokens]
+        assert sizes == sorted(sizes)
+        plan.close()
