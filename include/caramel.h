@@ -395,6 +395,35 @@ int caramel_residual_norm_gradient(caramel_plan* plan, uint32_t gain_tensor, con
                                    uint32_t dtype, uint64_t pitch, void* const* dx, int accumulate, void* ws, uint64_t ws_bytes,
                                    void* stream);
 
+/* A gated linear recurrence along packed sequences, every channel by itself:
+ *   a[t] = 1 / (1 + exp(-gate[w][t])),  states[w][t] = a[t] * states[w][t - 1] + (1 - a[t]) * input[w][t]
+ * Sequence s of worker w is its tokens starts[w][s] to starts[w][s + 1] - 1: starts[w] holds sequences[w] + 1 numbers (id_bytes, 4 or 8,
+ * each, signed, DEVICE memory) that do not descend, from 0 to tokens[w].  A sequence may be empty; tokens before the first one or behind the
+ * last belong to none, and their rows of the outputs are left as they are.  (Other numbers in starts give unspecified outputs, but
+ * no access outside the buffers.)
+ *   gate, input, states  rows of `channels` values of dtype; gate and input may be the halves of one matrix
+ *   before, after        fp32 [sequences][channels], optional: the states in front of every sequence (NULL: zeros) and behind it; an
+ *                        empty sequence's after is its before.  Sequences of one token with before and after are a step of serving.
+ * States are carried in fp32 and rounded where they are stored.  What a sequence holds, infinities and NaN too, reaches no other.
+ * EINVAL besides the above: more than 2^25 sequences at a worker. */
+int caramel_recurrence_workspace(const caramel_plan* plan, uint64_t channels, const uint64_t* tokens, uint64_t* bytes);
+int caramel_recurrence(caramel_plan* plan, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences,
+                       const void* const* starts, uint32_t id_bytes, const void* const* gate, const void* const* input, uint32_t dtype,
+                       uint64_t pitch, const float* const* before, void* const* states, uint64_t states_pitch, float* const* after,
+                       void* ws, uint64_t ws_bytes, void* stream);
+
+/* Its gradient, from gate, input and before as they were, the stored states, dstates = the gradient of the states (rows as states)
+ * and dafter = that of after (fp32, optional: zeros).  With e[t] = dstates[t] + a[t + 1] * e[t + 1] (a sequence's last token:
+ * + dafter) and p[t] = the state before token t (as stored; a sequence's first token: before):
+ *   dinput[t] = (1 - a[t]) * e[t],  dgate[t] = a[t] * (1 - a[t]) * e[t] * (p[t] - input[t])       rows as gate and input
+ *   dbefore[s] = a * e of the sequence's first token (an empty one: dafter)                       fp32, optional
+ * The workspace is as large as that of the recurrence. */
+int caramel_recurrence_gradient(caramel_plan* plan, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences,
+                                const void* const* starts, uint32_t id_bytes, const void* const* gate, const void* const* input,
+                                uint32_t dtype, uint64_t pitch, const float* const* before, const void* const* states,
+                                const void* const* dstates, uint64_t states_pitch, const float* const* dafter, void* const* dgate,
+                                void* const* dinput, float* const* dbefore, void* ws, uint64_t ws_bytes, void* stream);
+
 /* ---- launch tuning and timing (do not change results) ------------------------------------ */
 
 /* How the work is cut up for the GPU.  A "run" is a maximal piece of one tensor (or of the fused

@@ -145,6 +145,19 @@ def caramel_residual_norm_gradient(plan: Plan, gain_tensor, gain, tokens, x, rst
     plan.residual_norm_gradient(gain_tensor, gain, tokens, x, rstd, dy, dx, ws, ws_bytes, **kw)
 
 
+def caramel_recurrence_workspace(plan: Plan, channels, tokens) -> int:
+    return plan.recurrence_workspace(channels, tokens)
+
+
+def caramel_recurrence(plan: Plan, channels, tokens, sequences, starts, gate, input, states, ws, ws_bytes, **kw) -> None:
+    plan.recurrence(channels, tokens, sequences, starts, gate, input, states, ws, ws_bytes, **kw)
+
+
+def caramel_recurrence_gradient(plan: Plan, channels, tokens, sequences, starts, gate, input, states, dstates, dgate, dinput, ws,
+                                ws_bytes, **kw) -> None:
+    plan.recurrence_gradient(channels, tokens, sequences, starts, gate, input, states, dstates, dgate, dinput, ws, ws_bytes, **kw)
+
+
 def caramel_profile(plan: Plan, level: int) -> None:
     plan.profile(level)
 

@@ -38,6 +38,7 @@ EXPORTS = (
     "caramel_embedding_lookup", "caramel_embedding_workspace", "caramel_embedding_gradient", "caramel_checkpoint_bytes",
     "caramel_checkpoint_store", "caramel_checkpoint_load", "caramel_weight_gradient_workspace", "caramel_weight_gradient",
     "caramel_residual_norm", "caramel_residual_norm_workspace", "caramel_residual_norm_gradient",
+    "caramel_recurrence_workspace", "caramel_recurrence", "caramel_recurrence_gradient",
 )
 
 
@@ -138,6 +139,9 @@ def lib() -> C.CDLL:
     L.caramel_residual_norm.argtypes = [P, PP, U64, C.c_float, PU64, PP, PP, U32, U64, PP, PP, PP, PP, P]
     L.caramel_residual_norm_workspace.argtypes = [P, U32, PU64, PU64]
     L.caramel_residual_norm_gradient.argtypes = [P, U32, PP, PU64, PP, PP, PP, PP, U32, U64, PP, C.c_int, P, U64, P]
+    L.caramel_recurrence_workspace.argtypes = [P, U64, PU64, PU64]
+    L.caramel_recurrence.argtypes = [P, U64, PU64, PU64, PP, U32, PP, PP, U32, U64, PP, PP, U64, PP, P, U64, P]
+    L.caramel_recurrence_gradient.argtypes = [P, U64, PU64, PU64, PP, U32, PP, PP, U32, U64, PP, PP, PP, U64, PP, PP, PP, PP, P, U64, P]
     _lib = L
     return L
 
@@ -381,6 +385,42 @@ class Plan:
             per(C.c_void_p, rstd, "rstd"), per(C.c_void_p, dy, "dy"), self._optional(dsum, "dsum"),
             self.cfg.dtype if dtype is None else dtype, self._outputs(gain_tensor, 1) if pitch is None else pitch,
             per(C.c_void_p, dx, "dx"), int(accumulate), ws, ws_bytes, stream))
+
+    def recurrence_workspace(self, channels: int, tokens: Sequence[int]) -> int:
+        """Bytes of workspace that recurrence and recurrence_gradient need for these sizes (may be 0)."""
+        n = C.c_uint64()
+        _check(lib().caramel_recurrence_workspace(self._h, channels, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        return n.value
+
+    def recurrence(self, channels: int, tokens: Sequence[int], sequences: Sequence[int], starts: Sequence[int],
+                   gate: Sequence[int], input: Sequence[int], states: Sequence[int], ws: Optional[int], ws_bytes: int,
+                   before: Optional[Sequence[int]] = None, after: Optional[Sequence[int]] = None, id_bytes: int = 8,
+                   dtype: Optional[int] = None, pitch: Optional[int] = None, states_pitch: Optional[int] = None,
+                   stream: int = 0) -> None:
+        """dtype None: the plan's; pitches None: rows without gaps."""
+        per, opt = self._per_worker, self._optional
+        _check(lib().caramel_recurrence(
+            self._h, channels, per(C.c_uint64, tokens, "tokens"), per(C.c_uint64, sequences, "sequences"),
+            per(C.c_void_p, starts, "starts"), id_bytes, per(C.c_void_p, gate, "gate"), per(C.c_void_p, input, "input"),
+            self.cfg.dtype if dtype is None else dtype, channels if pitch is None else pitch, opt(before, "before"),
+            per(C.c_void_p, states, "states"), channels if states_pitch is None else states_pitch, opt(after, "after"), ws, ws_bytes,
+            stream))
+
+    def recurrence_gradient(self, channels: int, tokens: Sequence[int], sequences: Sequence[int], starts: Sequence[int],
+                            gate: Sequence[int], input: Sequence[int], states: Sequence[int], dstates: Sequence[int],
+                            dgate: Sequence[int], dinput: Sequence[int], ws: Optional[int], ws_bytes: int,
+                            before: Optional[Sequence[int]] = None, dafter: Optional[Sequence[int]] = None,
+                            dbefore: Optional[Sequence[int]] = None, id_bytes: int = 8, dtype: Optional[int] = None,
+                            pitch: Optional[int] = None, states_pitch: Optional[int] = None, stream: int = 0) -> None:
+        """dtype None: the plan's; pitches None: rows without gaps."""
+        per, opt = self._per_worker, self._optional
+        _check(lib().caramel_recurrence_gradient(
+            self._h, channels, per(C.c_uint64, tokens, "tokens"), per(C.c_uint64, sequences, "sequences"),
+            per(C.c_void_p, starts, "starts"), id_bytes, per(C.c_void_p, gate, "gate"), per(C.c_void_p, input, "input"),
+            self.cfg.dtype if dtype is None else dtype, channels if pitch is None else pitch, opt(before, "before"),
+            per(C.c_void_p, states, "states"), per(C.c_void_p, dstates, "dstates"), channels if states_pitch is None else states_pitch,
+            opt(dafter, "dafter"), per(C.c_void_p, dgate, "dgate"), per(C.c_void_p, dinput, "dinput"), opt(dbefore, "dbefore"), ws,
+            ws_bytes, stream))
 
     def profile(self, level: int) -> None:
         _check(lib().caramel_profile(self._h, int(level)))

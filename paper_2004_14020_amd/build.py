@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libcaramel.so")
 SOURCES = ["plan.cpp", "schedule.cpp", "tiles.cpp", "slices.cpp", "kernels.hip", "probe.hip", "embedding.hip",
-           "checkpoint.hip", "weight_gradient.hip", "norm.hip", "api.hip"]
+           "checkpoint.hip", "weight_gradient.hip", "norm.hip", "recurrence.hip",
+           "api.hip"]
 
 
 def hipcc() -> str:

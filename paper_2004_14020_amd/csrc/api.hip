@@ -1479,6 +1479,124 @@ int residual_norm_gradient(caramel_plan* p, uint32_t gain_tensor, const void* co
   return CARAMEL_OK;
 }
 
+int recurrence_workspace(const caramel_plan* p, uint64_t channels, const uint64_t* tokens, uint64_t* bytes) {
+  if (!p || !bytes) return fail(CARAMEL_EINVAL, "NULL argument");
+  uint32_t n[CARAMEL_MAX_WORLD], most = 0;
+  if (int rc = check_columns("channels", channels)) return rc;
+  if (int rc = take_tokens(p, tokens, n, &most)) return rc;
+  *bytes = recurrence_workspace_bytes(p->host.cfg.world, uint32_t(channels), most);
+  return CARAMEL_OK;
+}
+
+// What the recurrence and its gradient have in common: sizes, sequences, and what both read.
+int take_recurrence(caramel_plan* p, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences, const void* const* starts,
+                    uint32_t id_bytes, const void* const* gate, const void* const* input, uint32_t dtype, uint64_t pitch,
+                    const float* const* before, uint64_t states_pitch, void* ws, uint64_t ws_bytes, RecurrenceArgs& a,
+                    AllBuffers<kRecBuffers>& v, Memory& m) {
+  if (int rc = check_columns("channels", channels)) return rc;
+  if (id_bytes != 4 && id_bytes != 8) return fail(CARAMEL_EINVAL, "id_bytes must be 4 or 8, is %u", id_bytes);
+  if (int rc = check_dtype("dtype", dtype)) return rc;
+  const uint64_t es = size_of(dtype);
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
+  if (!sequences) return fail(CARAMEL_EINVAL, "sequences is NULL");
+  a.all = p->host.cfg.world;
+  for (uint32_t w = 0; w < a.all; ++w) {
+    if (sequences[w] > kMaxTokens)
+      return fail(CARAMEL_EINVAL, "sequences[%u] = %llu is more than 2^25", w, (unsigned long long)sequences[w]);
+    v.more[w] = uint32_t(sequences[w]);
+  }
+  if (int rc = check_rows("pitch", pitch, channels, a.max_tokens)) return rc;
+  if (int rc = check_rows("states_pitch", states_pitch, channels, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "starts", starts, v.tokens, id_bytes, v.at[kRecStarts])) return rc;
+  if (int rc = take_pointers(p, "gate", gate, v.tokens, es, v.at[kRecGate])) return rc;
+  if (int rc = take_pointers(p, "input", input, v.tokens, es, v.at[kRecInput])) return rc;
+  if (int rc = take_optional(p, "before", reinterpret_cast<const void* const*>(before), v.tokens, 4, v.at[kRecBefore])) return rc;
+  const uint64_t need = recurrence_workspace_bytes(a.all, uint32_t(channels), a.max_tokens);
+  if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
+  m.add(reinterpret_cast<uint64_t>(ws), need, true);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    const uint64_t n = v.tokens[w];
+    if (!n) continue;
+    m.add(v.at[kRecStarts][w], (uint64_t(v.more[w]) + 1) * id_bytes, false);
+    m.add_rows(v.at[kRecGate][w], n, pitch, channels, es, false);
+    m.add_rows(v.at[kRecInput][w], n, pitch, channels, es, false);
+    if (before) m.add(v.at[kRecBefore][w], v.more[w] * channels * 4, false);
+  }
+  a.channels = uint32_t(channels);
+  a.pitch = pitch;
+  a.states_pitch = states_pitch;
+  a.bf16 = dtype == CARAMEL_BF16;
+  a.starts64 = id_bytes == 8;
+  a.ws = static_cast<unsigned char*>(ws);
+  return CARAMEL_OK;
+}
+
+int recurrence(caramel_plan* p, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences, const void* const* starts,
+               uint32_t id_bytes, const void* const* gate, const void* const* input, uint32_t dtype, uint64_t pitch,
+               const float* const* before, void* const* states, uint64_t states_pitch, float* const* after, void* ws, uint64_t ws_bytes,
+               hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  RecurrenceArgs a{};
+  AllBuffers<kRecBuffers> v{};
+  Memory m;
+  if (int rc = take_recurrence(p, channels, tokens, sequences, starts, id_bytes, gate, input, dtype, pitch, before, states_pitch, ws,
+                               ws_bytes, a, v, m))
+    return rc;
+  const uint64_t es = size_of(dtype);
+  if (int rc = take_pointers(p, "states", states, v.tokens, es, v.at[kRecStates])) return rc;
+  if (int rc = take_optional(p, "after", reinterpret_cast<const void* const*>(after), v.tokens, 4, v.at[kRecAfter])) return rc;
+  for (uint32_t w = 0; w < a.all; ++w) {
+    if (!v.tokens[w]) continue;
+    m.add_rows(v.at[kRecStates][w], v.tokens[w], states_pitch, channels, es, true);
+    if (after) m.add(v.at[kRecAfter][w], v.more[w] * channels * 4, true);
+  }
+  if (int rc = check_memory(m)) return rc;
+  if (int rc = need_device(p)) return rc;
+  if (tracing())
+    std::fprintf(stderr, "caramel: recurrence stream %p, %u workers, up to %u tokens, %u channels\n", (void*)stream, a.all,
+                 a.max_tokens, a.channels);
+  HIP_TRY(launch_recurrence(a, v, stream));
+  return CARAMEL_OK;
+}
+
+int recurrence_gradient(caramel_plan* p, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences,
+                        const void* const* starts, uint32_t id_bytes, const void* const* gate, const void* const* input, uint32_t dtype,
+                        uint64_t pitch, const float* const* before, const void* const* states, const void* const* dstates,
+                        uint64_t states_pitch, const float* const* dafter, void* const* dgate, void* const* dinput,
+                        float* const* dbefore, void* ws, uint64_t ws_bytes, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  RecurrenceArgs a{};
+  AllBuffers<kRecBuffers> v{};
+  Memory m;
+  if (int rc = take_recurrence(p, channels, tokens, sequences, starts, id_bytes, gate, input, dtype, pitch, before, states_pitch, ws,
+                               ws_bytes, a, v, m))
+    return rc;
+  const uint64_t es = size_of(dtype);
+  if (int rc = take_pointers(p, "states", states, v.tokens, es, v.at[kRecStates])) return rc;
+  if (int rc = take_pointers(p, "dstates", dstates, v.tokens, es, v.at[kRecDstates])) return rc;
+  if (int rc = take_optional(p, "dafter", reinterpret_cast<const void* const*>(dafter), v.tokens, 4, v.at[kRecDafter])) return rc;
+  if (int rc = take_pointers(p, "dgate", dgate, v.tokens, es, v.at[kRecDgate])) return rc;
+  if (int rc = take_pointers(p, "dinput", dinput, v.tokens, es, v.at[kRecDinput])) return rc;
+  if (int rc = take_optional(p, "dbefore", reinterpret_cast<const void* const*>(dbefore), v.tokens, 4, v.at[kRecDbefore])) return rc;
+  for (uint32_t w = 0; w < a.all; ++w) {
+    const uint64_t n = v.tokens[w];
+    if (!n) continue;
+    m.add_rows(v.at[kRecStates][w], n, states_pitch, channels, es, false);
+    m.add_rows(v.at[kRecDstates][w], n, states_pitch, channels, es, false);
+    m.add_rows(v.at[kRecDgate][w], n, pitch, channels, es, true);
+    m.add_rows(v.at[kRecDinput][w], n, pitch, channels, es, true);
+    if (dafter) m.add(v.at[kRecDafter][w], v.more[w] * channels * 4, false);
+    if (dbefore) m.add(v.at[kRecDbefore][w], v.more[w] * channels * 4, true);
+  }
+  if (int rc = check_memory(m)) return rc;
+  if (int rc = need_device(p)) return rc;
+  if (tracing())
+    std::fprintf(stderr, "caramel: recurrence gradient stream %p, %u workers, up to %u tokens, %u channels\n", (void*)stream, a.all,
+                 a.max_tokens, a.channels);
+  HIP_TRY(launch_recurrence_gradient(a, v, stream));
+  return CARAMEL_OK;
+}
+
 }  // namespace
 
 int caramel_embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, uint64_t width, float scale,
@@ -1555,6 +1673,31 @@ int caramel_residual_norm_gradient(caramel_plan* p, uint32_t gain_tensor, const 
   return guarded([&] {
     return residual_norm_gradient(p, gain_tensor, gain, tokens, x, rstd, dy, dsum, dtype, pitch, dx, accumulate, ws, ws_bytes,
                                   hipStream_t(stream));
+  });
+}
+
+int caramel_recurrence_workspace(const caramel_plan* p, uint64_t channels, const uint64_t* tokens, uint64_t* bytes) {
+  return guarded([&] { return recurrence_workspace(p, channels, tokens, bytes); });
+}
+
+int caramel_recurrence(caramel_plan* p, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences,
+                       const void* const* starts, uint32_t id_bytes, const void* const* gate, const void* const* input, uint32_t dtype,
+                       uint64_t pitch, const float* const* before, void* const* states, uint64_t states_pitch, float* const* after,
+                       void* ws, uint64_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return recurrence(p, channels, tokens, sequences, starts, id_bytes, gate, input, dtype, pitch, before, states, states_pitch, after,
+                      ws, ws_bytes, hipStream_t(stream));
+  });
+}
+
+int caramel_recurrence_gradient(caramel_plan* p, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences,
+                                const void* const* starts, uint32_t id_bytes, const void* const* gate, const void* const* input,
+                                uint32_t dtype, uint64_t pitch, const float* const* before, const void* const* states,
+                                const void* const* dstates, uint64_t states_pitch, const float* const* dafter, void* const* dgate,
+                                void* const* dinput, float* const* dbefore, void* ws, uint64_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return recurrence_gradient(p, channels, tokens, sequences, starts, id_bytes, gate, input, dtype, pitch, before, states, dstates,
+                               states_pitch, dafter, dgate, dinput, dbefore, ws, ws_bytes, hipStream_t(stream));
   });
 }
 

@@ -1,6 +1,6 @@
 // Kernels that fill a plan's gradient tensors, and those of a training step before and between them: the
 // embedding lookup and its gradient, activation checkpoints in 8 bits, the weight and bias gradients that
-// read them, the residual norm and its gradient.  Launch wrappers; the arguments have been checked by the entry points.
+// read them, the residual norm and the gated recurrence with their gradients.  Launch wrappers; the arguments have been checked by the entry points.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -155,5 +155,22 @@ struct NormGradientArgs {
 };
 uint64_t norm_gradient_workspace(uint32_t world, uint32_t width, uint32_t max_tokens);
 hipError_t launch_norm_gradient(const NormGradientArgs& args, const AllBuffers<kNormGradBuffers>& v, hipStream_t s);
+
+enum {
+  kRecStarts, kRecGate, kRecInput, kRecBefore, kRecStates, kRecAfter,   // after: forward
+  kRecDstates, kRecDafter, kRecDgate, kRecDinput, kRecDbefore, kRecBuffers  // gradient
+};
+struct RecurrenceArgs {
+  Buffers<kRecBuffers> w;  // more: sequences
+  uint32_t world, all;     // workers of the launch, of the call
+  uint32_t max_tokens;     // of all workers
+  uint32_t channels;
+  uint64_t pitch, states_pitch;  // of gates, inputs and their gradients; of states and theirs; elements
+  bool bf16, starts64;
+  unsigned char* ws;
+};
+uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, uint32_t max_tokens);
+hipError_t launch_recurrence(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);
+hipError_t launch_recurrence_gradient(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);
 
 }  // namespace caramel

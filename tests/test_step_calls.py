@@ -79,3 +79,56 @@ def test_norm_workspaces_serve_fewer_tokens():
         sizes = [plan.residual_norm_workspace(0, [n] * plan.cfg.world) for n in tokens]
         assert sizes == sorted(sizes)
         plan.close()
+
+
+REC = dict(channels=16, tokens=[3, 3], sequences=[1, 2], starts=[A, A + 64], gate=[2 * A, 3 * A], input=[2 * A + 64, 3 * A + 64],
+           pitch=32, ws=None, ws_bytes=0, before=[20 * A, 21 * A])
+FORWARD = dict(states=[4 * A, 5 * A], after=[6 * A, 7 * A])
+BACKWARD = dict(states=[4 * A, 5 * A], dstates=[6 * A, 7 * A], dgate=[8 * A, 9 * A], dinput=[8 * A + 64, 9 * A + 64],
+                dafter=[10 * A, 11 * A], dbefore=[12 * A, 13 * A])
+BOTH = [dict(channels=0), dict(channels=(1 << 20) + 1, pitch=1 << 22), dict(id_bytes=2), dict(dtype=2), dict(tokens=[T, 1]),
+        dict(sequences=[1, T]), dict(pitch=15), dict(pitch=(1 << 23) + 1), dict(states_pitch=15), dict(states_pitch=(1 << 23) + 1),
+        dict(tokens=[1 << 25, 1], pitch=1 << 23), dict(starts=[A, None]), dict(starts=[A, A + 4]), dict(gate=[None, A]),
+        dict(gate=[2 * A + 2, 3 * A]), dict(input=[None, 3 * A]), dict(before=[20 * A, None]), dict(before=[20 * A + 2, 21 * A]),
+        dict(states=[4 * A, None]), dict(states=[4 * A + 2, 5 * A]), dict(tokens=[1000, 3]),
+        dict(tokens=[1000, 3], ws=30 * A + 8, ws_bytes=1 << 20), dict(tokens=[1000, 3], ws=30 * A, ws_bytes=16)]
+
+
+@pytest.mark.parametrize("change", BOTH + [
+    dict(after=[None, 7 * A]), dict(after=[6 * A, 6 * A]), dict(after=[20 * A, 7 * A]), dict(states=[2 * A, 5 * A]), dict(states=[A, 5 * A]),
+    dict(states=[4 * A, 4 * A + 128]), dict(states=[2 * A + 192, 5 * A]),                       # between rows of another pitch
+], ids=str)
+def test_recurrence_refusals(plan, change):
+    refused(E, plan.recurrence, **{**REC, **FORWARD, **change})
+
+
+@pytest.mark.parametrize("change", BOTH + [
+    dict(dstates=[6 * A, None]), dict(dstates=[6 * A + 2, 7 * A]), dict(dafter=[None, 11 * A]), dict(dgate=[None, 9 * A]),
+    dict(dinput=[8 * A + 64, None]), dict(dbefore=[12 * A, None]), dict(dgate=[2 * A, 9 * A]), dict(dinput=[8 * A, 9 * A + 64]),
+    dict(dinput=[8 * A + 60, 9 * A + 64]), dict(dgate=[6 * A, 9 * A]), dict(dbefore=[10 * A, 13 * A]), dict(dbefore=[20 * A, 13 * A]),
+], ids=str)
+def test_recurrence_gradient_refusals(plan, change):
+    refused(E, plan.recurrence_gradient, **{**REC, **BACKWARD, **change})
+
+
+def test_recurrence_null_arguments(plan):
+    L, two, n, b = cm.lib(), (C.c_void_p * 2)(A, 2 * A), (C.c_uint64 * 2)(0, 0), C.c_uint64()
+    forward = [plan._h, 16, n, n, two, 8, two, two, 0, 16, None, two, 16, None, None, 0, None]
+    backward = [plan._h, 16, n, n, two, 8, two, two, 0, 16, None, two, two, 16, None, two, two, None, None, 0, None]
+    for call, args, needed in ((L.caramel_recurrence, forward, (0, 2, 3, 4, 6, 7, 11)),
+                               (L.caramel_recurrence_gradient, backward, (0, 2, 3, 4, 6, 7, 11, 12, 15, 16)),
+                               (L.caramel_recurrence_workspace, [plan._h, 16, n, C.byref(b)], (0, 2, 3))):
+        for i in needed:
+            assert call(*[None if k == i else v for k, v in enumerate(args)]) == E, (call, i)
+    for bad in ((0, [1, 1]), ((1 << 20) + 1, [1, 1]), (16, [1, T])):
+        refused(E, plan.recurrence_workspace, *bad)
+
+
+def test_recurrence_workspaces_serve_fewer_tokens():
+    rng = random.Random(4)
+    for _ in range(200):
+        plan, channels = cm.Plan(rng.choice([1, 2, 3, 8, 16, 17, 64]), [1]), int(2 ** rng.uniform(0, 20))
+        tokens = sorted(int(2 ** rng.uniform(0, 25)) for _ in range(30))
+        sizes = [plan.recurrence_workspace(channels, [n] * plan.cfg.world) for n in tokens]
+        assert sizes == sorted(sizes)
+        plan.close()
