@@ -424,6 +424,28 @@ int caramel_recurrence_gradient(caramel_plan* plan, uint64_t channels, const uin
                                 const void* const* dstates, uint64_t states_pitch, const float* const* dafter, void* const* dgate,
                                 void* const* dinput, float* const* dbefore, void* ws, uint64_t ws_bytes, void* stream);
 
+/* The loss of a student that learns from a teacher's best logits, and from labels, and its gradient.  Per token, with z = its logits,
+ * T = temperature, Q = softmax(z / T), q = softmax(z), and P = softmax(t / T) over the teacher's entries (id, t) that are there:
+ *   loss       = soft * sum of P * (ln P - ln Q[id])  +  hard * (-ln q[label])
+ *   dlogits[j] = scale * (soft / T * (Q[j] - sum of the P with id j)  +  hard * (q[j] - (j == label)))      rounded to dtype
+ *   logits, dlogits  rows of `vocab` values of dtype.  dlogits may be NULL (the loss alone), or the logits themselves (all of a worker's rows,
+ *                    the same pitch)
+ *   teacher_ids      [tokens][top] numbers of id_bytes (4 or 8), signed; one below 0 or from vocab on is an entry that is not there.  An id
+ *                    may come twice
+ *   teacher_logits   [tokens][top] values of teacher_dtype; an entry of -infinity has P = 0, as if it were not there
+ *   labels           [tokens], as teacher_ids; one outside the vocabulary is none.  Not read if hard is 0, and may be NULL then
+ *   loss             fp32 [tokens]; not scaled
+ * A term with weight 0 is left out.  A token whose teacher has no entry has no first term, one without a label no second; a token with neither
+ * has a loss of 0 and a gradient of zeros, whatever its logits.  Where P or q ask for a logit of -infinity the loss is infinite;
+ * logits of which one is NaN or +infinity, or all are -infinity, give NaN.
+ * EINVAL besides the above: top not 1 to 256, temperature not 1/1024 to 1024, soft or hard negative or both 0, hard without labels. */
+int caramel_distillation_workspace(const caramel_plan* plan, uint64_t vocab, uint32_t top, const uint64_t* tokens, uint64_t* bytes);
+int caramel_distillation(caramel_plan* plan, uint64_t vocab, const uint64_t* tokens, const void* const* logits, uint32_t dtype,
+                         uint64_t pitch, const void* const* teacher_ids, const void* const* labels, uint32_t id_bytes,
+                         const void* const* teacher_logits, uint32_t teacher_dtype, uint32_t top, float temperature, float soft,
+                         float hard, float scale, float* const* loss, void* const* dlogits, uint64_t dlogits_pitch, void* ws,
+                         uint64_t ws_bytes, void* stream);
+
 /* ---- launch tuning and timing (do not change results) ------------------------------------ */
 
 /* How the work is cut up for the GPU.  A "run" is a maximal piece of one tensor (or of the fused

@@ -158,6 +158,14 @@ def caramel_recurrence_gradient(plan: Plan, channels, tokens, sequences, starts,
     plan.recurrence_gradient(channels, tokens, sequences, starts, gate, input, states, dstates, dgate, dinput, ws, ws_bytes, **kw)
 
 
+def caramel_distillation_workspace(plan: Plan, vocab, top, tokens) -> int:
+    return plan.distillation_workspace(vocab, top, tokens)
+
+
+def caramel_distillation(plan: Plan, vocab, tokens, logits, teacher_ids, teacher_logits, top, loss, ws, ws_bytes, **kw) -> None:
+    plan.distillation(vocab, tokens, logits, teacher_ids, teacher_logits, top, loss, ws, ws_bytes, **kw)
+
+
 def caramel_profile(plan: Plan, level: int) -> None:
     plan.profile(level)
 

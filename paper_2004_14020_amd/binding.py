@@ -39,6 +39,7 @@ EXPORTS = (
     "caramel_checkpoint_store", "caramel_checkpoint_load", "caramel_weight_gradient_workspace", "caramel_weight_gradient",
     "caramel_residual_norm", "caramel_residual_norm_workspace", "caramel_residual_norm_gradient",
     "caramel_recurrence_workspace", "caramel_recurrence", "caramel_recurrence_gradient",
+    "caramel_distillation_workspace", "caramel_distillation",
 )
 
 
@@ -142,6 +143,9 @@ def lib() -> C.CDLL:
     L.caramel_recurrence_workspace.argtypes = [P, U64, PU64, PU64]
     L.caramel_recurrence.argtypes = [P, U64, PU64, PU64, PP, U32, PP, PP, U32, U64, PP, PP, U64, PP, P, U64, P]
     L.caramel_recurrence_gradient.argtypes = [P, U64, PU64, PU64, PP, U32, PP, PP, U32, U64, PP, PP, PP, U64, PP, PP, PP, PP, P, U64, P]
+    F = C.c_float
+    L.caramel_distillation_workspace.argtypes = [P, U64, U32, PU64, PU64]
+    L.caramel_distillation.argtypes = [P, U64, PU64, PP, U32, U64, PP, PP, U32, PP, U32, U32, F, F, F, F, PP, PP, U64, P, U64, P]
     _lib = L
     return L
 
@@ -421,6 +425,28 @@ class Plan:
             per(C.c_void_p, states, "states"), per(C.c_void_p, dstates, "dstates"), channels if states_pitch is None else states_pitch,
             opt(dafter, "dafter"), per(C.c_void_p, dgate, "dgate"), per(C.c_void_p, dinput, "dinput"), opt(dbefore, "dbefore"), ws,
             ws_bytes, stream))
+
+    def distillation_workspace(self, vocab: int, top: int, tokens: Sequence[int]) -> int:
+        """Bytes of workspace that distillation needs for these sizes (may be 0)."""
+        n = C.c_uint64()
+        _check(lib().caramel_distillation_workspace(self._h, vocab, top, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        return n.value
+
+    def distillation(self, vocab: int, tokens: Sequence[int], logits: Sequence[int], teacher_ids: Sequence[int],
+                     teacher_logits: Sequence[int], top: int, loss: Sequence[int], ws: Optional[int], ws_bytes: int,
+                     labels: Optional[Sequence[int]] = None, dlogits: Optional[Sequence[int]] = None, temperature: float = 1.0,
+                     soft: float = 1.0, hard: float = 0.0, scale: float = 1.0, id_bytes: int = 8, dtype: Optional[int] = None,
+                     teacher_dtype: Optional[int] = None, pitch: Optional[int] = None, dlogits_pitch: Optional[int] = None,
+                     stream: int = 0) -> None:
+        """dlogits None: the loss alone; dtype None: the plan's; teacher_dtype None: dtype; pitches None: rows without gaps."""
+        per, opt = self._per_worker, self._optional
+        dtype = self.cfg.dtype if dtype is None else dtype
+        _check(lib().caramel_distillation(
+            self._h, vocab, per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, logits, "logits"), dtype,
+            vocab if pitch is None else pitch, per(C.c_void_p, teacher_ids, "teacher_ids"), opt(labels, "labels"), id_bytes,
+            per(C.c_void_p, teacher_logits, "teacher_logits"), dtype if teacher_dtype is None else teacher_dtype, top, temperature,
+            soft, hard, scale, per(C.c_void_p, loss, "loss"), opt(dlogits, "dlogits"),
+            vocab if dlogits_pitch is None else dlogits_pitch, ws, ws_bytes, stream))
 
     def profile(self, level: int) -> None:
         _check(lib().caramel_profile(self._h, int(level)))

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libcaramel.so")
 SOURCES = ["plan.cpp", "schedule.cpp", "tiles.cpp", "slices.cpp", "kernels.hip", "probe.hip", "embedding.hip",
            "checkpoint.hip", "weight_gradient.hip", "norm.hip", "recurrence.hip",
-           "api.hip"]
+           "distillation.hip", "api.hip"]
 
 
 def hipcc() -> str:

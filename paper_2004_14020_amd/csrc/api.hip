@@ -1597,6 +1597,88 @@ int recurrence_gradient(caramel_plan* p, uint64_t channels, const uint64_t* toke
   return CARAMEL_OK;
 }
 
+int check_distillation(uint64_t vocab, uint32_t top) {
+  if (int rc = check_columns("vocab", vocab)) return rc;
+  if (top == 0 || top > kDistillationTop) return fail(CARAMEL_EINVAL, "top must be 1 to %u, is %u", kDistillationTop, top);
+  return CARAMEL_OK;
+}
+
+int distillation_workspace(const caramel_plan* p, uint64_t vocab, uint32_t top, const uint64_t* tokens, uint64_t* bytes) {
+  if (!p || !bytes) return fail(CARAMEL_EINVAL, "NULL argument");
+  uint32_t n[CARAMEL_MAX_WORLD], most = 0;
+  if (int rc = check_distillation(vocab, top)) return rc;
+  if (int rc = take_tokens(p, tokens, n, &most)) return rc;
+  *bytes = distillation_workspace_bytes(p->host.cfg.world, uint32_t(vocab), top, most);
+  return CARAMEL_OK;
+}
+
+int distillation(caramel_plan* p, uint64_t vocab, const uint64_t* tokens, const void* const* logits, uint32_t dtype, uint64_t pitch,
+                 const void* const* teacher_ids, const void* const* labels, uint32_t id_bytes, const void* const* teacher_logits,
+                 uint32_t teacher_dtype, uint32_t top, float temperature, float soft, float hard, float scale, float* const* loss,
+                 void* const* dlogits, uint64_t dlogits_pitch, void* ws, uint64_t ws_bytes, hipStream_t stream) {
+  if (!p) return fail(CARAMEL_EINVAL, "plan is NULL");
+  DistillationArgs a{};
+  AllBuffers<kDistBuffers> v{};
+  if (int rc = check_distillation(vocab, top)) return rc;
+  if (id_bytes != 4 && id_bytes != 8) return fail(CARAMEL_EINVAL, "id_bytes must be 4 or 8, is %u", id_bytes);
+  if (int rc = check_dtype("dtype", dtype)) return rc;
+  if (int rc = check_dtype("teacher_dtype", teacher_dtype)) return rc;
+  if (!(temperature >= 1.0f / 1024 && temperature <= 1024.0f))
+    return fail(CARAMEL_EINVAL, "temperature must be 1/1024 to 1024, is %g", double(temperature));
+  if (!(soft >= 0.0f) || !(hard >= 0.0f) || !std::isfinite(soft) || !std::isfinite(hard) || (soft == 0.0f && hard == 0.0f))
+    return fail(CARAMEL_EINVAL, "soft and hard must be numbers from 0 on, not both 0, are %g and %g", double(soft), double(hard));
+  if (!std::isfinite(scale)) return fail(CARAMEL_EINVAL, "scale must be a number, is %g", double(scale));
+  if (hard > 0.0f && !labels) return fail(CARAMEL_EINVAL, "hard is not 0, and labels is NULL");
+  const uint64_t es = size_of(dtype), ts = size_of(teacher_dtype);
+  if (int rc = take_tokens(p, tokens, v.tokens, &a.max_tokens)) return rc;
+  if (int rc = check_rows("pitch", pitch, vocab, a.max_tokens)) return rc;
+  if (dlogits)
+    if (int rc = check_rows("dlogits_pitch", dlogits_pitch, vocab, a.max_tokens)) return rc;
+  if (int rc = take_pointers(p, "logits", logits, v.tokens, es, v.at[kDistLogits])) return rc;
+  if (int rc = take_pointers(p, "teacher_ids", teacher_ids, v.tokens, id_bytes, v.at[kDistIds])) return rc;
+  if (int rc = take_pointers(p, "teacher_logits", teacher_logits, v.tokens, ts, v.at[kDistTeacher])) return rc;
+  if (int rc = take_optional(p, "labels", labels, v.tokens, id_bytes, v.at[kDistLabels])) return rc;
+  if (int rc = take_pointers(p, "loss", reinterpret_cast<const void* const*>(loss), v.tokens, 4, v.at[kDistLoss])) return rc;
+  if (int rc = take_optional(p, "dlogits", dlogits, v.tokens, es, v.at[kDistGradient])) return rc;
+  a.all = p->host.cfg.world;
+  const uint64_t need = distillation_workspace_bytes(a.all, uint32_t(vocab), top, a.max_tokens);
+  if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
+  Memory m;
+  m.add(reinterpret_cast<uint64_t>(ws), need, true);
+  for (uint32_t w = 0; w < a.all; ++w) {
+    const uint64_t n = v.tokens[w];
+    if (!n) continue;
+    const bool in_place = dlogits && v.at[kDistGradient][w] == v.at[kDistLogits][w] && dlogits_pitch == pitch;
+    if (!in_place) m.add_rows(v.at[kDistLogits][w], n, pitch, vocab, es, false);
+    m.add(v.at[kDistIds][w], n * top * id_bytes, false);
+    m.add(v.at[kDistTeacher][w], n * top * ts, false);
+    if (labels) m.add(v.at[kDistLabels][w], n * id_bytes, false);
+    m.add(v.at[kDistLoss][w], n * 4, true);
+    if (dlogits) m.add_rows(v.at[kDistGradient][w], n, dlogits_pitch, vocab, es, true);
+  }
+  if (int rc = check_memory(m)) return rc;
+  if (int rc = need_device(p)) return rc;
+  a.vocab = uint32_t(vocab);
+  a.top = top;
+  a.pitch = pitch;
+  a.gradient_pitch = dlogits_pitch;
+  a.temperature = temperature;
+  a.soft = soft;
+  a.hard = hard;
+  a.scale = scale;
+  a.bf16 = dtype == CARAMEL_BF16;
+  a.teacher_bf16 = teacher_dtype == CARAMEL_BF16;
+  a.ids64 = id_bytes == 8;
+  a.has_labels = hard > 0.0f;
+  a.gradient = dlogits != nullptr;
+  a.ws = static_cast<unsigned char*>(ws);
+  if (tracing())
+    std::fprintf(stderr, "caramel: distillation stream %p, %u workers, up to %u tokens, %u logits\n", (void*)stream, a.all,
+                 a.max_tokens, a.vocab);
+  HIP_TRY(launch_distillation(a, v, stream));
+  return CARAMEL_OK;
+}
+
 }  // namespace
 
 int caramel_embedding_lookup(caramel_plan* p, const void* const* table, uint64_t vocab, uint64_t width, float scale,
@@ -1698,6 +1780,21 @@ int caramel_recurrence_gradient(caramel_plan* p, uint64_t channels, const uint64
   return guarded([&] {
     return recurrence_gradient(p, channels, tokens, sequences, starts, id_bytes, gate, input, dtype, pitch, before, states, dstates,
                                states_pitch, dafter, dgate, dinput, dbefore, ws, ws_bytes, hipStream_t(stream));
+  });
+}
+
+int caramel_distillation_workspace(const caramel_plan* p, uint64_t vocab, uint32_t top, const uint64_t* tokens, uint64_t* bytes) {
+  return guarded([&] { return distillation_workspace(p, vocab, top, tokens, bytes); });
+}
+
+int caramel_distillation(caramel_plan* p, uint64_t vocab, const uint64_t* tokens, const void* const* logits, uint32_t dtype,
+                         uint64_t pitch, const void* const* teacher_ids, const void* const* labels, uint32_t id_bytes,
+                         const void* const* teacher_logits, uint32_t teacher_dtype, uint32_t top, float temperature, float soft,
+                         float hard, float scale, float* const* loss, void* const* dlogits, uint64_t dlogits_pitch, void* ws,
+                         uint64_t ws_bytes, void* stream) {
+  return guarded([&] {
+    return distillation(p, vocab, tokens, logits, dtype, pitch, teacher_ids, labels, id_bytes, teacher_logits, teacher_dtype, top,
+                        temperature, soft, hard, scale, loss, dlogits, dlogits_pitch, ws, ws_bytes, hipStream_t(stream));
   });
 }
 

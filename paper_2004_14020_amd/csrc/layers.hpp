@@ -1,6 +1,6 @@
 // Kernels that fill a plan's gradient tensors, and those of a training step before and between them: the
 // embedding lookup and its gradient, activation checkpoints in 8 bits, the weight and bias gradients that
-// read them, the residual norm and the gated recurrence with their gradients.  Launch wrappers; the arguments have been checked by the entry points.
+// read them, the residual norm and the gated recurrence with their gradients, distillation.  Launch wrappers; the arguments have been checked by the entry points.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -172,5 +172,26 @@ struct RecurrenceArgs {
 uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, uint32_t max_tokens);
 hipError_t launch_recurrence(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);
 hipError_t launch_recurrence_gradient(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);
+
+constexpr uint32_t kDistillationTop = 256;  // most entries of the teacher per token
+
+enum { kDistLogits, kDistIds, kDistTeacher, kDistLabels, kDistLoss, kDistGradient, kDistBuffers };
+struct DistillationArgs {
+  Buffers<kDistBuffers> w;
+  uint32_t world, all;  // workers of the launch, of the call
+  uint32_t max_tokens;  // of all workers
+  uint32_t vocab, top;
+  uint64_t pitch, gradient_pitch;  // elements
+  float temperature, soft, hard, scale;
+  bool bf16, teacher_bf16, ids64, has_labels, gradient;
+  unsigned char* ws;
+  // made by the launch
+  uint32_t parts, part, stride;  // of a row; pieces of a part; floats of a row in the workspace
+  float warm_rate, cold_rate;  // log2(e) / temperature, log2(e)
+  double inverse;              // 1 / temperature
+  bool twice;
+};
+uint64_t distillation_workspace_bytes(uint32_t world, uint32_t vocab, uint32_t top, uint32_t max_tokens);
+hipError_t launch_distillation(const DistillationArgs& args, const AllBuffers<kDistBuffers>& v, hipStream_t s);
 
 }  // namespace caramel

@@ -38,12 +38,15 @@ __device__ __forceinline__ void load_gain(uint64_t gain, bool bf16, uint32_t col
   else load_gains<false, N>(gain, col, width, g);
 }
 
+constexpr uint32_t kGridGroups = 1u << 20;  // workgroups along x: a grid has less than 2^32 lanes in a direction
+
 // V pieces a lane, TEAM wavefronts to a row.
 template <bool BF16, int V, int TEAM>
 __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
   constexpr int N = kPiece<BF16>, ES = BF16 ? 2 : 4, kWaves = TEAM <= 4 ? 4 : 16;
   __shared__ double lds[TEAM];
-  const uint32_t w = blockIdx.y, row = blockIdx.x * (kWaves / TEAM) + uniform(threadIdx.x / 64) / TEAM;
+  const uint32_t w = blockIdx.y, group = blockIdx.x + blockIdx.z * kGridGroups;
+  const uint32_t row = group * (kWaves / TEAM) + uniform(threadIdx.x / 64) / TEAM;
   if (row >= a.w.tokens[w]) return;
   const uint32_t lane = threadIdx.x % (64 * TEAM);
   const uint64_t at = uint64_t(row) * a.pitch * ES;
@@ -212,7 +215,8 @@ hipError_t launch_norm(const NormArgs& args, const AllBuffers<kNormBuffers>& v, 
     by_shape(a.width, a.bf16 ? 8 : 4, [&](auto shape) {
       constexpr int V = decltype(shape)::kV, TEAM = decltype(shape)::kTeam;
       constexpr uint32_t kRows = (TEAM <= 4 ? 4 : 16) / TEAM;
-      const dim3 grid((a.max_tokens + kRows - 1) / kRows, a.world), block(TEAM <= 4 ? 256 : 1024);
+      const uint32_t groups = (a.max_tokens + kRows - 1) / kRows;
+      const dim3 grid(std::min(groups, kGridGroups), a.world, (groups + kGridGroups - 1) / kGridGroups), block(TEAM <= 4 ? 256 : 1024);
       if (a.bf16) hipLaunchKernelGGL((k_norm<true, V, TEAM>), grid, block, 0, s, a);
       else hipLaunchKernelGGL((k_norm<false, V, TEAM>), grid, block, 0, s, a);
     });

@@ -1,0 +1,318 @@
+"""Distillation from a teacher's best logits, against the formulas in 64 bits.
+
+Tolerances.  An exponential 2^(d log2(e) / T) carries the roundings of the distance d, of the rate and of their product, 3 * 2^-24 |d| / T in
+all, and its own 2^-23; where q's exponential is Q's to the power of T, T times that and two roundings.  A sum of positive numbers
+is off by the mean of what its terms are off by, and by 2^-24 for each of the additions that a term passes through, which are fewer than
+a lane has terms (vocab / 256) and 40 more.  Quotients, products and differences of these are one rounding each."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2004_14020_amd as cm
+
+from layer_util import DEV, HALF_STEP, TORCH, addresses, f64, rows, stream, untouched, workspace
+from test_gpu_layers import DTYPES, NAMES, close, counts, dtype_id
+
+pytestmark = pytest.mark.gpu
+
+STEP, TINY = 2.0 ** -24, 2.0 ** -115
+
+
+def softmax64(z, T):
+    """softmax(z / T), the logarithms, and how far fp32 may be off: the exponentials (rows x vocab), their sums (rows), relatively."""
+    with np.errstate(all="ignore"):
+        d = z - z.max(1, keepdims=True)
+        e = np.exp(d / T)
+        S = e.sum(1, keepdims=True)
+        far = np.where(e > 0, -d / T, 0.0)
+    return e / S, d / T - np.log(S), far, S
+
+
+def formulas(z, ids, t, labels, T, soft, hard, scale, vocab, squares):
+    """loss, dlogits, and how far fp32 may be off each."""
+    n = len(z)
+    adds = (vocab / 256 + 40) * STEP
+    Q, lnQ, far, _ = softmax64(z, T)
+    rho = 3 * STEP * far + 2 * STEP
+    off_S = (Q * rho).sum(1, keepdims=True) + adds
+    q, lnq, far1, _ = softmax64(z, 1.0)
+    rho1 = 3 * STEP * far1 + 2 * STEP * (T if squares else 1) + 2 * STEP
+    off_S1 = (q * rho1).sum(1, keepdims=True) + adds
+    there = (ids >= 0) & (ids < vocab)
+    tt = np.where(there, t, -np.inf)
+    most = tt.max(1, keepdims=True)
+    taught = (most > -np.inf) & (soft > 0)
+    with np.errstate(all="ignore"):
+        p = np.where(taught & (tt > -np.inf), np.exp((tt - most) / T), 0.0)
+        total = p.sum(1, keepdims=True)
+        P = np.where(taught, p / total, 0.0)
+        off_p = np.where(p > 0, 3 * STEP * (most - tt) / T + 2 * STEP, 0.0)
+        off_P = off_p + (P * off_p).sum(1, keepdims=True) + 12 * STEP
+    r = np.arange(n)[:, None]
+    at = np.where(there, ids, 0)
+    with np.errstate(all="ignore"):
+        terms = np.where(P > 0, P * ((tt - most) / T - np.log(total) - lnQ[r, at]), 0.0)
+        mag = np.where(P > 0, P * off_P * (np.abs(tt - most) + np.abs(z[r, at])) / T, 0.0)
+    loss = soft * terms.sum(1)
+    off_loss = np.where(taught[:, 0], soft * (mag.sum(1) + off_S[:, 0] + 12 * STEP), 0.0)
+    sum_P, off_sum = np.zeros((n, vocab)), np.zeros((n, vocab))
+    np.add.at(sum_P, (np.broadcast_to(r, ids.shape), at), np.where(there, P, 0.0))
+    np.add.at(off_sum, (np.broadcast_to(r, ids.shape), at), np.where(there, P * (off_P + 258 * STEP), 0.0))
+    ts = taught * soft / T
+    g = ts * (Q - sum_P)
+    off = ts * (Q * (rho + off_S + 6 * STEP) + off_sum + 4 * STEP * (Q + sum_P))
+    if hard > 0:
+        known = ((labels >= 0) & (labels < vocab))[:, None] * hard
+        lab = np.where((labels >= 0) & (labels < vocab), labels, 0)
+        with np.errstate(all="ignore"):
+            loss = loss + np.where(known[:, 0] > 0, -hard * lnq[r[:, 0], lab], 0.0)
+        off_loss = off_loss + known[:, 0] * off_S1[:, 0]
+        one = np.zeros((n, vocab))
+        one[r[:, 0], lab] = 1.0
+        g = g + known * (q - one)
+        off = off + known * (q * (rho1 + off_S1 + 6 * STEP) + 6 * STEP * one + 4 * STEP * q) + 2 * STEP * ts * (Q + sum_P)
+    off_loss = off_loss + STEP * np.abs(loss)
+    return loss, scale * g, off_loss, abs(scale) * (off + TINY) + 2 * STEP * np.abs(scale * g)
+
+
+KINDS = [(1.0, 1.0, 0.0), (1.0, 0.7, 0.5), (2.0, 1.0, 0.5), (4.0, 0.5, 1.0), (3.0, 1.0, 1.5), (0.7, 2.0, 0.25), (5.0, 0.0, 1.0),
+         (2.5, 1.0, 0.0)]
+
+CASES = [  # world, tokens, vocab, top, gap
+    (1, 1, 1, 1, 0), (2, 3, 2, 3, 1), (1, 5, 7, 2, 0), (3, 9, 100, 64, 3), (64, 4, 33, 5, 0), (20, 7, 1001, 65, 0), (2, 300, 777, 17, 1),
+    (1, 6, 8191, 256, 0), (2, 5, 8192, 32, 0), (1, 3, 30522, 8, 0), (1, 1, 130001, 64, 1), (2, 40, 16387, 12, 5), (1, 250, 8195, 33, 0),
+    (1, 230, 30522, 32, 0), (2, 120, 32769, 16, 1), (1, 200, 65536, 7, 0), (1, 200, 70003, 100, 1)]
+
+
+def case_of(rng, world, n, vocab, top, gap, dtype, teacher_dtype, id_bytes):
+    ns = counts(world, n)
+    ids, teacher, labels, z = [], [], [], []
+    for m in ns:
+        v = rng.standard_normal((m, vocab)) * 3
+        i = rng.integers(0, vocab, (m, top))
+        if m:
+            i[rng.random((m, top)) < 0.1] = -1
+            i[rng.random((m, top)) < 0.02] = vocab
+            i[m // 2] = i[m // 2, 0]                            # one id for all entries
+            i[m // 3] = -1                                      # no teacher
+        t = rng.standard_normal((m, top)) * 3
+        t[rng.random((m, top)) < 0.05] = -np.inf
+        lab = rng.integers(0, vocab, m)
+        lab[rng.random(m) < 0.3] = -1
+        if m:
+            lab[::4] = i[::4, 0]                                # the teacher's first one, or none
+            lab[m // 3] = -7 if m > 3 else lab[m // 3]
+        ids.append(i)
+        teacher.append(torch.tensor(t, dtype=torch.float32).to(TORCH[teacher_dtype]))
+        labels.append(lab)
+        z.append(torch.tensor(v, dtype=torch.float32).to(TORCH[dtype]))
+    it = torch.int64 if id_bytes == 8 else torch.int32
+    on = lambda v: [torch.tensor(x, dtype=it, device=DEV) for x in v]                    # noqa: E731
+    return ns, ids, teacher, labels, z, on(ids), [t.to(DEV) for t in teacher], on(labels)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+@pytest.mark.parametrize("T,soft,hard", KINDS)
+@pytest.mark.parametrize("world,n,vocab,top,gap", CASES)
+def test_distillation(world, n, vocab, top, gap, T, soft, hard, dtype):
+    if n * vocab > 4e6 and (T, soft, hard) not in KINDS[2:5]:
+        T, soft, hard = KINDS[4]                                # (the large cases: other kinds of exponentials by the smaller ones)
+    print(f"case: distillation world={world} n={n} vocab={vocab} top={top} T={T} {soft} {hard} {NAMES[dtype]}", flush=True)
+    rng = np.random.default_rng(n * vocab + top)
+    id_bytes, teacher_dtype = 8 if vocab % 2 else 4, cm.F32 if n % 2 else cm.BF16
+    ns, ids, teacher, labels, z, di, dt, dl = case_of(rng, world, n, vocab, top, gap, dtype, teacher_dtype, id_bytes)
+    plan, scale = cm.Plan(world, [1]), -3.0
+    logits = [rows(m, vocab, vocab + gap, dtype, v) for m, v in zip(ns, z)]
+    need = plan.distillation_workspace(vocab, top, ns)
+    results = []
+    for how in ("apart", "again", "in place", "loss alone"):
+        ws = workspace(need)
+        ws[:need] = 0x5A if how == "again" else 0xFF
+        loss = [torch.full((m + 3,), 9.0, device=DEV) for m in ns]
+        if how == "in place":
+            out = [(mem.clone(),) for mem, _ in logits]
+            out = [(mem, mem[:m * (vocab + gap)].view(m, vocab + gap)[:, :vocab]) for (mem,), m in zip(out, ns)]
+            src, pitch = out, vocab + gap
+        else:
+            src, pitch = logits, vocab + 2 * gap
+            out = [rows(m, vocab, pitch, dtype, fill=7.0) for m in ns]
+        plan.distillation(vocab, ns, addresses([v[0] for v in src]), addresses(di), addresses(dt), top, addresses(loss), ws.data_ptr(),
+                          need, labels=addresses(dl) if hard else None, dlogits=None if how == "loss alone" else addresses([o[0] for o in out]),
+                          temperature=T, soft=soft, hard=hard, scale=scale, id_bytes=id_bytes, dtype=dtype, teacher_dtype=teacher_dtype,
+                          pitch=vocab + gap, dlogits_pitch=pitch, stream=stream())
+        torch.cuda.synchronize()
+        assert untouched(ws, need) and all(bool((v[m:] == 9.0).all()) for v, m in zip(loss, ns))
+        if how == "loss alone":
+            assert all(bool((mem == 7.0).all()) for mem, _ in out)
+        results.append((loss, [o[1].clone() for o in out]))
+        if how == "apart":
+            for mem, view in out:
+                view.fill_(7.0)
+                assert bool((mem == 7.0).all()), "the gaps between the rows and what lies behind the last one stay"
+    for (loss, out), what in zip(results[1:], ("not reproducible", "in place", "loss alone")):
+        assert all(torch.equal(a, b) for a, b in zip(loss, results[0][0])), what
+        if what != "loss alone":
+            assert all(torch.equal(a, b) for a, b in zip(out, results[0][1])), what
+    for w, m in enumerate(ns):
+        if not m:
+            continue
+        want, g, off_loss, off = formulas(f64(z[w]), ids[w], f64(teacher[w]), labels[w], T, soft, hard, scale, vocab, T in (2.0, 4.0))
+        close(f64(results[0][0][w][:m]), want, off_loss, f"worker {w}: loss")
+        close(f64(results[0][1][w]), g, off + (HALF_STEP[cm.BF16] * (np.abs(g) + off) if dtype == cm.BF16 else 0), f"worker {w}: dlogits")
+    plan.close()
+
+
+def call(plan, z, ids, t, labels, T, soft, hard, dtype=cm.F32):
+    n, vocab = z.shape
+    need = plan.distillation_workspace(vocab, ids.shape[1], [n])
+    ws, loss, out = workspace(need), torch.empty(n, device=DEV), torch.empty_like(z, device=DEV)
+    d = [v.to(DEV) for v in (z, ids, t, labels)]
+    plan.distillation(vocab, [n], [d[0].data_ptr()], [d[1].data_ptr()], [d[2].data_ptr()], ids.shape[1], [loss.data_ptr()], ws.data_ptr(),
+                      need, labels=[d[3].data_ptr()], dlogits=[out.data_ptr()], temperature=T, soft=soft, hard=hard, dtype=dtype,
+                      teacher_dtype=cm.F32, stream=stream())
+    torch.cuda.synchronize()
+    return loss.cpu(), out.cpu()
+
+
+@pytest.mark.parametrize("vocab,n", [(50, 12), (9000, 12), (9000, 300), (70000, 250)])
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+def test_extreme_logits(dtype, T, vocab, n):
+    """Masked logits, the lowest and the largest numbers, infinities and NaN; tokens that learn nothing, whatever their logits."""
+    rng = np.random.default_rng(vocab)
+    inf, low, big = float("inf"), torch.finfo(TORCH[dtype]).min, torch.finfo(TORCH[dtype]).max
+    z = torch.tensor(rng.standard_normal((n, vocab)), dtype=torch.float32).to(TORCH[dtype])
+    ids, labels = torch.tensor(rng.integers(0, vocab // 2, (n, 3))), torch.tensor(rng.integers(0, vocab // 2, n))
+    t = torch.tensor(rng.standard_normal((n, 3)), dtype=torch.float32)
+    z[0, vocab // 2:] = -inf                                    # a masked half
+    z[1, vocab // 2:] = low
+    z[2] = low                                                  # all equal, as low as can be
+    z[3] = big
+    z[4, 5] = float("nan")
+    z[5, 5] = inf
+    z[6] = -inf
+    z[7], ids[7], labels[7] = float("nan"), -1, -100            # padding
+    z[8, ids[8, 0]] = -inf                                      # the teacher wants what the student cannot say
+    z[9, labels[9]], t[9] = -inf, -inf                          # so does the label; no teacher
+    t[10, 1] = float("nan")
+    t[11, 1] = inf
+    loss, g = call(cm.Plan(1, [1]), z, ids, t, labels, T, 1.0, 0.5, dtype)
+    z64 = z.double().numpy()
+    z64[2], z64[3] = 0.0, 0.0                                   # softmax of equal numbers
+    clean = [0, 1, 2, 3] + list(range(12, n))[:200]
+    want, dg, off_loss, off = formulas(z64[clean], ids.numpy()[clean], t.double().numpy()[clean], labels.numpy()[clean], T, 1.0, 0.5, 1.0,
+                                       vocab, T == 2.0)
+    # of rows 2 and 3, the loss is made of numbers as large as the logits, in 64 bits: off by 2^-50 of them
+    ok = [i for i, r in enumerate(clean) if r not in (2, 3)]
+    close(f64(loss[clean])[ok], want[ok], off_loss[ok])
+    close(f64(g[clean]), dg, off + (HALF_STEP[cm.BF16] * (np.abs(dg) + off) if dtype == cm.BF16 else 0))
+    for r in (4, 5, 6):
+        assert bool(loss[r].isnan()) and bool(g[r].isnan().all()), r
+    assert float(loss[7]) == 0.0 and bool((g[7] == 0.0).all())
+    assert float(loss[8]) == inf and bool(g[8].isfinite().all())
+    assert float(loss[9]) == inf and bool(g[9].isfinite().all())
+    for r in (10, 11):
+        assert bool(loss[r].isnan()) and bool(g[r, ids[r, 1]].isnan()) and int(g[r].isnan().sum()) <= 3
+
+
+def test_distillation_agrees_with_differences():
+    """Of the loss, in 64 bits, along directions of the logits."""
+    rng = np.random.default_rng(2)
+    n, vocab, h = 6, 41, 1e-6
+    plan = cm.Plan(1, [1])
+    for T, soft, hard in KINDS:
+        z, t = (torch.tensor(rng.standard_normal(s), dtype=torch.float32) for s in ((n, vocab), (n, 5)))
+        ids, labels = torch.tensor(rng.integers(-1, vocab, (n, 5))), torch.tensor(rng.integers(-1, vocab, n))
+        _, g = call(plan, z, ids, t, labels, T, soft, hard)
+        args = (ids.numpy(), f64(t), labels.numpy(), T, soft, hard, 1.0, vocab, T in (2.0, 4.0))
+        _, _, _, off = formulas(f64(z), *args)
+        for _ in range(3):
+            p = rng.standard_normal((n, vocab))
+            want = (formulas(f64(z) + h * p, *args)[0] - formulas(f64(z) - h * p, *args)[0]) / (2 * h)
+            # the differences: curvature of relative size h^2, and the roundings of the loss over h
+            assert (np.abs((f64(g) * p).sum(1) - want) <= (off * np.abs(p)).sum(1) + 1e-7 * (soft + hard)).all()
+    plan.close()
+
+
+def test_gradient_of_a_label_is_that_of_a_cross_entropy():
+    """soft 0: the labels alone, as torch has them on the CPU in 64 bits."""
+    n, vocab = 70, 300
+    z = torch.randn(n, vocab)
+    labels = torch.randint(0, vocab, (n,))
+    labels[5] = -100
+    loss, g = call(cm.Plan(1, [1]), z, torch.full((n, 1), -1), torch.zeros(n, 1), labels, 2.0, 0.0, 1.0)
+    x = z.double().requires_grad_()
+    want = torch.nn.functional.cross_entropy(x, labels, reduction="none", ignore_index=-100)
+    want.sum().backward()
+    assert torch.allclose(loss.double(), want.detach(), rtol=1e-5, atol=1e-6) and torch.allclose(g.double(), x.grad, rtol=1e-4, atol=1e-7)
+
+
+def test_no_tokens_and_logits_more_than_four_gib_apart():
+    plan = cm.Plan(2, [1])
+    plan.distillation(10, [0, 0], [None] * 2, [None] * 2, [None] * 2, 4, [None] * 2, None, 0, dlogits=[None] * 2, stream=stream())
+    n, vocab, pitch = 300, 40, 1 << 23
+    free, _ = torch.cuda.mem_get_info()
+    if free < 2 * n * pitch + (4 << 30):
+        pytest.skip("not enough memory")
+    z = torch.empty(n * pitch, dtype=torch.bfloat16, device=DEV)
+    view = z.view(n, pitch)[:, :vocab]
+    values = torch.randn(n, vocab).to(torch.bfloat16)
+    view.copy_(values)
+    rng = np.random.default_rng(0)
+    ids, t, loss = torch.tensor(rng.integers(0, vocab, (n, 4)), device=DEV), torch.randn(n, 4, device=DEV), torch.empty(n, device=DEV)
+    plan.distillation(vocab, [0, n], [None, z.data_ptr()], [None, ids.data_ptr()], [None, t.data_ptr()], 4, [None, loss.data_ptr()], None, 0,
+                      dlogits=[None, z.data_ptr()], temperature=2.5, dtype=cm.BF16, teacher_dtype=cm.F32, pitch=pitch,
+                      dlogits_pitch=pitch, stream=stream())
+    torch.cuda.synchronize()
+    want, g, off_loss, off = formulas(f64(values), ids.cpu().numpy(), f64(t), None, 2.5, 1.0, 0.0, 1.0, vocab, False)
+    close(f64(loss), want, off_loss)
+    close(f64(view), g, off + HALF_STEP[cm.BF16] * (np.abs(g) + off))
+    plan.close()
+
+
+@pytest.mark.parametrize("n,vocab", [(5, 20000), (300, 500)])
+def test_distillation_captured_into_a_graph(n, vocab):
+    """Replayed three times, with new inputs and eager calls of the same buffers in between."""
+    W, top = 2, 9
+    plan = cm.Plan(W, [1], dtype=cm.BF16)
+    z, out = ([torch.empty(n, vocab, dtype=torch.bfloat16, device=DEV) for _ in range(W)] for _ in range(2))
+    t, ids = [torch.empty(n, top, dtype=torch.bfloat16, device=DEV) for _ in range(W)], [torch.empty(n, top, dtype=torch.int64, device=DEV)
+                                                                                        for _ in range(W)]
+    labels, loss = [torch.empty(n, dtype=torch.int64, device=DEV) for _ in range(W)], [torch.empty(n, device=DEV) for _ in range(W)]
+    need = plan.distillation_workspace(vocab, top, [n] * W)
+    ws = workspace(need)
+
+    def step():
+        plan.distillation(vocab, [n] * W, addresses(z), addresses(ids), addresses(t), top, addresses(loss), ws.data_ptr(), need,
+                          labels=addresses(labels), dlogits=addresses(out), temperature=2.0, hard=1.0, stream=stream())
+
+    def outputs():
+        torch.cuda.synchronize()
+        return [v.clone() for v in out + loss]
+
+    def fill(seed):
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        for v in z + t:
+            v.copy_(torch.randn(v.shape, device=DEV, generator=g))
+        for v in ids + labels:
+            v.copy_(torch.randint(-1, vocab, v.shape, device=DEV, generator=g))
+        for v in out + loss + [ws]:
+            v.fill_(1)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        fill(0)
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (1, 2, 3):
+        fill(seed)
+        step()
+        want = outputs()
+        fill(seed)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(outputs(), want))
+    plan.close()

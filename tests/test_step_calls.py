@@ -132,3 +132,48 @@ def test_recurrence_workspaces_serve_fewer_tokens():
         sizes = [plan.recurrence_workspace(channels, [n] * plan.cfg.world) for n in tokens]
         assert sizes == sorted(sizes)
         plan.close()
+
+
+DIST = dict(vocab=16, tokens=[3, 3], logits=[A, 2 * A], teacher_ids=[3 * A, 4 * A], teacher_logits=[5 * A, 6 * A], top=2,
+            loss=[7 * A, 8 * A], ws=None, ws_bytes=0, labels=[9 * A, 10 * A], dlogits=[11 * A, 12 * A], hard=0.5)
+
+
+@pytest.mark.parametrize("change", [
+    dict(vocab=0), dict(vocab=(1 << 20) + 1, pitch=1 << 22, dlogits_pitch=1 << 22), dict(top=0), dict(top=257), dict(id_bytes=1),
+    dict(dtype=2), dict(teacher_dtype=2), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=2000.0),
+    dict(temperature=math.nan), dict(temperature=math.inf), dict(soft=-1.0), dict(soft=math.nan), dict(hard=-0.5), dict(hard=math.inf),
+    dict(soft=0.0, hard=0.0), dict(scale=math.nan), dict(scale=math.inf), dict(labels=None), dict(tokens=[T, 1]), dict(pitch=15),
+    dict(pitch=(1 << 23) + 1), dict(dlogits_pitch=15), dict(tokens=[1 << 25, 1], pitch=1 << 23), dict(logits=[None, A]),
+    dict(logits=[A + 2, 2 * A]), dict(teacher_ids=[3 * A, None]), dict(teacher_ids=[3 * A + 4, 4 * A]), dict(teacher_logits=[None, A]),
+    dict(teacher_logits=[5 * A + 2, 6 * A]), dict(labels=[9 * A, None]), dict(labels=[9 * A + 4, 10 * A]), dict(loss=[None, 8 * A]),
+    dict(loss=[7 * A + 2, 8 * A]), dict(dlogits=[11 * A, None]), dict(dlogits=[11 * A + 1, 12 * A]), dict(vocab=10000, pitch=10000),
+    dict(vocab=10000, ws=20 * A + 8, ws_bytes=1 << 20), dict(vocab=10000, ws=20 * A, ws_bytes=64),
+    # what is written overlaps: the other worker's, inputs; the logits with another pitch or place than theirs
+    dict(dlogits=[11 * A, 11 * A]), dict(dlogits=[3 * A, 12 * A]), dict(loss=[7 * A, 7 * A]), dict(loss=[A, 8 * A]),
+    dict(dlogits=[2 * A, A]), dict(dlogits=[A, 2 * A], dlogits_pitch=17), dict(dlogits=[A + 64, 2 * A]),
+], ids=str)
+def test_distillation_refusals(plan, change):
+    refused(E, plan.distillation, **{**DIST, **change})
+
+
+def test_distillation_null_arguments(plan):
+    L, two, n, b = cm.lib(), (C.c_void_p * 2)(A, 2 * A), (C.c_uint64 * 2)(0, 0), C.c_uint64()
+    args = [plan._h, 16, n, two, 0, 16, two, None, 8, two, 0, 2, 1.0, 1.0, 0.0, 1.0, two, None, 16, None, 0, None]
+    for i in (0, 2, 3, 6, 9, 16):
+        assert L.caramel_distillation(*[None if k == i else v for k, v in enumerate(args)]) == E, i
+    sizes = [plan._h, 16, 2, n, C.byref(b)]
+    for i in (0, 3, 4):
+        assert L.caramel_distillation_workspace(*[None if k == i else v for k, v in enumerate(sizes)]) == E, i
+    for bad in ((0, 1, [1, 1]), ((1 << 20) + 1, 1, [1, 1]), (16, 0, [1, 1]), (16, 257, [1, 1]), (16, 1, [1, T])):
+        refused(E, plan.distillation_workspace, *bad)
+
+
+def test_distillation_workspaces_serve_fewer_tokens():
+    rng = random.Random(4)
+    for _ in range(200):
+        plan = cm.Plan(rng.choice([1, 2, 3, 8, 16, 17, 64]), [1])
+        vocab, top = int(2 ** rng.uniform(0, 20)), rng.randint(1, 256)
+        tokens = sorted(int(2 ** rng.uniform(0, 25)) for _ in range(30))
+        sizes = [plan.distillation_workspace(vocab, top, [n] * plan.cfg.world) for n in tokens]
+        assert sizes == sorted(sizes)
+        plan.close()
