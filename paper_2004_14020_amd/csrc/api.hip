@@ -1608,7 +1608,7 @@ int distillation_workspace(const caramel_plan* p, uint64_t vocab, uint32_t top, 
   uint32_t n[CARAMEL_MAX_WORLD], most = 0;
   if (int rc = check_distillation(vocab, top)) return rc;
   if (int rc = take_tokens(p, tokens, n, &most)) return rc;
-  *bytes = distillation_workspace_bytes(p->host.cfg.world, uint32_t(vocab), top, most);
+  *bytes = distillation_workspace_bytes(p->host.cfg.world, uint32_t(vocab), most);
   return CARAMEL_OK;
 }
 
@@ -1641,7 +1641,7 @@ int distillation(caramel_plan* p, uint64_t vocab, const uint64_t* tokens, const 
   if (int rc = take_pointers(p, "loss", reinterpret_cast<const void* const*>(loss), v.tokens, 4, v.at[kDistLoss])) return rc;
   if (int rc = take_optional(p, "dlogits", dlogits, v.tokens, es, v.at[kDistGradient])) return rc;
   a.all = p->host.cfg.world;
-  const uint64_t need = distillation_workspace_bytes(a.all, uint32_t(vocab), top, a.max_tokens);
+  const uint64_t need = distillation_workspace_bytes(a.all, uint32_t(vocab), a.max_tokens);
   if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
   Memory m;
   m.add(reinterpret_cast<uint64_t>(ws), need, true);

@@ -20,16 +20,13 @@
 namespace caramel {
 namespace {
 
-enum { kOne, kPower, kTwo };             // exponentials: one for Q and q; those of q are powers of Q's; two
+enum { kOne, kSquare, kFourth, kTwo };   // exponentials: one for Q and q; those of q are Q's squared, or squared twice; two
 enum { kWhole, kMeasure, kWrite };       // a row at once; a part's largest logit and sums; the gradient of a part
 
 constexpr int kTop = int(kDistillationTop), kEntries = kTop + 1;  // of the teacher; and the label
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr uint32_t kGridRows = 1u << 20;  // along x: a grid has less than 2^32 lanes in a direction
-
-struct Sums {
-  float largest, warm, cold;  // warm: of 2^(d log2(e) / T); cold: of 2^(d log2(e))
-};
+constexpr float kLowest = -3.402823466e38f;
 
 __device__ __forceinline__ uint32_t read_id(uint64_t at, uint64_t i, bool wide, uint32_t vocab) {
   const uint64_t id = wide ? reinterpret_cast<const CARAMEL_GLOBAL uint64_t*>(at)[i]
@@ -43,286 +40,404 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// The exponential of q from that of Q (T = 2 or 4)
-__device__ __forceinline__ float power(float e, bool twice) {
-  e *= e;
-  return twice ? e * e : e;
+// Over one number of each of COUNT (16 at most) wavefronts, `step` apart in LDS: every group of 16 lanes for itself, so that it takes one
+// register and not COUNT.
+template <int COUNT>
+__device__ __forceinline__ float across_max(const float* lds, int step) {
+  float v = lds[min(int(threadIdx.x % 16), COUNT - 1) * step];
+#pragma unroll
+  for (int d = 8; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+template <int COUNT>
+__device__ __forceinline__ float across_sum(const float* lds, int step) {
+  const int k = threadIdx.x % 16;
+  float v = k < COUNT ? lds[k * step] : 0.0f;
+#pragma unroll
+  for (int d = 8; d; d /= 2) v += __shfl_xor(v, d);
+  return v;
 }
 
-// LANES lanes hold HELD logits each.
-template <bool BF16, int KIND, int PHASE, int LANES, int HELD>
-__global__ void __launch_bounds__(LANES) k_distillation(DistillationArgs a) {
-  constexpr int N = kPiece<BF16>, ES = BF16 ? 2 : 4, V = HELD / N, kWaves = LANES / 64;
-  constexpr bool kKeep = KIND != kTwo;  // exponentials stay in registers; else distances
+__device__ __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// The natural logarithm of a sum, whose exponent is taken apart: the rest is in [1/2, 1), and its logarithm off by 2^-25 at most.
+__device__ __forceinline__ double ln(float v) {
+  return double(__builtin_amdgcn_frexp_expf(v)) * 0.69314718055994531 + double(logf(__builtin_amdgcn_frexp_mantf(v)));
+}
+
+// What a row's teacher and label ask for: of entry k (the label: entry `top`) its id, the student's logit there, and what is taken
+// from the gradient there; taught: the loss without the logarithms of sums over the vocabulary; terms: bit 0 the teacher's, bit 1
+// the label's.
+struct Lesson {
+  uint32_t id[kEntries];
+  float logit[kEntries], weight[kEntries];
+  uint32_t terms;
+  double taught;
+};
+
+// By one wavefront.
+template <bool BF16>
+__device__ __forceinline__ void learn(const DistillationArgs& a, uint32_t w, uint32_t row, uint64_t z, Lesson& out) {
+  constexpr int ES = BF16 ? 2 : 4, kEach = kTop / 64;
+  const uint32_t lane = threadIdx.x % 64;
+  float t[kEach], v[kEach];
+  uint32_t id[kEach];
+  float most = -__builtin_inff();
+  bool bad = false, any = false;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const uint32_t k = i * 64 + lane;
+    id[i] = kNone;
+    t[i] = -__builtin_inff();
+    v[i] = 0.0f;
+    if (uint32_t(i) * 64 >= a.top || k >= a.top) continue;
+    id[i] = read_id(a.w.at[kDistIds][w], uint64_t(row) * a.top + k, a.ids64, a.vocab);
+    const uint64_t at = a.w.at[kDistTeacher][w] + (uint64_t(row) * a.top + k) * (a.teacher_bf16 ? 2 : 4);
+    if (a.teacher_bf16) load_elems<true, 1>(at, &t[i]);
+    else load_elems<false, 1>(at, &t[i]);
+  }
+  uint32_t label = kNone;
+  if (a.has_labels) label = uniform(read_id(a.w.at[kDistLabels][w], row, a.ids64, a.vocab));
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (uint32_t(i) * 64 >= a.top) continue;
+    if (id[i] != kNone) load_elems<BF16, 1>(z + uint64_t(id[i]) * ES, &v[i]);
+    else t[i] = -__builtin_inff();
+    most = fmaxf(most, t[i]);
+    bad = bad || t[i] != t[i];
+    any = any || t[i] > -__builtin_inff();
+  }
+  float label_logit = 0.0f;
+  if (label != kNone) load_elems<BF16, 1>(z + uint64_t(label) * ES, &label_logit);
+  most = wave_max(most);
+  const bool has_teacher = a.soft > 0.0f && (__ballot(any) || __ballot(bad));
+  float p[kEach], total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    p[i] = 0.0f;
+    if (uint32_t(i) * 64 >= a.top) continue;
+    if (has_teacher && t[i] != -__builtin_inff()) p[i] = exp2((t[i] - most) * a.warm_rate);
+    total += p[i];
+  }
+  total = wave_sum(total);
+  double part = 0.0;  // sum of P (ln P - z / T), with ln P but for the sum's logarithm
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const uint32_t k = i * 64 + lane;
+    if (uint32_t(i) * 64 >= a.top) continue;
+    p[i] /= total;
+    if (p[i] != 0.0f && has_teacher) part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
+    if (k < a.top) {
+      out.id[k] = has_teacher ? id[i] : kNone;
+      out.logit[k] = v[i];
+      out.weight[k] = a.soft * float(a.inverse) * p[i];
+    }
+  }
+  part = wave_sum(part);
+  if (lane == 0) {
+    out.id[a.top] = label;
+    out.logit[a.top] = label_logit;
+    out.weight[a.top] = a.hard;
+    out.terms = (has_teacher ? 1u : 0u) | (label != kNone ? 2u : 0u);
+    out.taught = has_teacher ? part - ln(total) : 0.0;
+  }
+}
+
+// From which number exponents count: 2^(rate (z - base) - shift), where rate (z - base) - shift is one multiply-add.  Next to usual logits base
+// is 0 and shift the rounded product of rate and the largest logit; `rest` is what the rounding left, a factor of 2^rest that all
+// exponentials share.  Where the product is so large that the factor might overflow, the largest logit is subtracted first.
+struct Origin {
+  float base, warm_shift, cold_shift, warm_rest, cold_rest;
+};
+template <int KIND>
+__device__ __forceinline__ Origin origin(const DistillationArgs& a, float largest, bool always) {
+  const float rate = KIND == kTwo ? fmaxf(a.warm_rate, a.cold_rate) : a.warm_rate;
+  const bool near = !always && fabsf(largest * rate) < 1048576.0f;
+  const float m = near ? largest : 0.0f;
+  Origin o;
+  o.base = near ? 0.0f : largest;
+  o.warm_shift = m * a.warm_rate;
+  o.cold_shift = m * a.cold_rate;
+  o.warm_rest = __builtin_fmaf(m, a.warm_rate, -o.warm_shift);
+  // a power of Q's exponential has that power of its factor
+  o.cold_rest = KIND == kSquare ? 2.0f * o.warm_rest : KIND == kFourth ? 4.0f * o.warm_rest
+                : KIND == kOne ? o.warm_rest : __builtin_fmaf(m, a.cold_rate, -o.cold_shift);
+  return o;
+}
+
+// LANES lanes hold HELD logits each in registers, and EXTRA in LDS.  Of a row at once, one wavefront more learns what the teacher
+// and the label ask for, while the others wait for the logits.
+template <int PHASE, int LANES>
+constexpr int kBlock = LANES + (PHASE == kWhole ? 64 : 0);
+
+template <bool BF16, int KIND, int PHASE, int LANES, int HELD, int EXTRA>
+__global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_distillation(DistillationArgs a) {
+  constexpr int N = kPiece<BF16>, ES = BF16 ? 2 : 4, V = HELD / N, X = EXTRA / N, kWaves = LANES / 64;
+  constexpr bool kKeep = KIND != kTwo;  // exponentials stay; else distances
   __shared__ float waves[kWaves][3];
-  __shared__ uint32_t ids[kEntries];
-  __shared__ float logit[kEntries], weight[kEntries];
-  __shared__ double taught;             // the loss without the logarithms of the sums over the vocabulary, and whose it has
-  __shared__ uint32_t terms;            // bit 0: the teacher's, bit 1: the label's
+  __shared__ Lesson lesson;
+  __shared__ f32x4 extra[X > 0 ? X * N / 4 : 1][X > 0 ? LANES : 1];
   const uint32_t w = blockIdx.z, row = blockIdx.x + (PHASE == kWhole ? blockIdx.y * kGridRows : 0), n = a.w.tokens[w];
   if (row >= n) return;
   const uint32_t lane = threadIdx.x, wave = uniform(threadIdx.x / 64);
   const uint64_t z = a.w.at[kDistLogits][w] + uint64_t(row) * a.pitch * ES;
-  // this workgroup's part of the row: whole pieces, and what is left behind the last one
-  const uint32_t whole = a.vocab / N, lo = PHASE == kWhole ? 0 : min(blockIdx.y * a.part, whole);
-  const uint32_t hi = PHASE == kWhole ? whole : min(lo + a.part, whole);
-  const bool last = PHASE == kWhole || blockIdx.y + 1 == a.parts, tells = PHASE == kWhole || blockIdx.y == 0;
-  const uint32_t tail = last ? a.vocab - whole * N : 0;
+  // of the row in the workspace: three numbers of every part, and the lesson behind them
   float* const ws = reinterpret_cast<float*>(a.ws) + (uint64_t(w) * a.max_tokens + row) * a.stride;
-
-  // all loads of the row first
-  float x[V][N], odd = -__builtin_inff();
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const uint32_t p = lo + i * LANES + lane;
-#pragma unroll
-    for (int j = 0; j < N; ++j) x[i][j] = -__builtin_inff();
-    if (lo + i * LANES < hi && p < hi) load_elems<BF16, N>(z + uint64_t(p) * N * ES, x[i]);
-  }
-  if (lane < tail) load_elems<BF16, 1>(z + (uint64_t(whole) * N + lane) * ES, &odd);
-
-  // the teacher and the label: the first wavefront, four entries a lane
-  constexpr int kEach = kTop / 64;
+  Lesson* const kept = reinterpret_cast<Lesson*>(ws + (3 * a.parts + 1) / 2 * 2);
   if constexpr (PHASE == kMeasure) {
-    if (tells && wave == 0) {
-#pragma unroll
-      for (int i = 0; i <= kEach; ++i) {
-        const uint32_t k = i * 64 + lane;
-        if (k > a.top) continue;
-        uint32_t id = kNone;
-        if (k < a.top) id = read_id(a.w.at[kDistIds][w], uint64_t(row) * a.top + k, a.ids64, a.vocab);
-        else if (a.has_labels) id = read_id(a.w.at[kDistLabels][w], row, a.ids64, a.vocab);
-        float v = 0.0f;
-        if (id != kNone) load_elems<BF16, 1>(z + uint64_t(id) * ES, &v);
-        ws[3 * a.parts + k] = v;
-      }
-    }
-  } else if (wave == 0) {
-    float t[kEach], v[kEach];
-    uint32_t id[kEach];
-    float most = -__builtin_inff();
-    bool bad = false, any = false;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t k = i * 64 + lane;
-      id[i] = kNone;
-      t[i] = -__builtin_inff();
-      v[i] = 0.0f;
-      if (uint32_t(i) * 64 >= a.top || k >= a.top) continue;
-      id[i] = read_id(a.w.at[kDistIds][w], uint64_t(row) * a.top + k, a.ids64, a.vocab);
-      const uint64_t at = a.w.at[kDistTeacher][w] + (uint64_t(row) * a.top + k) * (a.teacher_bf16 ? 2 : 4);
-      if (a.teacher_bf16) load_elems<true, 1>(at, &t[i]);
-      else load_elems<false, 1>(at, &t[i]);
-      if (id[i] == kNone) t[i] = -__builtin_inff();
-    }
-    uint32_t label = kNone;
-    if (a.has_labels) label = uniform(read_id(a.w.at[kDistLabels][w], row, a.ids64, a.vocab));
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t k = i * 64 + lane;
-      if (id[i] != kNone) {
-        if constexpr (PHASE == kWhole) load_elems<BF16, 1>(z + uint64_t(id[i]) * ES, &v[i]);
-        else v[i] = ws[3 * a.parts + k];
-      }
-      most = fmaxf(most, t[i]);
-      bad = bad || t[i] != t[i];
-      any = any || t[i] > -__builtin_inff();
-    }
-    float label_logit = 0.0f;
-    if (label != kNone) {
-      if constexpr (PHASE == kWhole) load_elems<BF16, 1>(z + uint64_t(label) * ES, &label_logit);
-      else label_logit = ws[3 * a.parts + a.top];
-    }
-    most = wave_max(most);
-    const bool has_teacher = a.soft > 0.0f && (__ballot(any) || __ballot(bad));
-    float p[kEach], total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      p[i] = 0.0f;
-      if (id[i] != kNone && has_teacher) p[i] = __builtin_amdgcn_exp2f((t[i] - most) * a.warm_rate);
-      if (t[i] == -__builtin_inff()) p[i] = 0.0f;
-      total += p[i];
-    }
-    total = wave_sum(total);
-    double part = 0.0;  // sum of P (ln P - z / T), with ln P but for the sum's logarithm
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t k = i * 64 + lane;
-      p[i] /= total;
-      if (p[i] != 0.0f && has_teacher) part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
-      if (k < a.top) {
-        ids[k] = has_teacher ? id[i] : kNone;
-        logit[k] = v[i];
-        weight[k] = a.soft * float(a.inverse) * p[i];
-      }
-    }
-    part = wave_sum(part);
-    if (lane == 0) {
-      const bool has_label = label != kNone;
-      ids[a.top] = has_label ? label : kNone;
-      logit[a.top] = label_logit;
-      weight[a.top] = a.hard;
-      terms = (has_teacher ? 1u : 0u) | (has_label ? 2u : 0u);
-      taught = has_teacher ? part - log(double(total)) : 0.0;
-    }
-  }
-
-  // the largest logit
-  Sums s{-3.402823466e38f, 0.0f, 0.0f};
-  if constexpr (PHASE != kWrite) {
-    // pieces that are not held: largest logit and sums together
-    for (uint32_t p = lo + V * LANES + lane; p < hi; p += LANES) {
-      float y[N], m = s.largest;
-      load_elems<BF16, N>(z + uint64_t(p) * N * ES, y);
-#pragma unroll
-      for (int j = 0; j < N; ++j) m = fmaxf(m, y[j]);
-      const float d = s.largest - m;
-      s.largest = m;
-      s.warm *= __builtin_amdgcn_exp2f(d * a.warm_rate);
-      if constexpr (KIND != kOne) s.cold *= __builtin_amdgcn_exp2f(d * a.cold_rate);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float e = __builtin_amdgcn_exp2f((y[j] - m) * a.warm_rate);
-        s.warm += e;
-        if constexpr (KIND == kPower) s.cold += power(e, a.twice);
-        if constexpr (KIND == kTwo) s.cold += __builtin_amdgcn_exp2f((y[j] - m) * a.cold_rate);
-      }
-    }
-    float m = fmaxf(s.largest, odd);
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-#pragma unroll
-      for (int j = 0; j < N; ++j) m = fmaxf(m, x[i][j]);
-    m = wave_max(m);
-    if (lane % 64 == 0) waves[wave][0] = m;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, waves[k][0]);
-    const float d = s.largest - m;
-    s.largest = m;
-    s.warm *= __builtin_amdgcn_exp2f(d * a.warm_rate);
-    if constexpr (KIND != kOne) s.cold *= __builtin_amdgcn_exp2f(d * a.cold_rate);
-  } else {
-    __syncthreads();
-    // the parts' sums, joined by every wavefront for itself
-    Sums mine{-3.402823466e38f, 0.0f, 0.0f};
-    for (uint32_t k = lane % 64; k < a.parts; k += 64) {
-      const Sums o{ws[3 * k], ws[3 * k + 1], ws[3 * k + 2]};
-      const float m = fmaxf(mine.largest, o.largest);
-      const float f = __builtin_amdgcn_exp2f((mine.largest - m) * a.warm_rate), g = __builtin_amdgcn_exp2f((o.largest - m) * a.warm_rate);
-      const float h = __builtin_amdgcn_exp2f((mine.largest - m) * a.cold_rate), i = __builtin_amdgcn_exp2f((o.largest - m) * a.cold_rate);
-      mine = {m, mine.warm * f + o.warm * g, mine.cold * h + o.cold * i};
-    }
-    s.largest = wave_max(mine.largest);
-    const float d = mine.largest - s.largest;
-    s.warm = wave_sum(mine.warm * __builtin_amdgcn_exp2f(d * a.warm_rate));
-    s.cold = wave_sum(mine.cold * __builtin_amdgcn_exp2f(d * a.cold_rate));
-  }
-
-  // distances and exponentials of what is held, and their sums
-  float odd_warm = 0.0f, odd_cold = 0.0f;
-#pragma unroll
-  for (int i = 0; i <= V; ++i) {
-    if (i < V && lo + i * LANES >= hi) continue;
-#pragma unroll
-    for (int j = 0; j < (i < V ? N : 1); ++j) {
-      const float d = (i < V ? x[i][j] : odd) - s.largest;
-      float warm = 0.0f, cold = 0.0f;
-      if (PHASE != kWrite || kKeep || i == V) {
-        warm = __builtin_amdgcn_exp2f(d * a.warm_rate);
-        if constexpr (KIND == kPower) cold = power(warm, a.twice);
-        if constexpr (KIND == kTwo) cold = __builtin_amdgcn_exp2f(d * a.cold_rate);
-      }
-      if constexpr (PHASE != kWrite) {
-        s.warm += warm;
-        s.cold += cold;
-      }
-      if (i < V) x[i][j] = kKeep ? warm : d;
-      else odd_warm = warm, odd_cold = cold;
-    }
-  }
-  if constexpr (PHASE != kWrite) {
-    const float warm = wave_sum(s.warm), cold = KIND != kOne ? wave_sum(s.cold) : 0.0f;
-    if (lane % 64 == 0) waves[wave][1] = warm, waves[wave][2] = cold;
-    __syncthreads();
-    s.warm = s.cold = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      s.warm += waves[k][1];
-      s.cold += waves[k][2];
-    }
-    if constexpr (PHASE == kMeasure) {
-      if (lane == 0) {
-        ws[3 * blockIdx.y] = s.largest;
-        ws[3 * blockIdx.y + 1] = s.warm;
-        ws[3 * blockIdx.y + 2] = s.cold;
-      }
+    if (blockIdx.y == a.parts) {
+      if (wave == 0) learn<BF16>(a, w, row, z, *kept);
       return;
     }
   }
-  if constexpr (PHASE != kMeasure) {
-    if constexpr (KIND == kOne) s.cold = s.warm;
-    const bool has_teacher = uniform(terms) & 1, has_label = uniform(terms) & 2;
-    if (lane == 0 && tells) {
+  // this workgroup's part of the row: whole pieces, and what is left behind the last one
+  const uint32_t whole = a.vocab / N, lo = PHASE == kWhole ? 0 : min(blockIdx.y * a.part, whole);
+  const uint32_t hi = PHASE == kWhole ? whole : min(lo + a.part, whole), count = hi - lo;
+  const bool last = PHASE == kWhole || blockIdx.y + 1 == a.parts;
+  const uint32_t tail = last ? a.vocab - whole * N : 0;
+  const uint64_t mine = z + (uint64_t(lo) + lane) * N * ES;
+  float x[V][N], odd = -__builtin_inff(), largest = kLowest, warm = 0.0f, cold = 0.0f;
+  Origin from{};
+
+  if (PHASE == kWhole && wave == kWaves) {
+    learn<BF16>(a, w, row, z, lesson);
+    __syncthreads();  // the others' largest logits
+    __syncthreads();  // their sums
+  } else {
+    // all loads first; what goes to LDS before what stays
+    if constexpr (X > 0) {
+      constexpr int kBatch = 5;
+      static_assert(X % kBatch == 0);
+#pragma unroll 1
+      for (int i = 0; i < X; i += kBatch) {
+        float y[kBatch][N];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const uint32_t p = (V + i + b) * LANES;
+#pragma unroll
+          for (int j = 0; j < N; ++j) y[b][j] = -__builtin_inff();
+          if (p + lane < count) load_elems<BF16, N>(mine + uint64_t(p) * N * ES, y[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+          for (int j = 0; j < N; j += 4) {
+            extra[((i + b) * N + j) / 4][lane] = f32x4{y[b][j], y[b][j + 1], y[b][j + 2], y[b][j + 3]};
+            largest = fmaxf(largest, fmaxf(fmaxf(y[b][j], y[b][j + 1]), fmaxf(y[b][j + 2], y[b][j + 3])));
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[i][j] = -__builtin_inff();
+      if (uint32_t(i) * LANES + lane < count) load_elems<BF16, N>(mine + uint64_t(i) * LANES * N * ES, x[i]);
+    }
+    if (lane < tail) load_elems<BF16, 1>(z + (uint64_t(whole) * N + lane) * ES, &odd);
+
+    if constexpr (PHASE != kWrite) {
+      // pieces that are not held: largest logit and sums together
+      for (uint32_t p = (V + X) * LANES; p + lane < count; p += LANES) {
+        float y[N], m = largest;
+        load_elems<BF16, N>(mine + uint64_t(p) * N * ES, y);
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = fmaxf(m, y[j]);
+        warm *= exp2((largest - m) * a.warm_rate);
+        cold *= exp2((largest - m) * a.cold_rate);
+        largest = m;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          warm += exp2((y[j] - m) * a.warm_rate);
+          if constexpr (KIND != kOne) cold += exp2((y[j] - m) * a.cold_rate);
+        }
+      }
+      float m = fmaxf(largest, odd);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = fmaxf(m, x[i][j]);
+      m = wave_max(m);
+      if (lane % 64 == 0) waves[wave][0] = m;
+      __syncthreads();
+      m = across_max<kWaves>(&waves[0][0], 3);
+      from = origin<KIND>(a, m, PHASE != kWhole);
+      warm *= exp2(__builtin_fmaf(largest - m, a.warm_rate, from.warm_rest));  // (a factor that the held ones have)
+      if constexpr (KIND != kOne) cold *= exp2(__builtin_fmaf(largest - m, a.cold_rate, from.cold_rest));
+      largest = m;
+    } else {
+      // the parts' sums, joined by every wavefront for itself; the lesson for all
+      float m = kLowest, sum_warm = 0.0f, sum_cold = 0.0f;
+      for (uint32_t k = lane % 64; k < a.parts; k += 64) {
+        const float its_largest = ws[3 * k], its_warm = ws[3 * k + 1], its_cold = ws[3 * k + 2];
+        const float top = fmaxf(m, its_largest), now = m - top, its = its_largest - top;
+        sum_warm = sum_warm * exp2(now * a.warm_rate) + its_warm * exp2(its * a.warm_rate);
+        sum_cold = sum_cold * exp2(now * a.cold_rate) + its_cold * exp2(its * a.cold_rate);
+        m = top;
+      }
+      for (uint32_t k = lane; k <= a.top; k += LANES) {
+        lesson.id[k] = kept->id[k];
+        lesson.logit[k] = kept->logit[k];
+        lesson.weight[k] = kept->weight[k];
+      }
+      if (lane == 0) {
+        lesson.terms = kept->terms;
+        lesson.taught = kept->taught;
+      }
+      largest = wave_max(m);
+      warm = wave_sum(sum_warm * exp2((m - largest) * a.warm_rate));
+      cold = wave_sum(sum_cold * exp2((m - largest) * a.cold_rate));
+      from = origin<KIND>(a, largest, true);
+      __syncthreads();
+    }
+
+    // distances or exponentials in place of what is held, and their sums
+    auto measure = [&](float& v) {
+      if (kKeep || PHASE != kWrite) {
+        const float e = exp2(__builtin_fmaf(v, a.warm_rate, -from.warm_shift));
+        if constexpr (PHASE != kWrite) {
+          warm += e;
+          if constexpr (KIND == kSquare) cold = __builtin_fmaf(e, e, cold);
+          if constexpr (KIND == kFourth) cold = __builtin_fmaf(e * e, e * e, cold);
+          if constexpr (KIND == kTwo) cold += exp2(__builtin_fmaf(v, a.cold_rate, -from.cold_shift));
+        }
+        if constexpr (kKeep) v = e;
+      }
+    };
+    if (from.base != 0.0f) {  // also where it is NaN
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[i][j] -= from.base;
+    }
+    odd -= from.base;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (uint32_t(i) * LANES >= count) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j) measure(x[i][j]);
+      __builtin_amdgcn_sched_barrier(0);  // piece by piece: all at once would take as many registers again
+    }
+    measure(odd);
+    if constexpr (X > 0) {
+#pragma unroll 1
+      for (int i = 0; i < X * N / 4; ++i) {
+        if (uint32_t(V + i * 4 / N) * LANES >= count) break;
+        f32x4 y = extra[i][lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float v = y[j] - from.base;
+          measure(v);
+          y[j] = v;
+        }
+        extra[i][lane] = y;
+      }
+    }
+    if constexpr (PHASE != kWrite) {
+      warm = wave_sum(warm);
+      if constexpr (KIND != kOne) cold = wave_sum(cold);
+      if (lane % 64 == 0) waves[wave][1] = warm, waves[wave][2] = cold;
+      __syncthreads();
+    }
+  }
+  if constexpr (PHASE != kWrite) {
+    if constexpr (PHASE == kWhole) largest = across_max<kWaves>(&waves[0][0], 3);
+    warm = across_sum<kWaves>(&waves[0][1], 3);
+    cold = KIND != kOne ? across_sum<kWaves>(&waves[0][2], 3) : warm;
+  }
+  if constexpr (PHASE == kMeasure) {
+    if (lane == 0) {
+      ws[3 * blockIdx.y] = largest;
+      ws[3 * blockIdx.y + 1] = warm;
+      ws[3 * blockIdx.y + 2] = cold;
+    }
+  } else {
+    if constexpr (KIND == kOne) cold = warm;
+    const bool has_teacher = uniform(lesson.terms) & 1, has_label = uniform(lesson.terms) & 2;
+    const float share = has_teacher ? a.soft * float(a.inverse) / warm : 0.0f, label_share = has_label ? a.hard / cold : 0.0f;
+    const uint64_t out = a.w.at[kDistGradient][w] + uint64_t(row) * a.gradient_pitch * ES;
+    const bool holds = PHASE != kWhole || wave < kWaves;
+    if (a.gradient && holds) {
+      const uint64_t to = out + (uint64_t(lo) + lane) * N * ES;
+      const float kw = a.scale * (KIND == kOne ? share + label_share : share), kc = a.scale * label_share;
+      const bool none = !has_teacher && !has_label;  // zeros, whatever the logits are
+      auto gradient = [&](float v) {  // of what is held
+        if constexpr (KIND == kOne) return kw * v;
+        else if constexpr (KIND == kSquare) return v * __builtin_fmaf(kc, v, kw);
+        else if constexpr (KIND == kFourth) return v * __builtin_fmaf(kc, v * (v * v), kw);
+        else return __builtin_fmaf(kw, exp2(__builtin_fmaf(v, a.warm_rate, -from.warm_shift)),
+                                   kc * exp2(__builtin_fmaf(v, a.cold_rate, -from.cold_shift)));
+      };
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (uint32_t(i) * LANES + lane < count) {
+          float g[N];
+#pragma unroll
+          for (int j = 0; j < N; ++j) g[j] = none ? 0.0f : gradient(x[i][j]);
+          store_elems<BF16, N>(to + uint64_t(i) * LANES * N * ES, g);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (X > 0) {
+#pragma unroll 1
+        for (int i = 0; i < X; ++i) {
+          if (uint32_t(V + i) * LANES + lane >= count) break;
+          float y[N];
+#pragma unroll
+          for (int j = 0; j < N; j += 4) {
+            const f32x4 e = extra[(i * N + j) / 4][lane];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[j + k] = none ? 0.0f : gradient(e[k]);
+          }
+          store_elems<BF16, N>(to + uint64_t(V + i) * LANES * N * ES, y);
+        }
+      }
+      for (uint32_t p = (V + X) * LANES; p + lane < count; p += LANES) {
+        float y[N];
+        load_elems<BF16, N>(mine + uint64_t(p) * N * ES, y);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          float v = y[j] - from.base;
+          if constexpr (kKeep) v = exp2(__builtin_fmaf(v, a.warm_rate, -from.warm_shift));
+          y[j] = none ? 0.0f : gradient(v);
+        }
+        store_elems<BF16, N>(to + uint64_t(p) * N * ES, y);
+      }
+      if (lane < tail) {
+        const float g = none ? 0.0f : gradient(odd);
+        store_elems<BF16, 1>(out + (uint64_t(whole) * N + lane) * ES, &g);
+      }
+    }
+    if (PHASE == kWhole) from = origin<KIND>(a, largest, false);  // (the wavefront that learned has none)
+    if (PHASE == kWhole ? lane == LANES : lane == 0 && blockIdx.y == 0) {
       double loss = 0.0;
-      if (has_teacher) loss += double(a.soft) * (taught + double(s.largest) * a.inverse + log(double(s.warm)));
-      if (has_label) loss += double(a.hard) * (log(double(s.cold)) - (double(logit[a.top]) - double(s.largest)));
+      if (has_teacher)
+        loss += double(a.soft) * (lesson.taught + double(largest) * a.inverse + (ln(warm) - double(from.warm_rest) * 0.69314718055994531));
+      if (has_label)
+        loss += double(a.hard) *
+                ((ln(cold) - double(from.cold_rest) * 0.69314718055994531) - (double(lesson.logit[a.top]) - double(largest)));
       reinterpret_cast<CARAMEL_GLOBAL float*>(a.w.at[kDistLoss][w])[row] = float(loss);
     }
     if (!a.gradient) return;
-    const uint64_t out = a.w.at[kDistGradient][w] + uint64_t(row) * a.gradient_pitch * ES;
-    const float warm = has_teacher ? a.soft * float(a.inverse) / s.warm : 0.0f, cold = has_label ? a.hard / s.cold : 0.0f;
-    const bool none = !has_teacher && !has_label;  // zeros, whatever the logits are
-    const float kw = a.scale * (KIND == kOne ? warm + cold : warm), kc = a.scale * cold;
-    auto gradient = [&](float v) {  // of what is held
-      float g;
-      if constexpr (KIND == kOne) g = kw * v;
-      else if constexpr (KIND == kPower) g = __builtin_fmaf(kw, v, kc * power(v, a.twice));
-      else g = __builtin_fmaf(kw, __builtin_amdgcn_exp2f(v * a.warm_rate), kc * __builtin_amdgcn_exp2f(v * a.cold_rate));
-      return none ? 0.0f : g;
-    };
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t p = lo + i * LANES + lane;
-      if (lo + i * LANES >= hi || p >= hi) continue;
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[i][j] = gradient(x[i][j]);
-      store_elems<BF16, N>(out + uint64_t(p) * N * ES, x[i]);
-    }
-    for (uint32_t p = lo + V * LANES + lane; p < hi; p += LANES) {
-      float y[N];
-      load_elems<BF16, N>(z + uint64_t(p) * N * ES, y);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float d = y[j] - s.largest;
-        y[j] = gradient(kKeep ? __builtin_amdgcn_exp2f(d * a.warm_rate) : d);
-      }
-      store_elems<BF16, N>(out + uint64_t(p) * N * ES, y);
-    }
-    if (lane < tail) {
-      float g = KIND == kOne ? kw * odd_warm : __builtin_fmaf(kw, odd_warm, kc * odd_cold);
-      if (none) g = 0.0f;
-      store_elems<BF16, 1>(out + (uint64_t(whole) * N + lane) * ES, &g);
-    }
     __syncthreads();
     // the entries' own logits, each written by its first entry
-    for (uint32_t k = lane; k <= a.top; k += LANES) {
-      const uint32_t id = ids[k];
+    for (uint32_t k = lane; k <= a.top; k += kBlock<PHASE, LANES>) {
+      const uint32_t id = lesson.id[k];
       if (id == kNone || id / N < lo || (id / N >= hi && !last)) continue;
       float less = 0.0f;
       bool first = true;
       for (uint32_t i = 0; i <= a.top; ++i) {
-        const bool same = ids[i] == id;
-        less += same ? weight[i] : 0.0f;
+        const bool same = lesson.id[i] == id;
+        less += same ? lesson.weight[i] : 0.0f;
         first = first && !(same && i < k);
       }
       if (!first) continue;
-      const float d = logit[k] - s.largest, e = __builtin_amdgcn_exp2f(d * a.warm_rate);
-      float g = warm * e - less;
-      if constexpr (KIND == kOne) g = (warm + cold) * e - less;
-      if constexpr (KIND == kPower) g = __builtin_fmaf(cold, power(e, a.twice), warm * e) - less;
-      if constexpr (KIND == kTwo) g = __builtin_fmaf(cold, __builtin_amdgcn_exp2f(d * a.cold_rate), warm * e) - less;
-      g *= a.scale;
+      const float d = lesson.logit[k] - from.base, e = exp2(__builtin_fmaf(d, a.warm_rate, -from.warm_shift));
+      float g = share * e;
+      if constexpr (KIND == kOne) g = (share + label_share) * e;
+      if constexpr (KIND == kSquare) g = __builtin_fmaf(label_share, e * e, g);
+      if constexpr (KIND == kFourth) g = __builtin_fmaf(label_share, (e * e) * (e * e), g);
+      if constexpr (KIND == kTwo) g = __builtin_fmaf(label_share, exp2(__builtin_fmaf(d, a.cold_rate, -from.cold_shift)), g);
+      g = a.scale * (g - less);
       store_elems<BF16, 1>(out + uint64_t(id) * ES, &g);
     }
   }
@@ -338,35 +453,43 @@ uint32_t parts_of(uint64_t rows, uint32_t vocab) {
   return uint32_t(std::min<uint64_t>(most, (kPartGroups + rows - 1) / rows));
 }
 
+template <int LANES, int HELD, int EXTRA>
+struct Shape {
+  static constexpr int kLanes = LANES, kHeld = HELD, kExtra = EXTRA;
+};
+
 template <bool BF16, int KIND>
 hipError_t launch(const DistillationArgs& a, hipStream_t s) {
   if (a.parts > 1) {
-    const dim3 grid(a.max_tokens, a.parts, a.world);
-    hipLaunchKernelGGL((k_distillation<BF16, KIND, kMeasure, kPartLanes, kPartHeld>), grid, dim3(kPartLanes), 0, s, a);
+    const dim3 grid(a.max_tokens, a.parts + 1, a.world);  // one more learns the lesson
+    hipLaunchKernelGGL((k_distillation<BF16, KIND, kMeasure, kPartLanes, kPartHeld, 0>), grid, dim3(kPartLanes), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const dim3 write(a.max_tokens, a.gradient ? a.parts : 1, a.world);
-    hipLaunchKernelGGL((k_distillation<BF16, KIND, kWrite, kPartLanes, kPartHeld>), write, dim3(kPartLanes), 0, s, a);
+    hipLaunchKernelGGL((k_distillation<BF16, KIND, kWrite, kPartLanes, kPartHeld, 0>), write, dim3(kPartLanes), 0, s, a);
     return hipGetLastError();
   }
   const dim3 grid(std::min(a.max_tokens, kGridRows), (a.max_tokens + kGridRows - 1) / kGridRows, a.world);
-  if (a.vocab <= 256 * 32) {
-    hipLaunchKernelGGL((k_distillation<BF16, KIND, kWhole, 256, 32>), grid, dim3(256), 0, s, a);
-  } else if (a.vocab <= 1024 * 32) {
-    hipLaunchKernelGGL((k_distillation<BF16, KIND, kWhole, 1024, 32>), grid, dim3(1024), 0, s, a);
-  } else {
-    hipLaunchKernelGGL((k_distillation<BF16, KIND, kWhole, 1024, 64>), grid, dim3(1024), 0, s, a);
-  }
+  // the smallest that holds a row
+  auto fits = [&](auto shape) {
+    constexpr int LANES = decltype(shape)::kLanes, HELD = decltype(shape)::kHeld, EXTRA = decltype(shape)::kExtra;
+    hipLaunchKernelGGL((k_distillation<BF16, KIND, kWhole, LANES, HELD, EXTRA>), grid, dim3(kBlock<kWhole, LANES>), 0, s, a);
+  };
+  if (a.vocab <= 192 * 32) fits(Shape<192, 32, 0>{});
+  else if (a.vocab <= 448 * 32) fits(Shape<448, 32, 0>{});
+  else if (a.vocab <= 960 * 32) fits(Shape<960, 32, 0>{});
+  else if (a.vocab <= 960 * 64) fits(Shape<960, 64, 0>{});
+  else fits(Shape<960, BF16 ? 80 : 96, 40>{});  // (two wavefronts' registers; with 96 numbers as bf16 the compiler would spill)
   return hipGetLastError();
 }
 
 }  // namespace
 
 // Of fewer rows, each may have more parts; all of them together, no more than this.
-uint64_t distillation_workspace_bytes(uint32_t world, uint32_t vocab, uint32_t top, uint32_t max_tokens) {
+uint64_t distillation_workspace_bytes(uint32_t world, uint32_t vocab, uint32_t max_tokens) {
   const uint64_t rows = std::min<uint64_t>(uint64_t(world) * max_tokens, kFewRows);
   if (rows == 0 || parts_of(1, vocab) == 1) return 0;
-  return (3 * (kPartGroups + rows) + rows * (top + 1)) * 4;
+  return (3 * (kPartGroups + rows) + rows * (1 + sizeof(Lesson) / 4)) * 4;
 }
 
 hipError_t launch_distillation(const DistillationArgs& args, const AllBuffers<kDistBuffers>& v, hipStream_t s) {
@@ -375,20 +498,21 @@ hipError_t launch_distillation(const DistillationArgs& args, const AllBuffers<kD
   all.parts = parts_of(uint64_t(args.all) * args.max_tokens, args.vocab);
   const uint32_t pieces = args.vocab / (args.bf16 ? 8 : 4);
   all.part = (pieces + all.parts - 1) / all.parts;
-  all.stride = 3 * all.parts + args.top + 1;
+  all.stride = (3 * all.parts + 1) / 2 * 2 + sizeof(Lesson) / 4;
   const bool both = args.soft > 0.0f && args.has_labels;
-  const bool squares = args.temperature == 2.0f || args.temperature == 4.0f;
-  const int kind = !both || args.temperature == 1.0f ? kOne : squares ? kPower : kTwo;
+  const int kind = !both || args.temperature == 1.0f ? kOne : args.temperature == 2.0f ? kSquare : args.temperature == 4.0f ? kFourth : kTwo;
   const double log2e = 1.4426950408889634;
   // without a teacher's part, all is at temperature 1
   all.warm_rate = float(log2e / (args.soft > 0.0f ? double(args.temperature) : 1.0));
   all.cold_rate = float(log2e);
   all.inverse = 1.0 / double(args.temperature);
-  all.twice = args.temperature == 4.0f;
   return in_groups(all, v, [&](DistillationArgs a, uint32_t g) {
     a.ws += uint64_t(g) * a.max_tokens * a.stride * 4;
-    if (a.bf16) return kind == kOne ? launch<true, kOne>(a, s) : kind == kPower ? launch<true, kPower>(a, s) : launch<true, kTwo>(a, s);
-    return kind == kOne ? launch<false, kOne>(a, s) : kind == kPower ? launch<false, kPower>(a, s) : launch<false, kTwo>(a, s);
+    const bool b = a.bf16;
+    if (kind == kOne) return b ? launch<true, kOne>(a, s) : launch<false, kOne>(a, s);
+    if (kind == kSquare) return b ? launch<true, kSquare>(a, s) : launch<false, kSquare>(a, s);
+    if (kind == kFourth) return b ? launch<true, kFourth>(a, s) : launch<false, kFourth>(a, s);
+    return b ? launch<true, kTwo>(a, s) : launch<false, kTwo>(a, s);
   });
 }
 

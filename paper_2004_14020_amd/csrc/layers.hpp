@@ -189,9 +189,8 @@ struct DistillationArgs {
   uint32_t parts, part, stride;  // of a row; pieces of a part; floats of a row in the workspace
   float warm_rate, cold_rate;  // log2(e) / temperature, log2(e)
   double inverse;              // 1 / temperature
-  bool twice;
 };
-uint64_t distillation_workspace_bytes(uint32_t world, uint32_t vocab, uint32_t top, uint32_t max_tokens);
+uint64_t distillation_workspace_bytes(uint32_t world, uint32_t vocab, uint32_t max_tokens);
 hipError_t launch_distillation(const DistillationArgs& args, const AllBuffers<kDistBuffers>& v, hipStream_t s);
 
 }  // namespace caramel
