@@ -28,35 +28,10 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr uint32_t kGridRows = 1u << 20;  // along x: a grid has less than 2^32 lanes in a direction
 constexpr float kLowest = -3.402823466e38f;
 
-__device__ __forceinline__ uint32_t read_id(uint64_t at, uint64_t i, bool wide, uint32_t vocab) {
-  const uint64_t id = wide ? reinterpret_cast<const CARAMEL_GLOBAL uint64_t*>(at)[i]
-                           : reinterpret_cast<const CARAMEL_GLOBAL uint32_t*>(at)[i];
-  return id < vocab ? uint32_t(id) : kNone;  // a negative id is a huge one
+__device__ __forceinline__ uint64_t load_id(uint64_t at, uint64_t i, bool wide) {
+  return wide ? reinterpret_cast<const CARAMEL_GLOBAL uint64_t*>(at)[i] : reinterpret_cast<const CARAMEL_GLOBAL uint32_t*>(at)[i];
 }
-
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-
-// Over one number of each of COUNT (16 at most) wavefronts, `step` apart in LDS: every group of 16 lanes for itself, so that it takes one
-// register and not COUNT.
-template <int COUNT>
-__device__ __forceinline__ float across_max(const float* lds, int step) {
-  float v = lds[min(int(threadIdx.x % 16), COUNT - 1) * step];
-#pragma unroll
-  for (int d = 8; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-template <int COUNT>
-__device__ __forceinline__ float across_sum(const float* lds, int step) {
-  const int k = threadIdx.x % 16;
-  float v = k < COUNT ? lds[k * step] : 0.0f;
-#pragma unroll
-  for (int d = 8; d; d /= 2) v += __shfl_xor(v, d);
-  return v;
-}
+__device__ __forceinline__ uint32_t known(uint64_t id, uint32_t vocab) { return id < vocab ? uint32_t(id) : kNone; }  // negative: huge
 
 __device__ __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -80,35 +55,35 @@ template <bool BF16>
 __device__ __forceinline__ void learn(const DistillationArgs& a, uint32_t w, uint32_t row, uint64_t z, Lesson& out) {
   constexpr int ES = BF16 ? 2 : 4, kEach = kTop / 64;
   const uint32_t lane = threadIdx.x % 64;
+  // everything that needs no id is asked for at once, by all lanes (those without an entry: the last one's)
   float t[kEach], v[kEach];
+  uint64_t asked[kEach], asked_label = ~uint64_t(0);
+  const uint64_t first = uint64_t(row) * a.top;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    asked[i] = ~uint64_t(0);
+    if (uint32_t(i) * 64 >= a.top) continue;
+    const uint64_t k = first + min(i * 64 + lane, a.top - 1);
+    asked[i] = load_id(a.w.at[kDistIds][w], k, a.ids64);
+    if (a.teacher_bf16) load_elems<true, 1>(a.w.at[kDistTeacher][w] + k * 2, &t[i]);
+    else load_elems<false, 1>(a.w.at[kDistTeacher][w] + k * 4, &t[i]);
+  }
+  if (a.has_labels) asked_label = load_id(a.w.at[kDistLabels][w], row, a.ids64);
   uint32_t id[kEach];
-  float most = -__builtin_inff();
+  const uint32_t label = uniform(known(asked_label, a.vocab));
+  float most = -__builtin_inff(), label_logit = 0.0f;
   bool bad = false, any = false;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const uint32_t k = i * 64 + lane;
-    id[i] = kNone;
-    t[i] = -__builtin_inff();
-    v[i] = 0.0f;
-    if (uint32_t(i) * 64 >= a.top || k >= a.top) continue;
-    id[i] = read_id(a.w.at[kDistIds][w], uint64_t(row) * a.top + k, a.ids64, a.vocab);
-    const uint64_t at = a.w.at[kDistTeacher][w] + (uint64_t(row) * a.top + k) * (a.teacher_bf16 ? 2 : 4);
-    if (a.teacher_bf16) load_elems<true, 1>(at, &t[i]);
-    else load_elems<false, 1>(at, &t[i]);
-  }
-  uint32_t label = kNone;
-  if (a.has_labels) label = uniform(read_id(a.w.at[kDistLabels][w], row, a.ids64, a.vocab));
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
+    id[i] = i * 64 + lane < a.top ? known(asked[i], a.vocab) : kNone;
     if (uint32_t(i) * 64 >= a.top) continue;
-    if (id[i] != kNone) load_elems<BF16, 1>(z + uint64_t(id[i]) * ES, &v[i]);
-    else t[i] = -__builtin_inff();
+    load_elems<BF16, 1>(z + uint64_t(id[i] != kNone ? id[i] : 0) * ES, &v[i]);
+    if (id[i] == kNone) t[i] = -__builtin_inff();
     most = fmaxf(most, t[i]);
     bad = bad || t[i] != t[i];
     any = any || t[i] > -__builtin_inff();
   }
-  float label_logit = 0.0f;
-  if (label != kNone) load_elems<BF16, 1>(z + uint64_t(label) * ES, &label_logit);
+  load_elems<BF16, 1>(z + uint64_t(label != kNone ? label : 0) * ES, &label_logit);
   most = wave_max(most);
   const bool has_teacher = a.soft > 0.0f && (__ballot(any) || __ballot(bad));
   float p[kEach], total = 0.0f;
@@ -126,7 +101,7 @@ __device__ __forceinline__ void learn(const DistillationArgs& a, uint32_t w, uin
     const uint32_t k = i * 64 + lane;
     if (uint32_t(i) * 64 >= a.top) continue;
     p[i] /= total;
-    if (p[i] != 0.0f && has_teacher) part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
+    if (id[i] != kNone && p[i] != 0.0f && has_teacher) part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
     if (k < a.top) {
       out.id[k] = has_teacher ? id[i] : kNone;
       out.logit[k] = v[i];
@@ -190,12 +165,17 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
       return;
     }
   }
-  // this workgroup's part of the row: whole pieces, and what is left behind the last one
-  const uint32_t whole = a.vocab / N, lo = PHASE == kWhole ? 0 : min(blockIdx.y * a.part, whole);
-  const uint32_t hi = PHASE == kWhole ? whole : min(lo + a.part, whole), count = hi - lo;
+  // this workgroup's part of the row
+  const uint32_t lo = PHASE == kWhole ? 0 : min(blockIdx.y * a.part, a.vocab);
   const bool last = PHASE == kWhole || blockIdx.y + 1 == a.parts;
-  const uint32_t tail = last ? a.vocab - whole * N : 0;
-  const uint64_t mine = z + (uint64_t(lo) + lane) * N * ES;
+  const uint32_t hi = last ? a.vocab : min(lo + a.part, a.vocab), count = (hi - lo) & ~uint32_t(BF16 ? 1 : 0);
+  const Row<BF16> in(z + uint64_t(lo) * ES, hi - lo);
+  const uint32_t col = lane * N;  // of a lane's first piece; the next one is LANES pieces on
+  // what is behind the part counts for nothing
+  auto cut = [&](uint32_t at, float* v) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = at + j < count ? v[j] : -__builtin_inff();
+  };
   float x[V][N], odd = -__builtin_inff(), largest = kLowest, warm = 0.0f, cold = 0.0f;
   Origin from{};
 
@@ -210,36 +190,40 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
       static_assert(X % kBatch == 0);
 #pragma unroll 1
       for (int i = 0; i < X; i += kBatch) {
-        float y[kBatch][N];
+        u32x4 raw[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) raw[b] = in.get(col + uint32_t(V + i + b) * LANES * N);
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-          const uint32_t p = (V + i + b) * LANES;
-#pragma unroll
-          for (int j = 0; j < N; ++j) y[b][j] = -__builtin_inff();
-          if (p + lane < count) load_elems<BF16, N>(mine + uint64_t(p) * N * ES, y[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b)
+          float y[N];
+          widen<BF16>(raw[b], y);
+          if (uint32_t(V + i + b + 1) * LANES * N > count) cut(col + uint32_t(V + i + b) * LANES * N, y);
 #pragma unroll
           for (int j = 0; j < N; j += 4) {
-            extra[((i + b) * N + j) / 4][lane] = f32x4{y[b][j], y[b][j + 1], y[b][j + 2], y[b][j + 3]};
-            largest = fmaxf(largest, fmaxf(fmaxf(y[b][j], y[b][j + 1]), fmaxf(y[b][j + 2], y[b][j + 3])));
+            extra[((i + b) * N + j) / 4][lane] = f32x4{y[j], y[j + 1], y[j + 2], y[j + 3]};
+            largest = fmaxf(largest, fmaxf(fmaxf(y[j], y[j + 1]), fmaxf(y[j + 2], y[j + 3])));
           }
+        }
       }
     }
+    {
+      u32x4 raw[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+      for (int i = 0; i < V; ++i) raw[i] = in.get(col + uint32_t(i) * LANES * N);
+      if (in.odd() && lane == 0) odd = bf16_low(in.get_last());
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[i][j] = -__builtin_inff();
-      if (uint32_t(i) * LANES + lane < count) load_elems<BF16, N>(mine + uint64_t(i) * LANES * N * ES, x[i]);
+      for (int i = 0; i < V; ++i) {
+        widen<BF16>(raw[i], x[i]);
+        if (uint32_t(i + 1) * LANES * N > count) cut(col + uint32_t(i) * LANES * N, x[i]);
+      }
     }
-    if (lane < tail) load_elems<BF16, 1>(z + (uint64_t(whole) * N + lane) * ES, &odd);
 
     if constexpr (PHASE != kWrite) {
       // pieces that are not held: largest logit and sums together
-      for (uint32_t p = (V + X) * LANES; p + lane < count; p += LANES) {
+      for (uint32_t p = (V + X) * LANES * N; p < count; p += LANES * N) {
         float y[N], m = largest;
-        load_elems<BF16, N>(mine + uint64_t(p) * N * ES, y);
+        widen<BF16>(in.get(p + col), y);
+        cut(p + col, y);
 #pragma unroll
         for (int j = 0; j < N; ++j) m = fmaxf(m, y[j]);
         warm *= exp2((largest - m) * a.warm_rate);
@@ -312,7 +296,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
     odd -= from.base;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (uint32_t(i) * LANES >= count) continue;
+      if (uint32_t(i) * LANES * N >= count) continue;
 #pragma unroll
       for (int j = 0; j < N; ++j) measure(x[i][j]);
       __builtin_amdgcn_sched_barrier(0);  // piece by piece: all at once would take as many registers again
@@ -321,7 +305,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
     if constexpr (X > 0) {
 #pragma unroll 1
       for (int i = 0; i < X * N / 4; ++i) {
-        if (uint32_t(V + i * 4 / N) * LANES >= count) break;
+        if (uint32_t(V + i * 4 / N) * LANES * N >= count) break;
         f32x4 y = extra[i][lane];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -357,7 +341,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
     const uint64_t out = a.w.at[kDistGradient][w] + uint64_t(row) * a.gradient_pitch * ES;
     const bool holds = PHASE != kWhole || wave < kWaves;
     if (a.gradient && holds) {
-      const uint64_t to = out + (uint64_t(lo) + lane) * N * ES;
+      const Row<BF16> to(out + uint64_t(lo) * ES, hi - lo);
       const float kw = a.scale * (KIND == kOne ? share + label_share : share), kc = a.scale * label_share;
       const bool none = !has_teacher && !has_label;  // zeros, whatever the logits are
       auto gradient = [&](float v) {  // of what is held
@@ -369,18 +353,17 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
       };
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (uint32_t(i) * LANES + lane < count) {
-          float g[N];
+        if (uint32_t(i) * LANES * N >= count) continue;
+        float g[N];
 #pragma unroll
-          for (int j = 0; j < N; ++j) g[j] = none ? 0.0f : gradient(x[i][j]);
-          store_elems<BF16, N>(to + uint64_t(i) * LANES * N * ES, g);
-        }
+        for (int j = 0; j < N; ++j) g[j] = none ? 0.0f : gradient(x[i][j]);
+        to.template put<true>(col + uint32_t(i) * LANES * N, narrow<BF16>(g));
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (X > 0) {
 #pragma unroll 1
         for (int i = 0; i < X; ++i) {
-          if (uint32_t(V + i) * LANES + lane >= count) break;
+          if (uint32_t(V + i) * LANES * N >= count) break;
           float y[N];
 #pragma unroll
           for (int j = 0; j < N; j += 4) {
@@ -388,23 +371,23 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
 #pragma unroll
             for (int k = 0; k < 4; ++k) y[j + k] = none ? 0.0f : gradient(e[k]);
           }
-          store_elems<BF16, N>(to + uint64_t(V + i) * LANES * N * ES, y);
+          to.template put<true>(col + uint32_t(V + i) * LANES * N, narrow<BF16>(y));
         }
       }
-      for (uint32_t p = (V + X) * LANES; p + lane < count; p += LANES) {
+      for (uint32_t p = (V + X) * LANES * N; p < count; p += LANES * N) {
         float y[N];
-        load_elems<BF16, N>(mine + uint64_t(p) * N * ES, y);
+        widen<BF16>(in.get(p + col), y);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           float v = y[j] - from.base;
           if constexpr (kKeep) v = exp2(__builtin_fmaf(v, a.warm_rate, -from.warm_shift));
           y[j] = none ? 0.0f : gradient(v);
         }
-        store_elems<BF16, N>(to + uint64_t(p) * N * ES, y);
+        to.template put<true>(p + col, narrow<BF16>(y));
       }
-      if (lane < tail) {
+      if (in.odd() && lane == 0) {
         const float g = none ? 0.0f : gradient(odd);
-        store_elems<BF16, 1>(out + (uint64_t(whole) * N + lane) * ES, &g);
+        store_elems<BF16, 1>(out + uint64_t(hi - 1) * ES, &g);
       }
     }
     if (PHASE == kWhole) from = origin<KIND>(a, largest, false);  // (the wavefront that learned has none)
@@ -422,7 +405,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
     // the entries' own logits, each written by its first entry
     for (uint32_t k = lane; k <= a.top; k += kBlock<PHASE, LANES>) {
       const uint32_t id = lesson.id[k];
-      if (id == kNone || id / N < lo || (id / N >= hi && !last)) continue;
+      if (id == kNone || id < lo || id >= hi) continue;
       float less = 0.0f;
       bool first = true;
       for (uint32_t i = 0; i <= a.top; ++i) {
@@ -496,8 +479,7 @@ hipError_t launch_distillation(const DistillationArgs& args, const AllBuffers<kD
   if (args.max_tokens == 0) return hipSuccess;
   DistillationArgs all = args;
   all.parts = parts_of(uint64_t(args.all) * args.max_tokens, args.vocab);
-  const uint32_t pieces = args.vocab / (args.bf16 ? 8 : 4);
-  all.part = (pieces + all.parts - 1) / all.parts;
+  all.part = ((args.vocab + all.parts - 1) / all.parts + 7) / 8 * 8;
   all.stride = (3 * all.parts + 1) / 2 * 2 + sizeof(Lesson) / 4;
   const bool both = args.soft > 0.0f && args.has_labels;
   const int kind = !both || args.temperature == 1.0f ? kOne : args.temperature == 2.0f ? kSquare : args.temperature == 4.0f ? kFourth : kTwo;

@@ -186,7 +186,7 @@ struct DistillationArgs {
   bool bf16, teacher_bf16, ids64, has_labels, gradient;
   unsigned char* ws;
   // made by the launch
-  uint32_t parts, part, stride;  // of a row; pieces of a part; floats of a row in the workspace
+  uint32_t parts, part, stride;  // of a row; logits of a part; floats of a row in the workspace
   float warm_rate, cold_rate;  // log2(e) / temperature, log2(e)
   double inverse;              // 1 / temperature
 };

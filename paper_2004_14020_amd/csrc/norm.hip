@@ -18,25 +18,71 @@
 namespace caramel {
 namespace {
 
-// N gains; they are in the plan's type, which need not be that of the rows.
-template <bool BF16, int N>
-__device__ __forceinline__ void load_gains(uint64_t gain, uint32_t col, uint32_t width, float* g) {
-  constexpr int ES = BF16 ? 2 : 4;
-  if (col + N <= width) {
-    load_elems<BF16, N>(gain + uint64_t(col) * ES, g);
-  } else {
+// The pieces of a lane: V of a row of a team of LANES.
+template <bool BF16, int V, int LANES>
+struct Pieces {
+  static constexpr int N = kPiece<BF16>;
+  u32x4 raw[V];
+  uint32_t last;
+
+  static __device__ __forceinline__ uint32_t column(uint32_t lane, int v) { return (v * LANES + lane) * N; }
+  __device__ __forceinline__ void load(const Row<BF16>& row, uint32_t lane) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      g[j] = 0.0f;
-      if (col + j < width) load_elems<BF16, 1>(gain + uint64_t(col + j) * ES, g + j);
+    for (int v = 0; v < V; ++v) raw[v] = row.get(column(lane, v));
+    if (row.odd()) last = row.get_last();
+  }
+  // before the first use of an odd row's values
+  __device__ __forceinline__ void finish(const Row<BF16>& row, uint32_t lane) {
+    if (row.odd()) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) row.merge_last(column(lane, v), last, raw[v]);
     }
   }
+};
+
+template <bool BF16, bool STREAM>
+__device__ __forceinline__ void store_piece(const Row<BF16>& row, uint32_t col, const float* v) {
+  const u32x4 raw = narrow<BF16>(v);
+  row.template put<STREAM>(col, raw);
+  if (row.odd()) row.put_last(col, raw);
 }
-template <int N>
-__device__ __forceinline__ void load_gain(uint64_t gain, bool bf16, uint32_t col, uint32_t width, float* g) {
-  if (bf16) load_gains<true, N>(gain, col, width, g);
-  else load_gains<false, N>(gain, col, width, g);
-}
+
+// Gains are in the plan's type, which need not be that of the rows: the N of a piece of the rows.
+template <bool BF16, int V, int LANES>
+struct Gains {
+  static constexpr int N = kPiece<BF16>;
+  u32x4 raw[V][2];
+  uint32_t last;
+
+  // (bf16 gains of fp32 rows: the 16 bytes hold twice as many as are needed, and what is behind the row is not read)
+  __device__ __forceinline__ void load(uint64_t at, bool bf16, uint32_t width, uint32_t lane) {
+    if (bf16) {
+      const Row<true> row(at, width);
+#pragma unroll
+      for (int v = 0; v < V; ++v) raw[v][0] = row.get((v * LANES + lane) * N);
+      if (row.odd()) last = row.get_last();
+    } else {
+      const Row<false> row(at, width);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q) raw[v][q] = row.get((v * LANES + lane) * N + 4 * q);
+    }
+  }
+  __device__ __forceinline__ void get(bool bf16, uint32_t width, uint32_t lane, int v, float* g) const {
+    if (bf16) {
+      u32x4 r = raw[v][0];
+      if (width % 2) Row<true>(0, width).merge_last((v * LANES + lane) * N, last, r);
+      float all[8];
+      widen<true>(r, all);
+#pragma unroll
+      for (int j = 0; j < N; ++j) g[j] = all[j];
+    } else {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) widen<false>(raw[v][q], g + 4 * q);
+    }
+  }
+};
 
 constexpr uint32_t kGridGroups = 1u << 20;  // workgroups along x: a grid has less than 2^32 lanes in a direction
 
@@ -48,23 +94,33 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
   const uint32_t w = blockIdx.y, group = blockIdx.x + blockIdx.z * kGridGroups;
   const uint32_t row = group * (kWaves / TEAM) + uniform(threadIdx.x / 64) / TEAM;
   if (row >= a.w.tokens[w]) return;
-  const uint32_t lane = threadIdx.x % (64 * TEAM);
+  constexpr int LANES = 64 * TEAM;
+  const uint32_t lane = threadIdx.x % LANES;
   const uint64_t at = uint64_t(row) * a.pitch * ES;
+  using P = Pieces<BF16, V, LANES>;
+  const Row<BF16> rx(a.w.at[kNormX][w] + at, a.width), rr(a.w.at[kNormResidual][w] + at, a.width);
+  P x, r;
+  x.load(rx, lane);
+  if (a.residual) r.load(rr, lane);
+  Gains<BF16, V, LANES> gain;
+  gain.load(a.w.at[kNormGain][w], a.gain_bf16, a.width, lane);
+  x.finish(rx, lane);
   float h[V][N];
 #pragma unroll
-  for (int v = 0; v < V; ++v) load_piece<BF16>(a.w.at[kNormX][w] + at, (v * 64 * TEAM + lane) * N, a.width, h[v]);
+  for (int v = 0; v < V; ++v) widen<BF16>(x.raw[v], h[v]);
   if (a.residual) {
+    const Row<BF16> rs(a.w.at[kNormSum][w] + at, a.width);
+    r.finish(rr, lane);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const uint32_t col = (v * 64 * TEAM + lane) * N;
-      float r[N];
-      load_piece<BF16>(a.w.at[kNormResidual][w] + at, col, a.width, r);
+      float y[N];
+      widen<BF16>(r.raw[v], y);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        h[v][j] += r[j];
+        h[v][j] += y[j];
         if constexpr (BF16) h[v][j] = bf16_low(bf16_pair(h[v][j], 0.0f));
       }
-      store_piece<BF16>(a.w.at[kNormSum][w] + at, col, a.width, h[v]);
+      store_piece<BF16, false>(rs, P::column(lane, v), h[v]);
     }
   }
   double ss = 0.0;
@@ -73,16 +129,16 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) ss = __builtin_fma(double(h[v][j]), double(h[v][j]), ss);
   ss = team_sum<TEAM>(ss, lds);
-  const float r = float(1.0 / sqrt(ss / double(a.width) + double(a.eps)));
-  if (lane == 0) reinterpret_cast<CARAMEL_GLOBAL float*>(a.w.at[kNormRstd][w])[row] = r;
+  const float rstd = float(1.0 / sqrt(ss / double(a.width) + double(a.eps)));
+  if (lane == 0) reinterpret_cast<CARAMEL_GLOBAL float*>(a.w.at[kNormRstd][w])[row] = rstd;
+  const Row<BF16> ry(a.w.at[kNormY][w] + at, a.width);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const uint32_t col = (v * 64 * TEAM + lane) * N;
     float g[N];
-    load_gain<N>(a.w.at[kNormGain][w], a.gain_bf16, col, a.width, g);
+    gain.get(a.gain_bf16, a.width, lane, v, g);
 #pragma unroll
-    for (int j = 0; j < N; ++j) h[v][j] = (h[v][j] * r) * g[j];
-    store_piece<BF16>(a.w.at[kNormY][w] + at, col, a.width, h[v]);
+    for (int j = 0; j < N; ++j) h[v][j] = (h[v][j] * rstd) * g[j];
+    store_piece<BF16, false>(ry, P::column(lane, v), h[v]);
   }
 }
 
@@ -105,61 +161,80 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
   __shared__ float sums[kTeams > 1 ? (kTeams - 1) * 64 * TEAM * N : 1];
   const uint32_t w = blockIdx.y, n = a.w.tokens[w], first = blockIdx.x * span, last = min(first + span, n);
   if (first >= n) return;
-  const uint32_t lane = threadIdx.x % (64 * TEAM), team = uniform(threadIdx.x / 64) / TEAM;
+  constexpr int LANES = 64 * TEAM;
+  const uint32_t lane = threadIdx.x % LANES, team = uniform(threadIdx.x / 64) / TEAM;
+  using P = Pieces<BF16, V, LANES>;
+  Gains<BF16, V, LANES> gain;
+  gain.load(a.w.at[kNormGradGain][w], a.gain_bf16, a.width, lane);
   float sum[V][N] = {};
   uint32_t turn = 0;
   for (uint32_t row = first + team; row < last; row += kTeams) {
     const uint64_t at = uint64_t(row) * a.pitch * ES;
+    const Row<BF16> rx(a.w.at[kNormGradX][w] + at, a.width), ry(a.w.at[kNormGradDy][w] + at, a.width);
+    const Row<BF16> rd(a.w.at[kNormGradDsum][w] + at, a.width), ro(a.w.at[kNormGradDx][w] + at, a.width);
+    P x, y, d;
+    x.load(rx, lane);
+    y.load(ry, lane);
+    if (a.dsum) d.load(rd, lane);
     const float r = reinterpret_cast<const CARAMEL_GLOBAL float*>(a.w.at[kNormGradRstd][w])[row];
-    float x[V][N], u[V][N], c = 0.0f;
+    x.finish(rx, lane);
+    y.finish(ry, lane);
+    float c = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const uint32_t col = (v * 64 * TEAM + lane) * N;
-      float g[N];
-      load_piece<BF16>(a.w.at[kNormGradX][w] + at, col, a.width, x[v]);
-      load_piece<BF16>(a.w.at[kNormGradDy][w] + at, col, a.width, u[v]);
-      load_gain<N>(a.w.at[kNormGradGain][w], a.gain_bf16, col, a.width, g);
+      float n[N], u[N], g[N];
+      widen<BF16>(x.raw[v], n);
+      widen<BF16>(y.raw[v], u);
+      gain.get(a.gain_bf16, a.width, lane, v, g);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        x[v][j] *= r;
-        sum[v][j] = __builtin_fmaf(u[v][j], x[v][j], sum[v][j]);
-        u[v][j] *= g[j];
-        c = __builtin_fmaf(u[v][j], x[v][j], c);
+        n[j] *= r;
+        sum[v][j] = __builtin_fmaf(u[j], n[j], sum[v][j]);
+        c = __builtin_fmaf(u[j] * g[j], n[j], c);
       }
     }
     c = team_sum<TEAM>(c, lds[turn]) / float(a.width);
     turn ^= 1;
+    if (a.dsum) d.finish(rd, lane);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const uint32_t col = (v * 64 * TEAM + lane) * N;
-      float d[N] = {};
-      if (a.dsum) load_piece<BF16>(a.w.at[kNormGradDsum][w] + at, col, a.width, d);
+      float n[N], u[N], g[N], o[N];
+      widen<BF16>(x.raw[v], n);
+      widen<BF16>(y.raw[v], u);
+      gain.get(a.gain_bf16, a.width, lane, v, g);
+      if (a.dsum) {
+        widen<BF16>(d.raw[v], o);
+      } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j) d[j] = __builtin_fmaf(r, __builtin_fmaf(-x[v][j], c, u[v][j]), d[j]);
-      store_piece<BF16>(a.w.at[kNormGradDx][w] + at, col, a.width, d);
+        for (int j = 0; j < N; ++j) o[j] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) o[j] = __builtin_fmaf(r, __builtin_fmaf(-(n[j] * r), c, u[j] * g[j]), o[j]);
+      store_piece<BF16, false>(ro, P::column(lane, v), o);
     }
   }
   // the workgroup's teams, one piece of every lane after the other
-  float* const out = reinterpret_cast<float*>(a.ws) + w * stride + uint64_t(blockIdx.x) * a.width;
+  const Row<false> out(reinterpret_cast<uint64_t>(a.ws) + (w * stride + uint64_t(blockIdx.x) * a.width) * 4, a.width);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     if constexpr (kTeams > 1) {
       if (team) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) sums[((team - 1) * N + j) * 64 * TEAM + lane] = sum[v][j];
+        for (int j = 0; j < N; ++j) sums[((team - 1) * N + j) * LANES + lane] = sum[v][j];
       }
       __syncthreads();
       if (!team) {
 #pragma unroll
         for (int k = 0; k < kTeams - 1; ++k)
 #pragma unroll
-          for (int j = 0; j < N; ++j) sum[v][j] += sums[(k * N + j) * 64 * TEAM + lane];
+          for (int j = 0; j < N; ++j) sum[v][j] += sums[(k * N + j) * LANES + lane];
       }
       __syncthreads();
     }
-    if (!team) store_piece<false>(reinterpret_cast<uint64_t>(out), (v * 64 * TEAM + lane) * N, a.width, sum[v]);
-    if constexpr (N == 8)
-      if (!team) store_piece<false>(reinterpret_cast<uint64_t>(out), (v * 64 * TEAM + lane) * N + 4, a.width, sum[v] + 4);
+    if (!team) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) out.put(P::column(lane, v) + 4 * q, narrow<false>(sum[v] + 4 * q));
+    }
   }
 }
 

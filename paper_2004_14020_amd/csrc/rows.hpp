@@ -1,61 +1,108 @@
-// Rows that stay in the registers of a team of wavefronts: how their columns are dealt out, and sums over them.
+// Rows that stay in the registers of a team of wavefronts: loads and stores of pieces of them, and sums over them.
 #pragma once
 
 #include "vec.hpp"
 
 namespace caramel {
 
-// Columns that a lane takes at once: 16 bytes.  Lane l of a team has the pieces l, l + lanes, l + 2 lanes, ... of a row.
+// Columns that a lane takes at once: 16 bytes.
 template <bool BF16>
 constexpr int kPiece = BF16 ? 8 : 4;
 
-// A piece of a row that has `width` columns; zeros behind them.
+constexpr int kStreaming = 2;  // of a buffer access: non-temporal
+
+// A row of `columns` values, or a stretch of one.  The hardware checks every 32 bits of an access against the row's end (loads behind it give
+// zeros, stores there are dropped), so no lane needs a branch, and all loads are in flight before the first is waited for.  Of an odd
+// number of bf16 columns the last one shares its 32 bits with what is behind the row, and is left to accesses of its own.
 template <bool BF16>
-__device__ __forceinline__ void load_piece(uint64_t row, uint32_t col, uint32_t width, float* v) {
-  constexpr int N = kPiece<BF16>, ES = BF16 ? 2 : 4;
-  if (col + N <= width) {
-    load_elems<BF16, N>(row + uint64_t(col) * ES, v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      v[j] = 0.0f;
-      if (col + j < width) load_elems<BF16, 1>(row + uint64_t(col + j) * ES, v + j);
-    }
+struct Row {
+  static constexpr int ES = BF16 ? 2 : 4, N = kPiece<BF16>;
+  __amdgpu_buffer_rsrc_t at;
+  uint32_t columns;
+
+  __device__ __forceinline__ Row(uint64_t base, uint32_t n) : at(buffer(base, n * ES)), columns(n) {}
+  __device__ __forceinline__ bool odd() const { return BF16 && columns % 2; }
+
+  // 16 bytes from column `col` on
+  __device__ __forceinline__ u32x4 get(uint32_t col) const {
+    return __builtin_amdgcn_raw_buffer_load_b128(at, int(col * ES), 0, 0);
   }
-}
+  template <bool STREAM = false>
+  __device__ __forceinline__ void put(uint32_t col, u32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(v, at, int(col * ES), 0, STREAM ? kStreaming : 0);
+  }
+  // the last one of an odd number
+  __device__ __forceinline__ uint32_t get_last() const {
+    return uint32_t(__builtin_amdgcn_raw_buffer_load_b16(at, int((columns - 1) * ES), 0, 0));
+  }
+  // ... into the piece from `col` on, if it is there (what is behind it is 0 already)
+  __device__ __forceinline__ void merge_last(uint32_t col, uint32_t last, u32x4& v) const {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) v[d] = col + 2 * d == columns - 1 ? last : v[d];
+  }
+  __device__ __forceinline__ void put_last(uint32_t col, u32x4 v) const {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      if (col + 2 * d == columns - 1) __builtin_amdgcn_raw_buffer_store_b16(uint16_t(v[d]), at, int((columns - 1) * ES), 0, 0);
+  }
+};
 
 template <bool BF16>
-__device__ __forceinline__ void store_piece(uint64_t row, uint32_t col, uint32_t width, const float* v) {
-  constexpr int N = kPiece<BF16>, ES = BF16 ? 2 : 4;
-  if (col + N <= width) {
-    store_elems<BF16, N>(row + uint64_t(col) * ES, v);
-  } else {
+__device__ __forceinline__ void widen(u32x4 raw, float* v) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (col + j < width) store_elems<BF16, 1>(row + uint64_t(col + j) * ES, v + j);
+  for (int j = 0; j < kPiece<BF16>; ++j) {
+    if constexpr (BF16) v[j] = j % 2 ? bf16_high(raw[j / 2]) : bf16_low(raw[j / 2]);
+    else v[j] = as_float(raw[j]);
   }
 }
+template <bool BF16>
+__device__ __forceinline__ u32x4 narrow(const float* v) {
+  u32x4 raw;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) raw[d] = BF16 ? bf16_pair(v[2 * d % kPiece<BF16>], v[(2 * d + 1) % kPiece<BF16>]) : as_bits(v[d]);
+  return raw;
+}
 
-// The sum over a wavefront, in every lane, in the same order everywhere.
+// Over a wavefront, in every lane, in the same order everywhere.
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v) {
 #pragma unroll
   for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
   return v;
 }
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
 
-// ... over TEAM wavefronts, which are the whole workgroup where they are more than one.  Calls that follow each other take
+// Over one number of each of COUNT (16 at most) wavefronts, `step` apart in LDS: every group of 16 lanes for itself, so that it takes one
+// register and not COUNT.
+template <int COUNT, typename T>
+__device__ __forceinline__ T across_sum(const T* lds, int step) {
+  const int k = threadIdx.x % 16;
+  T v = k < COUNT ? lds[k * step] : T(0);
+#pragma unroll
+  for (int d = 8; d; d /= 2) v += __shfl_xor(v, d);
+  return v;
+}
+template <int COUNT>
+__device__ __forceinline__ float across_max(const float* lds, int step) {
+  float v = lds[min(int(threadIdx.x % 16), COUNT - 1) * step];
+#pragma unroll
+  for (int d = 8; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+// The sum over a team of TEAM wavefronts, which are the whole workgroup where they are more than one.  Calls that follow each other take
 // `lds` (TEAM values each) in turn, so that one barrier is enough.
 template <int TEAM, typename T>
 __device__ __forceinline__ T team_sum(T v, T* lds) {
   v = wave_sum(v);
   if constexpr (TEAM > 1) {
-    const uint32_t wave = threadIdx.x / 64;
-    if (threadIdx.x % 64 == 0) lds[wave] = v;
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int k = 1; k < TEAM; ++k) v += lds[k];
+    v = across_sum<TEAM>(lds, 1);
   }
   return v;
 }
