@@ -50,73 +50,85 @@ struct Lesson {
   double taught;
 };
 
-// By one wavefront.
+// One wavefront's way to it: ask() begins all loads, learn() waits for them.
 template <bool BF16>
-__device__ __forceinline__ void learn(const DistillationArgs& a, uint32_t w, uint32_t row, uint64_t z, Lesson& out) {
-  constexpr int ES = BF16 ? 2 : 4, kEach = kTop / 64;
-  const uint32_t lane = threadIdx.x % 64;
-  // everything that needs no id is asked for at once, by all lanes (those without an entry: the last one's)
-  float t[kEach], v[kEach];
-  uint64_t asked[kEach], asked_label = ~uint64_t(0);
-  const uint64_t first = uint64_t(row) * a.top;
+struct Student {
+  static constexpr int ES = BF16 ? 2 : 4, kEach = kTop / 64;  // entries of a lane
+  float t[kEach], v[kEach], label_logit;
+  uint32_t id[kEach], label;
+
+  // What needs no id is asked for at once, by all lanes (those without an entry: the last one's).
+  __device__ __forceinline__ void ask(const DistillationArgs& a, uint32_t w, uint32_t row, uint64_t z) {
+    const uint32_t lane = threadIdx.x % 64;
+    uint64_t asked[kEach], asked_label = ~uint64_t(0);
+    const uint64_t first = uint64_t(row) * a.top;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    asked[i] = ~uint64_t(0);
-    if (uint32_t(i) * 64 >= a.top) continue;
-    const uint64_t k = first + min(i * 64 + lane, a.top - 1);
-    asked[i] = load_id(a.w.at[kDistIds][w], k, a.ids64);
-    if (a.teacher_bf16) load_elems<true, 1>(a.w.at[kDistTeacher][w] + k * 2, &t[i]);
-    else load_elems<false, 1>(a.w.at[kDistTeacher][w] + k * 4, &t[i]);
-  }
-  if (a.has_labels) asked_label = load_id(a.w.at[kDistLabels][w], row, a.ids64);
-  uint32_t id[kEach];
-  const uint32_t label = uniform(known(asked_label, a.vocab));
-  float most = -__builtin_inff(), label_logit = 0.0f;
-  bool bad = false, any = false;
+    for (int i = 0; i < kEach; ++i) {
+      asked[i] = ~uint64_t(0);
+      if (uint32_t(i) * 64 >= a.top) continue;
+      const uint64_t k = first + min(i * 64 + lane, a.top - 1);
+      asked[i] = load_id(a.w.at[kDistIds][w], k, a.ids64);
+      if (a.teacher_bf16) load_elems<true, 1>(a.w.at[kDistTeacher][w] + k * 2, &t[i]);
+      else load_elems<false, 1>(a.w.at[kDistTeacher][w] + k * 4, &t[i]);
+    }
+    if (a.has_labels) asked_label = load_id(a.w.at[kDistLabels][w], row, a.ids64);
+    label = uniform(known(asked_label, a.vocab));
+    load_elems<BF16, 1>(z + uint64_t(label != kNone ? label : 0) * ES, &label_logit);
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    id[i] = i * 64 + lane < a.top ? known(asked[i], a.vocab) : kNone;
-    if (uint32_t(i) * 64 >= a.top) continue;
-    load_elems<BF16, 1>(z + uint64_t(id[i] != kNone ? id[i] : 0) * ES, &v[i]);
-    if (id[i] == kNone) t[i] = -__builtin_inff();
-    most = fmaxf(most, t[i]);
-    bad = bad || t[i] != t[i];
-    any = any || t[i] > -__builtin_inff();
-  }
-  load_elems<BF16, 1>(z + uint64_t(label != kNone ? label : 0) * ES, &label_logit);
-  most = wave_max(most);
-  const bool has_teacher = a.soft > 0.0f && (__ballot(any) || __ballot(bad));
-  float p[kEach], total = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    p[i] = 0.0f;
-    if (uint32_t(i) * 64 >= a.top) continue;
-    if (has_teacher && t[i] != -__builtin_inff()) p[i] = exp2((t[i] - most) * a.warm_rate);
-    total += p[i];
-  }
-  total = wave_sum(total);
-  double part = 0.0;  // sum of P (ln P - z / T), with ln P but for the sum's logarithm
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const uint32_t k = i * 64 + lane;
-    if (uint32_t(i) * 64 >= a.top) continue;
-    p[i] /= total;
-    if (id[i] != kNone && p[i] != 0.0f && has_teacher) part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
-    if (k < a.top) {
-      out.id[k] = has_teacher ? id[i] : kNone;
-      out.logit[k] = v[i];
-      out.weight[k] = a.soft * float(a.inverse) * p[i];
+    for (int i = 0; i < kEach; ++i) {
+      id[i] = i * 64 + lane < a.top ? known(asked[i], a.vocab) : kNone;
+      if (uint32_t(i) * 64 >= a.top) continue;
+      load_elems<BF16, 1>(z + uint64_t(id[i] != kNone ? id[i] : 0) * ES, &v[i]);
     }
   }
-  part = wave_sum(part);
-  if (lane == 0) {
-    out.id[a.top] = label;
-    out.logit[a.top] = label_logit;
-    out.weight[a.top] = a.hard;
-    out.terms = (has_teacher ? 1u : 0u) | (label != kNone ? 2u : 0u);
-    out.taught = has_teacher ? part - ln(total) : 0.0;
+
+  __device__ __forceinline__ void learn(const DistillationArgs& a, Lesson& out) {
+    const uint32_t lane = threadIdx.x % 64;
+    float most = -__builtin_inff();
+    bool bad = false, any = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (uint32_t(i) * 64 >= a.top) continue;
+      if (id[i] == kNone) t[i] = -__builtin_inff();
+      most = fmaxf(most, t[i]);
+      bad = bad || t[i] != t[i];
+      any = any || t[i] > -__builtin_inff();
+    }
+    most = wave_max(most);
+    const bool has_teacher = a.soft > 0.0f && (__ballot(any) || __ballot(bad));
+    float p[kEach], total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      p[i] = 0.0f;
+      if (uint32_t(i) * 64 >= a.top) continue;
+      if (has_teacher && t[i] != -__builtin_inff()) p[i] = exp2((t[i] - most) * a.warm_rate);
+      total += p[i];
+    }
+    total = wave_sum(total);
+    double part = 0.0;  // sum of P (ln P - z / T), with ln P but for the sum's logarithm
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const uint32_t k = i * 64 + lane;
+      if (uint32_t(i) * 64 >= a.top) continue;
+      p[i] /= total;
+      if (id[i] != kNone && p[i] != 0.0f && has_teacher)
+        part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
+      if (k < a.top) {
+        out.id[k] = has_teacher ? id[i] : kNone;
+        out.logit[k] = v[i];
+        out.weight[k] = a.soft * float(a.inverse) * p[i];
+      }
+    }
+    part = wave_sum(part);
+    if (lane == 0) {
+      out.id[a.top] = label;
+      out.logit[a.top] = label_logit;
+      out.weight[a.top] = a.hard;
+      out.terms = (has_teacher ? 1u : 0u) | (label != kNone ? 2u : 0u);
+      out.taught = has_teacher ? part - ln(total) : 0.0;
+    }
   }
-}
+};
 
 // From which number exponents count: 2^(rate (z - base) - shift), where rate (z - base) - shift is one multiply-add.  Next to usual logits base
 // is 0 and shift the rounded product of rate and the largest logit; `rest` is what the rounding left, a factor of 2^rest that all
@@ -161,7 +173,10 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
   Lesson* const kept = reinterpret_cast<Lesson*>(ws + (3 * a.parts + 1) / 2 * 2);
   if constexpr (PHASE == kMeasure) {
     if (blockIdx.y == a.parts) {
-      if (wave == 0) learn<BF16>(a, w, row, z, *kept);
+      if (wave) return;
+      Student<BF16> student;
+      student.ask(a, w, row, z);
+      student.learn(a, *kept);
       return;
     }
   }
@@ -180,8 +195,10 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
   Origin from{};
 
   if (PHASE == kWhole && wave == kWaves) {
-    learn<BF16>(a, w, row, z, lesson);
+    Student<BF16> student;
+    student.ask(a, w, row, z);
     __syncthreads();  // the others' largest logits
+    student.learn(a, lesson);
     __syncthreads();  // their sums
   } else {
     // all loads first; what goes to LDS before what stays
@@ -344,6 +361,13 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
       const Row<BF16> to(out + uint64_t(lo) * ES, hi - lo);
       const float kw = a.scale * (KIND == kOne ? share + label_share : share), kc = a.scale * label_share;
       const bool none = !has_teacher && !has_label;  // zeros, whatever the logits are
+      if (none) {
+        from = Origin{};
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) x[i][j] = 0.0f;
+      }
       auto gradient = [&](float v) {  // of what is held
         if constexpr (KIND == kOne) return kw * v;
         else if constexpr (KIND == kSquare) return v * __builtin_fmaf(kc, v, kw);
@@ -356,7 +380,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
         if (uint32_t(i) * LANES * N >= count) continue;
         float g[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) g[j] = none ? 0.0f : gradient(x[i][j]);
+        for (int j = 0; j < N; ++j) g[j] = gradient(x[i][j]);
         to.template put<true>(col + uint32_t(i) * LANES * N, narrow<BF16>(g));
         __builtin_amdgcn_sched_barrier(0);
       }

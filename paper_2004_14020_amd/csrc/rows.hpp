@@ -63,35 +63,64 @@ __device__ __forceinline__ u32x4 narrow(const float* v) {
   return raw;
 }
 
-// Over a wavefront, in every lane, in the same order everywhere.
-template <typename T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
-  return v;
+// The value of the lane that a step of a reduction within 16 lanes pairs this one with: a neighbour, the pair beside, the other
+// half, ... (moves between lanes of a row of 16 go through no memory).
+template <int STEP, typename T>
+__device__ __forceinline__ T beside(T v) {
+  constexpr int kControl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;  // pairs, quads, mirrored half row, mirrored row
+  if constexpr (sizeof(T) == 8) {
+    const u32x2 x = __builtin_bit_cast(u32x2, v);
+    const u32x2 y = {uint32_t(__builtin_amdgcn_update_dpp(0, int(x[0]), kControl, 15, 15, false)),
+                     uint32_t(__builtin_amdgcn_update_dpp(0, int(x[1]), kControl, 15, 15, false))};
+    return __builtin_bit_cast(T, y);
+  } else {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kControl, 15, 15, false));
+  }
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+template <typename T>
+__device__ __forceinline__ T of_lane(T v, int lane) {
+  if constexpr (sizeof(T) == 8) {
+    const u32x2 x = __builtin_bit_cast(u32x2, v);
+    const u32x2 y = {uint32_t(__builtin_amdgcn_readlane(int(x[0]), lane)), uint32_t(__builtin_amdgcn_readlane(int(x[1]), lane))};
+    return __builtin_bit_cast(T, y);
+  } else {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  }
 }
 
-// Over one number of each of COUNT (16 at most) wavefronts, `step` apart in LDS: every group of 16 lanes for itself, so that it takes one
-// register and not COUNT.
+// Over every row of 16 lanes, in each of them; over the wavefront, in all lanes.  The same order everywhere.
+template <typename T>
+__device__ __forceinline__ T row_sum(T v) {
+  v += beside<0>(v);
+  v += beside<1>(v);
+  v += beside<2>(v);
+  return v + beside<3>(v);
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, beside<0>(v));
+  v = fmaxf(v, beside<1>(v));
+  v = fmaxf(v, beside<2>(v));
+  return fmaxf(v, beside<3>(v));
+}
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) {
+  v = row_sum(v);
+  return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = row_max(v);
+  return fmaxf(fmaxf(of_lane(v, 0), of_lane(v, 16)), fmaxf(of_lane(v, 32), of_lane(v, 48)));
+}
+
+// Over one number of each of COUNT (16 at most) wavefronts, `step` apart in LDS: every row of 16 lanes for itself.
 template <int COUNT, typename T>
 __device__ __forceinline__ T across_sum(const T* lds, int step) {
   const int k = threadIdx.x % 16;
-  T v = k < COUNT ? lds[k * step] : T(0);
-#pragma unroll
-  for (int d = 8; d; d /= 2) v += __shfl_xor(v, d);
-  return v;
+  return row_sum(k < COUNT ? lds[k * step] : T(0));
 }
 template <int COUNT>
 __device__ __forceinline__ float across_max(const float* lds, int step) {
-  float v = lds[min(int(threadIdx.x % 16), COUNT - 1) * step];
-#pragma unroll
-  for (int d = 8; d; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return row_max(lds[min(int(threadIdx.x % 16), COUNT - 1) * step]);
 }
 
 // The sum over a team of TEAM wavefronts, which are the whole workgroup where they are more than one.  Calls that follow each other take
