@@ -139,6 +139,7 @@ struct NormArgs {
   uint32_t width;
   uint64_t pitch;  // of all rows, elements
   float eps;
+  double inverse_width;  // made by the launch
   bool bf16, gain_bf16, residual, checkpoint;
 };
 hipError_t launch_norm(const NormArgs& args, const AllBuffers<kNormBuffers>& v, hipStream_t s);

@@ -11,6 +11,7 @@
 //
 // A row stays in the registers of a team of wavefronts, so that every matrix is read and written once.
 #include <algorithm>
+#include <type_traits>
 
 #include "layers.hpp"
 #include "rows.hpp"
@@ -47,42 +48,57 @@ __device__ __forceinline__ void store_piece(const Row<BF16>& row, uint32_t col, 
   if (row.odd()) row.put_last(col, raw);
 }
 
-// Gains are in the plan's type, which need not be that of the rows: the N of a piece of the rows.
+// The gains of a piece of a row; they are in the plan's type, which need not be that of the rows.
+template <int N>
+__device__ __forceinline__ void load_gains(uint64_t at, bool bf16, uint32_t width, uint32_t col, float* g) {
+  if (bf16) {
+    const Row<true> row(at, width);
+    u32x4 raw = row.get(col);  // (of fp32 rows, twice as many as are needed)
+    if (row.odd()) row.merge_last(col, row.get_last(), raw);
+    float all[8];
+    widen<true>(raw, all);
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = all[j];
+  } else {
+    const Row<false> row(at, width);
+#pragma unroll
+    for (int q = 0; q < N; q += 4) widen<false>(row.get(col + q), g + q);
+  }
+}
+
+// Those of all pieces of a lane: kept for all rows where that takes few registers, else loaded (from the caches) when they are needed.
 template <bool BF16, int V, int LANES>
 struct Gains {
   static constexpr int N = kPiece<BF16>;
-  u32x4 raw[V][2];
-  uint32_t last;
+  static constexpr bool kKept = V * N <= 16;
+  uint64_t at;
+  bool bf16;
+  uint32_t width, lane;
+  float kept[kKept ? V : 1][N];
 
-  // (bf16 gains of fp32 rows: the 16 bytes hold twice as many as are needed, and what is behind the row is not read)
-  __device__ __forceinline__ void load(uint64_t at, bool bf16, uint32_t width, uint32_t lane) {
-    if (bf16) {
-      const Row<true> row(at, width);
+  __device__ __forceinline__ Gains(uint64_t from, bool is_bf16, uint32_t columns, uint32_t l)
+      : at(from), bf16(is_bf16), width(columns), lane(l) {
+    if constexpr (kKept) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) raw[v][0] = row.get((v * LANES + lane) * N);
-      if (row.odd()) last = row.get_last();
-    } else {
-      const Row<false> row(at, width);
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int q = 0; q < N / 4; ++q) raw[v][q] = row.get((v * LANES + lane) * N + 4 * q);
+      for (int v = 0; v < V; ++v) load_gains<N>(at, bf16, width, (v * LANES + lane) * N, kept[v]);
     }
   }
-  __device__ __forceinline__ void get(bool bf16, uint32_t width, uint32_t lane, int v, float* g) const {
-    if (bf16) {
-      u32x4 r = raw[v][0];
-      if (width % 2) Row<true>(0, width).merge_last((v * LANES + lane) * N, last, r);
-      float all[8];
-      widen<true>(r, all);
+  __device__ __forceinline__ void get(int v, float* g) const {
+    if constexpr (kKept) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) g[j] = all[j];
+      for (int j = 0; j < N; ++j) g[j] = kept[v][j];
     } else {
-#pragma unroll
-      for (int q = 0; q < N / 4; ++q) widen<false>(raw[v][q], g + 4 * q);
+      load_gains<N>(at, bf16, width, (v * LANES + lane) * N, g);
     }
   }
 };
+
+// 1 / sqrt(sum / width + eps): the hardware's 64-bit estimate and one step of Newton's method, right to 2^-50 and then rounded.
+__device__ __forceinline__ float rstd_of(double sum, double inverse_width, float eps) {
+  const double m = __builtin_fma(sum, inverse_width, double(eps)), y = __builtin_amdgcn_rsq(m);
+  const double r = __builtin_fma(0.5 * y, __builtin_fma(-m * y, y, 1.0), y);
+  return float(m == __builtin_inf() ? 0.0 : r);
+}
 
 constexpr uint32_t kGridGroups = 1u << 20;  // workgroups along x: a grid has less than 2^32 lanes in a direction
 
@@ -102,8 +118,7 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
   P x, r;
   x.load(rx, lane);
   if (a.residual) r.load(rr, lane);
-  Gains<BF16, V, LANES> gain;
-  gain.load(a.w.at[kNormGain][w], a.gain_bf16, a.width, lane);
+  const Gains<BF16, V, LANES> gain(a.w.at[kNormGain][w], a.gain_bf16, a.width, lane);
   x.finish(rx, lane);
   float h[V][N];
 #pragma unroll
@@ -129,13 +144,13 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) ss = __builtin_fma(double(h[v][j]), double(h[v][j]), ss);
   ss = team_sum<TEAM>(ss, lds);
-  const float rstd = float(1.0 / sqrt(ss / double(a.width) + double(a.eps)));
+  const float rstd = rstd_of(ss, a.inverse_width, a.eps);
   if (lane == 0) reinterpret_cast<CARAMEL_GLOBAL float*>(a.w.at[kNormRstd][w])[row] = rstd;
   const Row<BF16> ry(a.w.at[kNormY][w] + at, a.width);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     float g[N];
-    gain.get(a.gain_bf16, a.width, lane, v, g);
+    gain.get(v, g);
 #pragma unroll
     for (int j = 0; j < N; ++j) h[v][j] = (h[v][j] * rstd) * g[j];
     store_piece<BF16, false>(ry, P::column(lane, v), h[v]);
@@ -164,8 +179,8 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
   constexpr int LANES = 64 * TEAM;
   const uint32_t lane = threadIdx.x % LANES, team = uniform(threadIdx.x / 64) / TEAM;
   using P = Pieces<BF16, V, LANES>;
-  Gains<BF16, V, LANES> gain;
-  gain.load(a.w.at[kNormGradGain][w], a.gain_bf16, a.width, lane);
+  const Gains<BF16, V, LANES> gain(a.w.at[kNormGradGain][w], a.gain_bf16, a.width, lane);
+  constexpr bool kLate = TEAM == 16 && V * N >= 32;  // dsum is loaded when it is added, for the registers
   float sum[V][N] = {};
   uint32_t turn = 0;
   for (uint32_t row = first + team; row < last; row += kTeams) {
@@ -175,7 +190,7 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
     P x, y, d;
     x.load(rx, lane);
     y.load(ry, lane);
-    if (a.dsum) d.load(rd, lane);
+    if (a.dsum && !kLate) d.load(rd, lane);
     const float r = reinterpret_cast<const CARAMEL_GLOBAL float*>(a.w.at[kNormGradRstd][w])[row];
     x.finish(rx, lane);
     y.finish(ry, lane);
@@ -185,7 +200,7 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
       float n[N], u[N], g[N];
       widen<BF16>(x.raw[v], n);
       widen<BF16>(y.raw[v], u);
-      gain.get(a.gain_bf16, a.width, lane, v, g);
+      gain.get(v, g);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         n[j] *= r;
@@ -195,14 +210,23 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
     }
     c = team_sum<TEAM>(c, lds[turn]) / float(a.width);
     turn ^= 1;
-    if (a.dsum) d.finish(rd, lane);
+    if (a.dsum && !kLate) d.finish(rd, lane);
+    // (left to itself, the compiler keeps what it has widened, in twice the registers of what it came from)
+    if constexpr (BF16) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) asm volatile("" : "+v"(x.raw[v]), "+v"(y.raw[v]));
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float n[N], u[N], g[N], o[N];
       widen<BF16>(x.raw[v], n);
       widen<BF16>(y.raw[v], u);
-      gain.get(a.gain_bf16, a.width, lane, v, g);
+      gain.get(v, g);
       if (a.dsum) {
+        if constexpr (kLate) {
+          d.raw[v] = rd.get(P::column(lane, v));
+          if (rd.odd()) rd.merge_last(P::column(lane, v), rd.get_last(), d.raw[v]);
+        }
         widen<BF16>(d.raw[v], o);
       } else {
 #pragma unroll
@@ -238,20 +262,30 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
   }
 }
 
-// 64 columns to a workgroup; its four wavefronts share the parts, and their sums are added in order.
-__global__ void __launch_bounds__(256) k_norm_join(NormGradientArgs a, uint32_t span, uint64_t stride) {
-  __shared__ float lds[4][64];
+// 64 columns to a workgroup; its sixteen wavefronts share the parts, and their sums are added in order.
+__global__ void __launch_bounds__(1024) k_norm_join(NormGradientArgs a, uint32_t span, uint64_t stride) {
+  __shared__ float lds[16][64];
   const uint32_t w = blockIdx.y, parts = (a.w.tokens[w] + span - 1) / span, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const uint32_t col = blockIdx.x * 64 + lane;
-  const uint32_t each = (parts + 3) / 4, first = wave * each, last = min(first + each, parts);
+  const uint32_t each = (parts + 15) / 16, first = wave * each, last = min(first + each, parts);
   const CARAMEL_GLOBAL float* const in = reinterpret_cast<const CARAMEL_GLOBAL float*>(reinterpret_cast<uint64_t>(a.ws)) + w * stride;
   float sum = 0.0f;
-  if (col < a.width)
-    for (uint32_t k = first; k < last; ++k) sum += in[uint64_t(k) * a.width + col];
+  if (col < a.width) {
+    uint32_t k = first;
+    for (; k + 8 <= last; k += 8) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = in[uint64_t(k + i) * a.width + col];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += v[i];
+    }
+    for (; k < last; ++k) sum += in[uint64_t(k) * a.width + col];
+  }
   lds[wave][lane] = sum;
   __syncthreads();
   if (wave || col >= a.width) return;
-  sum = ((lds[0][lane] + lds[1][lane]) + lds[2][lane]) + lds[3][lane];
+#pragma unroll
+  for (int k = 1; k < 16; ++k) sum += lds[k][lane];
   const uint64_t out = a.w.at[kNormGradOut][w] + uint64_t(col) * (a.gain_bf16 ? 2 : 4);
   float old = 0.0f;
   if (a.gain_bf16) {
@@ -265,36 +299,61 @@ __global__ void __launch_bounds__(256) k_norm_join(NormGradientArgs a, uint32_t 
   }
 }
 
-// The fewest wavefronts and pieces that hold a row of `width` columns: launch(pieces, wavefronts) as compile-time numbers.
 template <int V, int TEAM>
 struct Shape {
   static constexpr int kV = V, kTeam = TEAM;
 };
-template <typename LAUNCH>
-void by_shape(uint32_t width, int piece, LAUNCH&& launch) {
-  const uint32_t wave = 64 * uint32_t(piece);
-  if (width <= wave) launch(Shape<1, 1>{});
-  else if (width <= 2 * wave) launch(Shape<2, 1>{});
-  else if (width <= 4 * wave) launch(Shape<4, 1>{});
-  else if (width <= 8 * wave) launch(Shape<2, 4>{});
-  else if (width <= 16 * wave) launch(Shape<4, 4>{});
-  else if (width <= 64 * wave) launch(Shape<4, 16>{});
-  else launch(Shape<8, 16>{});
+
+// Wavefronts and pieces that hold a row of `width` columns: launch(pieces, wavefronts) as compile-time numbers.  As few wavefronts as can do, but no
+// more than four pieces a lane, for the registers (8 x 2048 x 2048 bf16 48.9 us and 52.3 with eight; the gradient 63 and 119;
+// two a lane and four wavefronts 54.8 and 61.8).
+template <int PIECE, typename LAUNCH>
+void row_shape(uint32_t width, LAUNCH&& launch) {
+  constexpr uint32_t kWave = 64 * PIECE;
+  if (width <= kWave) launch(Shape<1, 1>{});
+  else if (width <= 2 * kWave) launch(Shape<2, 1>{});
+  else if (width <= 4 * kWave) launch(Shape<4, 1>{});
+  else if (width <= 4 * 2 * kWave) launch(Shape<2, 4>{});
+  else if (width <= 4 * 4 * kWave) launch(Shape<4, 4>{});
+  else if (width <= 16 * 2 * kWave) launch(Shape<2, 16>{});
+  else if (width <= 16 * 4 * kWave) launch(Shape<4, 16>{});
+  else if constexpr (16 * 4 * kWave < kNormWidth) launch(Shape<8, 16>{});
+}
+// The gradient holds more: bf16 rows whose four pieces would leave two wavefronts per SIMD take three (3 x 1500 x 4104 52 us, with four 70) or
+// sixteen wavefronts (8 x 1000 x 8192 119, with four 126).
+template <int PIECE, typename LAUNCH>
+void gradient_shape(uint32_t width, LAUNCH&& launch) {
+  constexpr uint32_t kWave = 64 * PIECE;
+  if constexpr (PIECE == 8) {
+    if (width <= kWave) launch(Shape<1, 1>{});
+    else if (width <= 2 * kWave) launch(Shape<2, 1>{});
+    else if (width <= 4 * kWave) launch(Shape<4, 1>{});
+    else if (width <= 4 * 2 * kWave) launch(Shape<2, 4>{});
+    else if (width <= 4 * 3 * kWave) launch(Shape<3, 4>{});
+    else if (width <= 16 * kWave) launch(Shape<1, 16>{});
+    else if (width <= 16 * 2 * kWave) launch(Shape<2, 16>{});
+    else launch(Shape<4, 16>{});
+  } else {
+    row_shape<PIECE>(width, launch);
+  }
 }
 
 }  // namespace
 
-hipError_t launch_norm(const NormArgs& args, const AllBuffers<kNormBuffers>& v, hipStream_t s) {
-  if (args.max_tokens == 0) return hipSuccess;
+hipError_t launch_norm(const NormArgs& all, const AllBuffers<kNormBuffers>& v, hipStream_t s) {
+  if (all.max_tokens == 0) return hipSuccess;
+  NormArgs args = all;
+  args.inverse_width = 1.0 / double(all.width);
   const hipError_t e = in_groups(args, v, [&](const NormArgs& a, uint32_t) {
-    by_shape(a.width, a.bf16 ? 8 : 4, [&](auto shape) {
+    auto rows = [&](auto bf16, auto shape) {
       constexpr int V = decltype(shape)::kV, TEAM = decltype(shape)::kTeam;
       constexpr uint32_t kRows = (TEAM <= 4 ? 4 : 16) / TEAM;
       const uint32_t groups = (a.max_tokens + kRows - 1) / kRows;
       const dim3 grid(std::min(groups, kGridGroups), a.world, (groups + kGridGroups - 1) / kGridGroups), block(TEAM <= 4 ? 256 : 1024);
-      if (a.bf16) hipLaunchKernelGGL((k_norm<true, V, TEAM>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((k_norm<false, V, TEAM>), grid, block, 0, s, a);
-    });
+      hipLaunchKernelGGL((k_norm<decltype(bf16)::value, V, TEAM>), grid, block, 0, s, a);
+    };
+    if (a.bf16) row_shape<kPiece<true>>(a.width, [&](auto shape) { rows(std::true_type{}, shape); });
+    else row_shape<kPiece<false>>(a.width, [&](auto shape) { rows(std::false_type{}, shape); });
     return hipGetLastError();
   });
   if (e != hipSuccess || !args.checkpoint) return e;
@@ -323,16 +382,17 @@ hipError_t launch_norm_gradient(const NormGradientArgs& args, const AllBuffers<k
   return in_groups(args, v, [&](NormGradientArgs a, uint32_t g) {
     a.ws += g * stride * 4;
     if (a.max_tokens) {
-      by_shape(a.width, a.bf16 ? 8 : 4, [&](auto shape) {
+      auto rows = [&](auto bf16, auto shape) {
         constexpr int V = decltype(shape)::kV, TEAM = decltype(shape)::kTeam;
         const dim3 grid(parts, a.world), block(TEAM <= 4 ? 256 : 1024);
-        if (a.bf16) hipLaunchKernelGGL((k_norm_gradient<true, V, TEAM>), grid, block, 0, s, a, span, stride);
-        else hipLaunchKernelGGL((k_norm_gradient<false, V, TEAM>), grid, block, 0, s, a, span, stride);
-      });
+        hipLaunchKernelGGL((k_norm_gradient<decltype(bf16)::value, V, TEAM>), grid, block, 0, s, a, span, stride);
+      };
+      if (a.bf16) gradient_shape<kPiece<true>>(a.width, [&](auto shape) { rows(std::true_type{}, shape); });
+      else gradient_shape<kPiece<false>>(a.width, [&](auto shape) { rows(std::false_type{}, shape); });
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(k_norm_join, dim3((a.width + 63) / 64, a.world), dim3(256), 0, s, a, span, stride);
+    hipLaunchKernelGGL(k_norm_join, dim3((a.width + 63) / 64, a.world), dim3(1024), 0, s, a, span, stride);
     return hipGetLastError();
   });
 }
