@@ -4,15 +4,16 @@
 //   gradient, with e_t = dL/ds_t = ds_t + a_(t+1) e_(t+1):   du_t = b_t e_t,   dgate_t = a_t b_t e_t (s_(t-1) - u_t)
 //
 // A step is an affine map, and two of them in a row are one: (A, B) after (A', B') is (A A', A B' + B).  A workgroup takes a
-// span of a worker's tokens for 64 C channels and walks it in tiles; in a tile every wavefront maps its own K tokens, all
+// span of a worker's tokens for 64 C channels and walks it in tiles; in a tile every wavefront maps its own tokens, all
 // exchange what their maps are, and each starts its tokens from the state that the maps before it give.  So every value is read
-// and written once.  Where workers and channels are too few for the GPU, the tokens are cut into parts, and a launch
-// before this one leaves every part's map; it starts at the last sequence that begins in the part and does nothing where the
-// part ends with its sequence.  The gradient walks the same way from the last token to the first.
+// and written once.  Where workers and channels are too few for the GPU, the tokens are cut into parts, at the start of a
+// sequence if one is near; where a sequence goes on behind a part, a launch before this one leaves the map of its tokens in the part.
+// The gradient walks the same way from the last token to the first.
 //
 // A sequence's first token (its last one, in the gradient) takes nothing from what was before: where it stands, the map is replaced
 // and not multiplied by zero, so that an infinity or NaN ends with its sequence.  States are fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "layers.hpp"
 #include "vec.hpp"
@@ -22,27 +23,29 @@ namespace {
 
 constexpr int kSteps = 8;            // tokens of a wavefront in a tile
 constexpr int kWalkWaves = 8;        // wavefronts of a workgroup
+constexpr int kAhead = 16;           // rows of gates that a wavefront asks for at once where it only maps
 constexpr uint32_t kTile = kSteps * kWalkWaves;
 constexpr uint32_t kLanes = 64 * kWalkWaves;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
-// C neighbouring channels, as they lie in memory, and widened
+// C neighbouring channels, as they lie in memory, and widened.  A row's address is the same for all lanes, so it stays in scalar registers;
+// `at` is a lane's distance from it in bytes.
 template <bool BF16, int C>
 struct Raw {
   uint32_t w[BF16 && C == 2 ? 1 : C];
 };
 template <bool BF16, int C>
-__device__ __forceinline__ Raw<BF16, C> load_raw(uint64_t at) {
+__device__ __forceinline__ Raw<BF16, C> load_raw(uint64_t row, uint32_t at) {
   Raw<BF16, C> r;
   if constexpr (C == 1) {
-    if constexpr (BF16) r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL uint16_t*>(at);
-    else r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL uint32_t*>(at);
+    if constexpr (BF16) r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL uint16_t*>(row + at);
+    else r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL uint32_t*>(row + at);
   } else if constexpr (BF16) {
     typedef uint32_t word __attribute__((aligned(2)));
-    r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL word*>(at);
+    r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL word*>(row + at);
   } else {
     typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(4)));
-    const pair p = *reinterpret_cast<const CARAMEL_GLOBAL pair*>(at);
+    const pair p = *reinterpret_cast<const CARAMEL_GLOBAL pair*>(row + at);
     r.w[0] = p[0];
     r.w[1] = p[1];
   }
@@ -54,16 +57,16 @@ __device__ __forceinline__ float widen(const Raw<BF16, C>& r, int c) {
   else return c ? bf16_high(r.w[0]) : bf16_low(r.w[0]);
 }
 template <bool BF16, int C>
-__device__ __forceinline__ void store_channels(uint64_t at, const float* v) {
+__device__ __forceinline__ void store_channels(uint64_t row, uint32_t at, const float* v) {
   if constexpr (C == 1) {
-    store_elems<BF16, 1>(at, v);
+    store_elems<BF16, 1>(row + at, v);
   } else if constexpr (BF16) {
     typedef uint32_t word __attribute__((aligned(2)));
-    *reinterpret_cast<CARAMEL_GLOBAL word*>(at) = bf16_pair(v[0], v[1]);
+    *reinterpret_cast<CARAMEL_GLOBAL word*>(row + at) = bf16_pair(v[0], v[1]);
   } else {
     typedef float pair __attribute__((ext_vector_type(2), aligned(4)));
     const pair p = {v[0], v[1]};
-    *reinterpret_cast<CARAMEL_GLOBAL pair*>(at) = p;
+    *reinterpret_cast<CARAMEL_GLOBAL pair*>(row + at) = p;
   }
 }
 
@@ -173,159 +176,183 @@ __device__ __forceinline__ Marks marks(const Starts& s, const Window& v, uint32_
 
 // ---- walking --------------------------------------------------------------------------------
 
-// The buffers of one worker, at the lane's first channel.
-struct Columns {
-  uint64_t gate, input, states, dstates, dgate, dinput;  // rows
-  uint64_t begin, end;  // fp32 rows of the sequences: what their walk starts from, and what it leaves (0: not there)
-  uint64_t before;      // gradient: the states before the sequences
-};
-
+// A workgroup's place: worker w, part, channels.  The last lanes take the last C channels once more: equal values go to equal places.
 template <bool BF16, int C, bool BACK>
 struct Walk {
   static constexpr int ES = BF16 ? 2 : 4;
-  struct Rows {
-    Raw<BF16, C> gate[kSteps], input[kSteps];
-    Raw<BF16, C> prior[BACK ? kSteps : 1], ds[BACK ? kSteps : 1];
-  };
+  typedef Raw<BF16, C> raw;
+  const RecurrenceArgs& r;
+  uint32_t w, at, at32;  // a lane's distance in bytes from the rows of dtype, and from fp32 rows
 
-  // The rows of tokens t0 to t0 + kSteps - 1; of those from `stop` on, the last one before it.  (MAPS: only what the maps are made of.)
-  template <bool MAPS>
-  static __device__ __forceinline__ void load(const RecurrenceArgs& r, const Columns& q, uint32_t t0, uint32_t stop, Rows& x) {
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const uint64_t t = min(t0 + k, stop - 1);
-      x.gate[k] = load_raw<BF16, C>(q.gate + t * r.pitch * ES);
-      if constexpr (!BACK || !MAPS) x.input[k] = load_raw<BF16, C>(q.input + t * r.pitch * ES);
-      if constexpr (BACK) {
-        x.ds[k] = load_raw<BF16, C>(q.dstates + t * r.states_pitch * ES);
-        if constexpr (!MAPS) x.prior[k] = load_raw<BF16, C>(q.states + (t ? t - 1 : 0) * r.states_pitch * ES);
-      }
-    }
+  __device__ __forceinline__ Walk(const RecurrenceArgs& args) : r(args), w(blockIdx.z) {
+    const uint32_t channel = min((blockIdx.x * 64 + threadIdx.x % 64) * C, r.channels - C);
+    at = channel * ES;
+    at32 = channel * 4;
+  }
+  __device__ __forceinline__ uint64_t row(int which, uint64_t t, uint64_t pitch) const { return r.w.at[which][w] + t * pitch * ES; }
+  __device__ __forceinline__ raw load(int which, uint64_t t, uint64_t pitch) const {
+    return load_raw<BF16, C>(row(which, t, pitch), at);
   }
 
-  // What a sequence's walk starts from.
-  static __device__ __forceinline__ void begin(const RecurrenceArgs& r, uint64_t at, uint32_t sequence, float* v) {
+  // fp32 rows of the sequences (zeros, or nothing, where the call has none)
+  __device__ __forceinline__ void get(int which, uint32_t sequence, float* v) const {
 #pragma unroll
     for (int c = 0; c < C; ++c) v[c] = 0.0f;
-    if (at) {
-      const CARAMEL_GLOBAL float* const row =
-          reinterpret_cast<const CARAMEL_GLOBAL float*>(at + uint64_t(sequence) * r.channels * 4);
+    if (!r.w.at[which][w]) return;
+    const raw32 x = load_raw<false, C>(r.w.at[which][w] + uint64_t(sequence) * r.channels * 4, at32);
 #pragma unroll
-      for (int c = 0; c < C; ++c) v[c] = row[c];
-    }
+    for (int c = 0; c < C; ++c) v[c] = as_float(x.w[c]);
   }
-  static __device__ __forceinline__ void leave(const RecurrenceArgs& r, uint64_t at, uint32_t sequence, const float* v) {
-    if (!at) return;
-    CARAMEL_GLOBAL float* const row = reinterpret_cast<CARAMEL_GLOBAL float*>(at + uint64_t(sequence) * r.channels * 4);
-#pragma unroll
-    for (int c = 0; c < C; ++c) row[c] = v[c];
+  __device__ __forceinline__ void put(int which, uint32_t sequence, const float* v) const {
+    if (r.w.at[which][w]) store_channels<false, C>(r.w.at[which][w] + uint64_t(sequence) * r.channels * 4, at32, v);
+  }
+  typedef Raw<false, C> raw32;
+  // what a sequence's walk starts from, and where it leaves what it ends with
+  static constexpr int kBegin = BACK ? kRecDafter : kRecBefore, kEnd = BACK ? kRecDbefore : kRecAfter;
+
+  // a part's map in the workspace: two fp32 rows
+  __device__ __forceinline__ uint64_t map_of(uint32_t parts, uint32_t part) const {
+    return reinterpret_cast<uint64_t>(r.ws) + (uint64_t(w) * parts + part) * r.channels * 8;
   }
 };
 
-// The tokens of a worker that belong to some sequence
-struct Range {
-  uint32_t lo, hi;
-};
-
-template <bool BF16, int C>
-__device__ __forceinline__ Columns columns(const RecurrenceArgs& r, uint32_t w, uint32_t ch, bool back) {
-  constexpr int ES = BF16 ? 2 : 4;
-  Columns q{};
-  auto at = [&](int which, uint32_t es) { return r.w.at[which][w] ? r.w.at[which][w] + uint64_t(ch) * es : 0; };
-  q.gate = at(kRecGate, ES);
-  q.input = at(kRecInput, ES);
-  q.states = at(kRecStates, ES);
-  q.before = at(kRecBefore, 4);
-  if (back) {
-    q.dstates = at(kRecDstates, ES);
-    q.dgate = at(kRecDgate, ES);
-    q.dinput = at(kRecDinput, ES);
-    q.begin = at(kRecDafter, 4);
-    q.end = at(kRecDbefore, 4);
-  } else {
-    q.begin = q.before;
-    q.end = at(kRecAfter, 4);
-  }
-  return q;
+// Where a part begins: at a multiple of `span`, or at the sequence that starts next if that is less than half a part on.
+__device__ __forceinline__ uint32_t border(const Starts& s, uint32_t part, uint32_t span) {
+  const uint32_t x = min(part * span, s.tokens), next = uniform(s.get(s.lower(x)));
+  return part && next >= x && next - x < span / 2 ? min(next, s.tokens) : x;
 }
 
-// MAPS: the parts' maps, left in the workspace; else: the walk itself.  Parts are `span` tokens, a multiple of the tile.
-// blockIdx: x channels, y part, z worker.
-template <bool BF16, int C, bool BACK, bool MAPS>
-__global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32_t span, uint32_t parts) {
-  using W = Walk<BF16, C, BACK>;
-  constexpr int ES = BF16 ? 2 : 4;
-  __shared__ float maps[2][kWalkWaves][2][C][64];
-  __shared__ uint32_t cuts[2][kWalkWaves];
-  const uint32_t w = blockIdx.z, n = r.w.tokens[w], part = blockIdx.y;
-  const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
-  uint32_t lo = part * span;
-  if (lo >= n) return;
-  uint32_t hi = min(lo + span, n);
-  const Starts starts{r.w.at[kRecStarts][w], r.w.more[w], n, r.starts64};
-  // the last lanes take the last C channels once more: equal values go to equal places
-  const uint32_t ch = min((blockIdx.x * 64 + lane) * C, r.channels - C);
-  const Columns q = columns<BF16, C>(r, w, ch, BACK);
-  const uint32_t none_before = uniform(starts.get(0)), none_behind = uniform(starts.get(starts.sequences));
+// The sequence that goes on across the border in front of token x: its number, its first token and the one behind its last.
+struct Crossing {
+  bool there;
+  uint32_t sequence, first, behind;
+};
+__device__ __forceinline__ Crossing crossing(const Starts& s, uint32_t x) {
+  const uint32_t next = s.lower(x);  // the first start from x on
+  Crossing c;
+  c.behind = uniform(s.get(next));
+  c.there = next > 0 && next <= s.sequences && c.behind != x;
+  c.sequence = next - 1;
+  c.first = c.there ? uniform(s.get(next - 1)) : 0;
+  return c;
+}
 
-  // the sequence that goes on across the part's border, from the side the walk comes from
-  const uint32_t border = BACK ? hi : lo;
-  uint32_t from = 0, to = 0;  // parts whose maps lead up to this one
-  {
-    const uint32_t next = starts.lower(border);                      // the first start at or behind the border
-    const bool goes_on = uniform(starts.get(next)) != border && border > none_before && border < none_behind && next > 0;
-    if constexpr (MAPS) {
-      // the other border: what leaves the part there
-      const uint32_t out = BACK ? lo : hi;
-      const uint32_t after = starts.lower(out);
-      const bool leaves = uniform(starts.get(after)) != out && out > none_before && out < none_behind && after > 0;
-      if (!leaves) return;
-      const uint32_t cut = uniform(starts.get(BACK ? after : after - 1));
-      if constexpr (BACK) hi = min(hi, max(cut, lo + 1));
-      else lo = max(lo, min(cut, hi - 1) / kTile * kTile);
-    } else if (goes_on) {
-      const uint32_t cut = uniform(starts.get(BACK ? next : next - 1));
-      if constexpr (BACK) {
-        from = part + 1;
-        to = min((max(cut, 1u) - 1) / span + 1, parts);
-      } else {
-        from = cut / span;
-        to = part;
+// The maps of the parts out of which a sequence goes on: of its tokens there, all of which are inside.  Every wavefront has a stretch of them.
+// blockIdx: x channels, y part, z worker.
+template <bool BF16, int C, bool BACK>
+__global__ void __launch_bounds__(kLanes) k_walk_maps(RecurrenceArgs r, uint32_t span, uint32_t parts) {
+  __shared__ float maps[kWalkWaves][2][C][64];
+  const Walk<BF16, C, BACK> walk(r);
+  const uint32_t n = r.w.tokens[walk.w], part = blockIdx.y, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+  if (part * span >= n) return;
+  const Starts starts{r.w.at[kRecStarts][walk.w], r.w.more[walk.w], n, r.starts64};
+  uint32_t lo = border(starts, part, span), hi = part + 1 < parts ? border(starts, part + 1, span) : n;
+  if (lo >= hi) return;
+  const Crossing x = crossing(starts, BACK ? lo : hi);
+  if (!x.there) return;
+  const bool begins = BACK ? x.behind <= hi : x.first >= lo;  // inside the part
+  if constexpr (BACK) hi = max(min(hi, x.behind), lo + 1);
+  else lo = min(max(lo, x.first), hi - 1);
+  // stretches in the order of the walk
+  const uint32_t each = (hi - lo + kWalkWaves - 1) / kWalkWaves, place = BACK ? kWalkWaves - 1 - wave : wave;
+  const uint32_t from = min(lo + place * each, hi), to = min(from + each, hi);
+  float A[C], B[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) A[c] = 1.0f, B[c] = 0.0f;
+  if (begins && wave == 0) walk.get(walk.kBegin, x.sequence, B);
+  auto steps = [&](uint32_t done, auto count) {
+    constexpr int N = decltype(count)::value;
+    typename Walk<BF16, C, BACK>::raw gate[N], add[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const uint32_t t = BACK ? to - 1 - done - k : from + done + k;
+      gate[k] = walk.load(kRecGate, t, r.pitch);
+      add[k] = BACK ? walk.load(kRecDstates, t, r.states_pitch) : walk.load(kRecInput, t, r.pitch);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float a, b;
+        gates<BF16>(widen<BF16, C>(gate[k], c), &a, &b);
+        const float v = widen<BF16, C>(add[k], c);
+        B[c] = BACK ? a * (v + B[c]) : __builtin_fmaf(a, B[c], b * v);
+        A[c] *= a;
+      }
+    }
+  };
+  uint32_t done = 0;
+  for (; done + kAhead <= to - from; done += kAhead) steps(done, std::integral_constant<int, kAhead>{});
+  for (; done < to - from; ++done) steps(done, std::integral_constant<int, 1>{});
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    maps[wave][0][c][lane] = A[c];
+    maps[wave][1][c][lane] = B[c];
+  }
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int v = 1; v < kWalkWaves; ++v) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      A[c] *= maps[v][0][c][lane];
+      B[c] = __builtin_fmaf(maps[v][0][c][lane], B[c], maps[v][1][c][lane]);
+    }
+  }
+  store_channels<false, C>(walk.map_of(parts, part), walk.at32, A);
+  store_channels<false, C>(walk.map_of(parts, part) + uint64_t(r.channels) * 4, walk.at32, B);
+}
+
+// The walk itself.
+template <bool BF16, int C, bool BACK>
+__global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32_t span, uint32_t parts) {
+  typedef float Map __attribute__((ext_vector_type(2 * C)));
+  __shared__ Map maps[2][kWalkWaves][64];
+  __shared__ uint32_t cuts[2][kWalkWaves];
+  const Walk<BF16, C, BACK> walk(r);
+  const uint32_t n = r.w.tokens[walk.w], part = blockIdx.y, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+  if (part * span >= n) return;
+  const Starts starts{r.w.at[kRecStarts][walk.w], r.w.more[walk.w], n, r.starts64};
+  const uint32_t lo = border(starts, part, span), hi = part + 1 < parts ? border(starts, part + 1, span) : n;
+  // sequences without tokens leave what they start from
+  if (r.w.at[walk.kEnd][walk.w]) {
+    for (uint32_t s0 = (part * kWalkWaves + wave) * 64; s0 < starts.sequences; s0 += parts * kWalkWaves * 64) {
+      uint64_t empty = __ballot(s0 + lane < starts.sequences && starts.get(s0 + lane) >= starts.get(s0 + lane + 1));
+      while (empty) {
+        const uint32_t one = s0 + uint32_t(__builtin_ctzll(empty));
+        float v[C];
+        walk.get(walk.kBegin, one, v);
+        walk.put(walk.kEnd, one, v);
+        empty &= empty - 1;
       }
     }
   }
+  if (lo >= hi) return;
+  const uint32_t none_before = uniform(starts.get(0)), none_behind = uniform(starts.get(starts.sequences));
+
+  // the maps that lead up to this part: of the sequence that comes in, from the part where it begins
   float state[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) state[c] = 0.0f;
-  if constexpr (!MAPS) {
-    const uint64_t stride = uint64_t(r.channels) * 2 * 4;  // bytes of a part's maps
-    const uint64_t mine = reinterpret_cast<uint64_t>(r.ws) + uint64_t(w) * parts * stride + uint64_t(ch) * 4;
-    for (uint32_t k = from; k < to; ++k) {
-      const uint64_t at = mine + uint64_t(BACK ? to - 1 - (k - from) : k) * stride;
-      const CARAMEL_GLOBAL float* const A = reinterpret_cast<const CARAMEL_GLOBAL float*>(at);
-      const CARAMEL_GLOBAL float* const B = reinterpret_cast<const CARAMEL_GLOBAL float*>(at + uint64_t(r.channels) * 4);
-#pragma unroll
-      for (int c = 0; c < C; ++c) state[c] = k == from ? B[c] : __builtin_fmaf(A[c], state[c], B[c]);
+  const Crossing x = crossing(starts, BACK ? hi : lo);
+  if (x.there) {
+    uint32_t from = part, to = part;  // parts, without the last one
+    if constexpr (BACK) {
+      uint32_t last = (max(x.behind, 1u) - 1) / span;
+      if (last && x.behind >= last * span && x.behind - last * span < span / 2) --last;  // that part begins where the sequence ends
+      from = part + 1;
+      to = min(last + 1, parts);
+    } else {
+      from = x.first / span;
     }
-    // sequences without tokens leave what they start from
-    if (q.end) {
-      for (uint32_t s0 = (part * kWalkWaves + wave) * 64; s0 < starts.sequences; s0 += parts * kWalkWaves * 64) {
-        const uint32_t s = s0 + lane;
-        uint64_t empty = __ballot(s < starts.sequences && starts.get(s) >= starts.get(s + 1));
-        while (empty) {
-          const uint32_t one = s0 + uint32_t(__builtin_ctzll(empty));
-          float v[C];
-          W::begin(r, q.begin, one, v);
-          W::leave(r, q.end, one, v);
-          empty &= empty - 1;
-        }
-      }
+    for (uint32_t k = from; k < to; ++k) {
+      const uint64_t map = walk.map_of(parts, BACK ? to - 1 - (k - from) : k);
+      const Raw<false, C> A = load_raw<false, C>(map, walk.at32), B = load_raw<false, C>(map + uint64_t(r.channels) * 4, walk.at32);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        state[c] = k == from ? as_float(B.w[c]) : __builtin_fmaf(as_float(A.w[c]), state[c], as_float(B.w[c]));
     }
   }
-  float all_a[C], all_b[C];  // MAPS: the part's map so far
-  bool any_cut = false;
-#pragma unroll
-  for (int c = 0; c < C; ++c) all_a[c] = 1.0f, all_b[c] = 0.0f;
 
   const uint32_t tiles = (hi - lo + kTile - 1) / kTile;
   const bool whole_list = starts.sequences < 64;
@@ -335,113 +362,120 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
     const uint32_t tile = lo + (BACK ? tiles - 1 - i : i) * kTile;
     const uint32_t t0 = tile + (BACK ? kWalkWaves - 1 - wave : wave) * kSteps;
     const uint32_t count = t0 < hi ? min(hi - t0, uint32_t(kSteps)) : 0;
-    typename W::Rows x;
-    W::template load<MAPS>(r, q, t0, hi, x);
+    typename Walk<BF16, C, BACK>::raw gate[kSteps], input[kSteps], prior[BACK ? kSteps : 1], ds[BACK ? kSteps : 1];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const uint32_t t = min(t0 + k, hi - 1);
+      gate[k] = walk.load(kRecGate, t, r.pitch);
+      if constexpr (BACK) ds[k] = walk.load(kRecDstates, t, r.states_pitch);
+      input[k] = walk.load(kRecInput, t, r.pitch);
+      if constexpr (BACK) prior[k] = walk.load(kRecStates, t ? t - 1 : 0, r.states_pitch);
+    }
     if (!whole_list) view = window(starts, t0);
     const Marks mark = marks(starts, view, t0);
+    const bool plain = !mark.any && count == kSteps && t0 >= none_before && t0 + kSteps <= none_behind;  // all inside one sequence
 
     // this wavefront's map
-    float a[kSteps][C], b[kSteps][C], A[C], B[C], first[kSteps][C];
+    float a[kSteps][C], b[kSteps][C], first[kSteps][C];
+    Map map;
     bool cut = false;
 #pragma unroll
-    for (int c = 0; c < C; ++c) A[c] = 1.0f, B[c] = 0.0f;
-    if (mark.any) {
+    for (int c = 0; c < C; ++c) map[c] = 1.0f, map[C + c] = 0.0f;
+    auto step = [&](int k) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        if constexpr (BACK) map[C + c] = a[k][c] * (widen<BF16, C>(ds[k], c) + map[C + c]);
+        else map[C + c] = __builtin_fmaf(a[k][c], map[C + c], b[k][c] * widen<BF16, C>(input[k], c));
+        map[c] *= a[k][c];
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+      for (int c = 0; c < C; ++c) gates<BF16>(widen<BF16, C>(gate[k], c), &a[k][c], &b[k][c]);
+    if (plain) {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) step(BACK ? kSteps - 1 - j : j);
+    } else {
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) {
         const uint32_t s = BACK ? mark.ends[k] : mark.begins[k];
-#pragma unroll
-        for (int c = 0; c < C; ++c) first[k][c] = 0.0f;
-        if (s != kNone && uint32_t(k) < count) W::begin(r, q.begin, s, first[k]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int k = BACK ? kSteps - 1 - j : j;
-      const uint32_t t = t0 + k;
-#pragma unroll
-      for (int c = 0; c < C; ++c) gates<BF16>(widen<BF16, C>(x.gate[k], c), &a[k][c], &b[k][c]);
-      if (uint32_t(k) >= count || t < none_before || t >= none_behind) continue;
-      const bool begins = mark.any && (BACK ? mark.ends[k] : mark.begins[k]) != kNone;
-      if (begins) {
-        cut = true;
-#pragma unroll
-        for (int c = 0; c < C; ++c) B[c] = first[k][c];
+        if (s != kNone && uint32_t(k) < count) walk.get(walk.kBegin, s, first[k]);
       }
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        if constexpr (BACK) B[c] = a[k][c] * (widen<BF16, C>(x.ds[k], c) + B[c]);
-        else B[c] = __builtin_fmaf(a[k][c], B[c], b[k][c] * widen<BF16, C>(x.input[k], c));
-        A[c] *= a[k][c];
+      for (int j = 0; j < kSteps; ++j) {
+        const int k = BACK ? kSteps - 1 - j : j;
+        if (uint32_t(k) >= count || t0 + k < none_before || t0 + k >= none_behind) continue;
+        if ((BACK ? mark.ends[k] : mark.begins[k]) != kNone) {
+          cut = true;
+#pragma unroll
+          for (int c = 0; c < C; ++c) map[C + c] = first[k][c];
+        }
+        step(k);
       }
     }
     const uint32_t turn = i % 2;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      maps[turn][wave][0][c][lane] = A[c];
-      maps[turn][wave][1][c][lane] = B[c];
-    }
+    maps[turn][wave][lane] = map;
     if (lane == 0) cuts[turn][wave] = cut;
     __syncthreads();
     float s[C];  // the state this wavefront's tokens start from
-#pragma unroll
-    for (int c = 0; c < C; ++c) s[c] = state[c];
+    const uint64_t cut_by = __ballot(lane < kWalkWaves && cuts[turn][lane % kWalkWaves]);
 #pragma unroll
     for (int v = 0; v < kWalkWaves; ++v) {
-      const bool from_here = uniform(cuts[turn][v]) != 0;
-      any_cut = any_cut || from_here;
+      const Map m = maps[turn][v][lane];
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         if (uint32_t(v) == wave) s[c] = state[c];
-        const float mA = maps[turn][v][0][c][lane], mB = maps[turn][v][1][c][lane];
-        if constexpr (MAPS) {
-          all_a[c] *= mA;
-          all_b[c] = from_here ? mB : __builtin_fmaf(mA, all_b[c], mB);
-        } else {
-          state[c] = from_here ? mB : __builtin_fmaf(mA, state[c], mB);
-        }
+        state[c] = cut_by >> v & 1 ? m[C + c] : __builtin_fmaf(m[c], state[c], m[C + c]);
       }
     }
-    if constexpr (MAPS) continue;
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int k = BACK ? kSteps - 1 - j : j;
-      const uint32_t t = t0 + k;
-      if (uint32_t(k) >= count || t < none_before || t >= none_behind) continue;
-      const bool begins = mark.any && (BACK ? mark.ends[k] : mark.begins[k]) != kNone;
-      if (begins) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) s[c] = first[k][c];
-      }
-      const uint32_t over = !mark.any ? kNone : BACK ? mark.begins[k] : mark.ends[k];
+    auto out = [&](int k, const float* before) {
+      const uint64_t t = t0 + k;
       if constexpr (BACK) {
-        float prior[C], du[C], dg[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) prior[c] = widen<BF16, C>(x.prior[k], c);
-        if (over != kNone) W::begin(r, q.before, over, prior);
+        float du[C], dg[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          const float e = widen<BF16, C>(x.ds[k], c) + s[c];
+          const float e = widen<BF16, C>(ds[k], c) + s[c];
           du[c] = b[k][c] * e;
-          dg[c] = (a[k][c] * du[c]) * (prior[c] - widen<BF16, C>(x.input[k], c));
+          dg[c] = (a[k][c] * du[c]) * (before[c] - widen<BF16, C>(input[k], c));
           s[c] = a[k][c] * e;
         }
-        store_channels<BF16, C>(q.dinput + t * r.pitch * ES, du);
-        store_channels<BF16, C>(q.dgate + t * r.pitch * ES, dg);
+        store_channels<BF16, C>(walk.row(kRecDinput, t, r.pitch), walk.at, du);
+        store_channels<BF16, C>(walk.row(kRecDgate, t, r.pitch), walk.at, dg);
       } else {
 #pragma unroll
-        for (int c = 0; c < C; ++c) s[c] = __builtin_fmaf(a[k][c], s[c], b[k][c] * widen<BF16, C>(x.input[k], c));
-        store_channels<BF16, C>(q.states + t * r.states_pitch * ES, s);
+        for (int c = 0; c < C; ++c) s[c] = __builtin_fmaf(a[k][c], s[c], b[k][c] * widen<BF16, C>(input[k], c));
+        store_channels<BF16, C>(walk.row(kRecStates, t, r.states_pitch), walk.at, s);
       }
-      if (over != kNone) W::leave(r, q.end, over, s);
-    }
-  }
-  if constexpr (MAPS) {
-    if (wave) return;
-    const uint64_t at = reinterpret_cast<uint64_t>(r.ws) + (uint64_t(w) * parts + part) * r.channels * 2 * 4 + uint64_t(ch) * 4;
+    };
+    auto before = [&](int k, float* v) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      reinterpret_cast<CARAMEL_GLOBAL float*>(at)[c] = any_cut ? 0.0f : all_a[c];
-      reinterpret_cast<CARAMEL_GLOBAL float*>(at + uint64_t(r.channels) * 4)[c] = all_b[c];
+      for (int c = 0; c < C; ++c) v[c] = BACK ? widen<BF16, C>(prior[BACK ? k : 0], c) : 0.0f;
+    };
+    if (plain) {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const int k = BACK ? kSteps - 1 - j : j;
+        float p[C];
+        before(k, p);
+        out(k, p);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const int k = BACK ? kSteps - 1 - j : j;
+        if (uint32_t(k) >= count || t0 + k < none_before || t0 + k >= none_behind) continue;
+        if ((BACK ? mark.ends[k] : mark.begins[k]) != kNone) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) s[c] = first[k][c];
+        }
+        const uint32_t over = BACK ? mark.begins[k] : mark.ends[k];
+        float p[C];
+        before(k, p);
+        if (BACK && over != kNone) walk.get(kRecBefore, over, p);
+        out(k, p);
+        if (over != kNone) walk.put(walk.kEnd, over, s);
+      }
     }
   }
 }
@@ -461,11 +495,11 @@ template <bool BF16, int C, bool BACK>
 hipError_t launch_walk(const RecurrenceArgs& a, uint32_t span, uint32_t parts, hipStream_t s) {
   const dim3 grid((a.channels + 64 * C - 1) / (64 * C), parts, a.world);
   if (parts > 1) {
-    hipLaunchKernelGGL((k_walk_tokens<BF16, C, BACK, true>), grid, dim3(kLanes), 0, s, a, span, parts);
+    hipLaunchKernelGGL((k_walk_maps<BF16, C, BACK>), grid, dim3(kLanes), 0, s, a, span, parts);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_walk_tokens<BF16, C, BACK, false>), grid, dim3(kLanes), 0, s, a, span, parts);
+  hipLaunchKernelGGL((k_walk_tokens<BF16, C, BACK>), grid, dim3(kLanes), 0, s, a, span, parts);
   return hipGetLastError();
 }
 
