@@ -1484,7 +1484,7 @@ int recurrence_workspace(const caramel_plan* p, uint64_t channels, const uint64_
   uint32_t n[CARAMEL_MAX_WORLD], most = 0;
   if (int rc = check_columns("channels", channels)) return rc;
   if (int rc = take_tokens(p, tokens, n, &most)) return rc;
-  *bytes = recurrence_workspace_bytes(p->host.cfg.world, uint32_t(channels), most);
+  *bytes = recurrence_workspace_bytes(p->host.cfg.world, uint32_t(channels), n);
   return CARAMEL_OK;
 }
 
@@ -1511,7 +1511,7 @@ int take_recurrence(caramel_plan* p, uint64_t channels, const uint64_t* tokens, 
   if (int rc = take_pointers(p, "gate", gate, v.tokens, es, v.at[kRecGate])) return rc;
   if (int rc = take_pointers(p, "input", input, v.tokens, es, v.at[kRecInput])) return rc;
   if (int rc = take_optional(p, "before", reinterpret_cast<const void* const*>(before), v.tokens, 4, v.at[kRecBefore])) return rc;
-  const uint64_t need = recurrence_workspace_bytes(a.all, uint32_t(channels), a.max_tokens);
+  const uint64_t need = recurrence_workspace_bytes(a.all, uint32_t(channels), v.tokens);
   if (int rc = check_workspace(ws, ws_bytes, need)) return rc;
   m.add(reinterpret_cast<uint64_t>(ws), need, true);
   for (uint32_t w = 0; w < a.all; ++w) {

@@ -169,8 +169,12 @@ struct RecurrenceArgs {
   uint64_t pitch, states_pitch;  // of gates, inputs and their gradients; of states and theirs; elements
   bool bf16, starts64;
   unsigned char* ws;
+  // made by the launch: tokens are cut into parts of `span`, and the parts are counted through all workers
+  uint32_t span, first_part[kGroup + 1];
+  bool cut;    // a worker has more than one
+  bool lines;  // rows are whole cache lines
 };
-uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, uint32_t max_tokens);
+uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, const uint32_t* tokens);
 hipError_t launch_recurrence(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);
 hipError_t launch_recurrence_gradient(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);
 

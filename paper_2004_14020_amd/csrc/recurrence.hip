@@ -6,9 +6,8 @@
 // A step is an affine map, and two of them in a row are one: (A, B) after (A', B') is (A A', A B' + B).  A workgroup takes a
 // span of a worker's tokens for 64 C channels and walks it in tiles; in a tile every wavefront maps its own tokens, all
 // exchange what their maps are, and each starts its tokens from the state that the maps before it give.  So every value is read
-// and written once.  Where workers and channels are too few for the GPU, the tokens are cut into parts, at the start of a
-// sequence if one is near; where a sequence goes on behind a part, a launch before this one leaves the map of its tokens in the part.
-// The gradient walks the same way from the last token to the first.
+// and written once.  Where workers and channels are too few for the GPU, the tokens are cut into parts, and where a sequence goes on
+// behind a part, a launch before this one leaves the map of its tokens in the part.  The gradient walks the same way from the last token to the first.
 //
 // A sequence's first token (its last one, in the gradient) takes nothing from what was before: where it stands, the map is replaced
 // and not multiplied by zero, so that an infinity or NaN ends with its sequence.  States are fp32.
@@ -16,36 +15,35 @@
 #include <type_traits>
 
 #include "layers.hpp"
-#include "vec.hpp"
+#include "rows.hpp"
 
 namespace caramel {
 namespace {
 
-constexpr int kSteps = 8;            // tokens of a wavefront in a tile
+constexpr int kSteps = 4;            // tokens of a wavefront in a tile
 constexpr int kWalkWaves = 8;        // wavefronts of a workgroup
-constexpr int kAhead = 16;           // rows of gates that a wavefront asks for at once where it only maps
+constexpr int kAhead = 8;            // rows of gates that a wavefront asks for at once where it only maps
 constexpr uint32_t kTile = kSteps * kWalkWaves;
 constexpr uint32_t kLanes = 64 * kWalkWaves;
+constexpr uint32_t kDies = 8;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
-// C neighbouring channels, as they lie in memory, and widened.  A row's address is the same for all lanes, so it stays in scalar registers;
-// `at` is a lane's distance from it in bytes.
+// C neighbouring channels, as they lie in memory, and widened.  Rows are reached through buffer resources: where a wavefront's rows begin, and how
+// far a row is from there, are the same for all lanes and stay in scalar registers; `at` is a lane's distance in a row, in bytes.
 template <bool BF16, int C>
 struct Raw {
   uint32_t w[BF16 && C == 2 ? 1 : C];
 };
-template <bool BF16, int C>
-__device__ __forceinline__ Raw<BF16, C> load_raw(uint64_t row, uint32_t at) {
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(uint64_t first) { return buffer(first, 0xFFFFFFFFu); }
+template <bool BF16, int C, bool STREAM = false>
+__device__ __forceinline__ Raw<BF16, C> load_raw(const __amdgpu_buffer_rsrc_t& rows, uint32_t at, uint32_t row) {
   Raw<BF16, C> r;
-  if constexpr (C == 1) {
-    if constexpr (BF16) r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL uint16_t*>(row + at);
-    else r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL uint32_t*>(row + at);
-  } else if constexpr (BF16) {
-    typedef uint32_t word __attribute__((aligned(2)));
-    r.w[0] = *reinterpret_cast<const CARAMEL_GLOBAL word*>(row + at);
+  if constexpr (C == 1 && BF16) {
+    r.w[0] = uint32_t(__builtin_amdgcn_raw_buffer_load_b16(rows, int(at), int(row), STREAM ? kStreaming : 0));
+  } else if constexpr (C == 1 || BF16) {
+    r.w[0] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(rows, int(at), int(row), STREAM ? kStreaming : 0));
   } else {
-    typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(4)));
-    const pair p = *reinterpret_cast<const CARAMEL_GLOBAL pair*>(row + at);
+    const u32x2 p = __builtin_amdgcn_raw_buffer_load_b64(rows, int(at), int(row), STREAM ? kStreaming : 0);
     r.w[0] = p[0];
     r.w[1] = p[1];
   }
@@ -56,17 +54,15 @@ __device__ __forceinline__ float widen(const Raw<BF16, C>& r, int c) {
   if constexpr (!BF16) return as_float(r.w[c]);
   else return c ? bf16_high(r.w[0]) : bf16_low(r.w[0]);
 }
-template <bool BF16, int C>
-__device__ __forceinline__ void store_channels(uint64_t row, uint32_t at, const float* v) {
-  if constexpr (C == 1) {
-    store_elems<BF16, 1>(row + at, v);
-  } else if constexpr (BF16) {
-    typedef uint32_t word __attribute__((aligned(2)));
-    *reinterpret_cast<CARAMEL_GLOBAL word*>(row + at) = bf16_pair(v[0], v[1]);
+template <bool BF16, int C, bool STREAM = false>
+__device__ __forceinline__ void store_channels(const __amdgpu_buffer_rsrc_t& rows, uint32_t at, uint32_t row, const float* v) {
+  if constexpr (BF16) {
+    const uint32_t p = bf16_pair(v[0], v[C - 1]);
+    if constexpr (C == 1) __builtin_amdgcn_raw_buffer_store_b16(uint16_t(p), rows, int(at), int(row), STREAM ? kStreaming : 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(p, rows, int(at), int(row), STREAM ? kStreaming : 0);
   } else {
-    typedef float pair __attribute__((ext_vector_type(2), aligned(4)));
-    const pair p = {v[0], v[1]};
-    *reinterpret_cast<CARAMEL_GLOBAL pair*>(row + at) = p;
+    if constexpr (C == 1) __builtin_amdgcn_raw_buffer_store_b32(as_bits(v[0]), rows, int(at), int(row), STREAM ? kStreaming : 0);
+    else __builtin_amdgcn_raw_buffer_store_b64(u32x2{as_bits(v[0]), as_bits(v[1])}, rows, int(at), int(row), STREAM ? kStreaming : 0);
   }
 }
 
@@ -92,11 +88,19 @@ __device__ __forceinline__ void gates(float g, float* a, float* b) {
 
 // ---- where sequences begin ------------------------------------------------------------------
 
-// The list of a worker's starts, in device memory; what is no place among the tokens counts as the nearest one.
+// The list of a worker's starts, in device memory; what is no place among the tokens counts as the nearest one.  A list of up to 64
+// numbers is loaded once, one to a lane, and everything is asked of the lanes (a longer one takes a chain of loads for every question, some
+// microseconds at the start of a workgroup).
 struct Starts {
   uint64_t at;
   uint32_t sequences, tokens;
-  bool wide;
+  bool wide, whole;
+  uint32_t mine;  // whole: the lane's entry
+
+  __device__ __forceinline__ Starts(uint64_t list, uint32_t n, uint32_t most, bool is_wide)
+      : at(list), sequences(n), tokens(most), wide(is_wide), whole(n < 64), mine(0) {
+    if (whole) mine = get(threadIdx.x % 64);
+  }
   // lanes ask for entries by themselves; behind the list there is what no token reaches
   __device__ __forceinline__ uint32_t get(uint32_t i) const {
     if (i > sequences) return 0x7FFFFFFFu;
@@ -104,15 +108,21 @@ struct Starts {
                            : int64_t(reinterpret_cast<const CARAMEL_GLOBAL int32_t*>(at)[i]);
     return v < 0 ? 0u : v > int64_t(tokens) ? tokens : uint32_t(v);
   }
+  // an entry that all lanes ask for
+  __device__ __forceinline__ uint32_t one(uint32_t i) const {
+    if (whole) return i > sequences ? 0x7FFFFFFFu : uint32_t(__builtin_amdgcn_readlane(int(mine), int(i)));
+    return uniform(get(i));
+  }
   // the first entry that is x or more, by the whole wavefront: 64 probes at a time
   __device__ __forceinline__ uint32_t lower(uint32_t x) const {
     const uint32_t lane = threadIdx.x % 64;
+    if (whole) return uint32_t(__builtin_popcountll(__ballot(mine < x)));
     uint32_t lo = 0, len = sequences + 1;
     while (len > 0) {
       const uint32_t step = (len + 63) / 64, probe = lane * step + step - 1;
       const uint32_t below = uint32_t(__builtin_popcountll(__ballot(probe < len && get(lo + probe) < x)));
       lo += below * step;
-      len = step == 1 ? 0 : below == 64 ? 0 : min(step - 1, len - min(len, below * step));
+      len = step == 1 ? 0 : min(step - 1, len - min(len, below * step));
     }
     return uniform(min(lo, sequences + 1));
   }
@@ -125,8 +135,8 @@ struct Window {
 };
 __device__ __forceinline__ Window window(const Starts& s, uint32_t token) {
   Window w;
-  w.first = s.sequences < 64 ? 0 : s.lower(token);  // a short list is seen whole
-  w.entry = s.get(w.first + threadIdx.x % 64);
+  w.first = s.whole ? 0 : s.lower(token);
+  w.entry = s.whole ? s.mine : s.get(w.first + threadIdx.x % 64);
   return w;
 }
 
@@ -157,7 +167,7 @@ __device__ __forceinline__ Marks marks(const Starts& s, const Window& v, uint32_
 #pragma unroll 1
     for (int k = 0; k < kSteps; ++k) {
       const uint32_t next = s.lower(t0 + k + 1);
-      const bool begins = next > at, ends = uniform(s.get(next)) == t0 + k + 1;
+      const bool begins = next > at, ends = s.one(next) == t0 + k + 1;
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {  // (the index of an array in registers is a constant)
         if (j == k && begins) m.begins[j] = next - 1;
@@ -182,45 +192,51 @@ struct Walk {
   static constexpr int ES = BF16 ? 2 : 4;
   typedef Raw<BF16, C> raw;
   const RecurrenceArgs& r;
-  uint32_t w, at, at32;  // a lane's distance in bytes from the rows of dtype, and from fp32 rows
+  uint32_t w, part, parts;  // parts of the worker
+  bool there;               // the grid may have more workgroups than there are parts
+  uint32_t at, at32;        // a lane's distance in bytes from the rows of dtype, and from fp32 rows
 
-  __device__ __forceinline__ Walk(const RecurrenceArgs& args) : r(args), w(blockIdx.z) {
-    const uint32_t channel = min((blockIdx.x * 64 + threadIdx.x % 64) * C, r.channels - C);
+  __device__ __forceinline__ Walk(const RecurrenceArgs& args) : r(args), w(0) {
+    // Workgroups go to the eight dies in turn: all channels of a part go to one of them, whose cache then has whole rows (8 x 4096 tokens of
+    // 1000 bf16, whose rows end inside a cache line: gradient 130 us, so 89).
+    const uint32_t slabs = (r.channels + 64 * C - 1) / (64 * C), turn = blockIdx.x / kDies, k = turn / slabs * kDies + blockIdx.x % kDies;
+    there = k < r.first_part[kGroup];
+#pragma unroll
+    for (uint32_t i = 1; i < kGroup; ++i) w += there && k >= r.first_part[i] ? 1 : 0;
+    part = k - r.first_part[w];
+    parts = r.first_part[w + 1] - r.first_part[w];
+    const uint32_t channel = min((turn % slabs * 64 + threadIdx.x % 64) * C, r.channels - C);
     at = channel * ES;
     at32 = channel * 4;
   }
-  __device__ __forceinline__ uint64_t row(int which, uint64_t t, uint64_t pitch) const { return r.w.at[which][w] + t * pitch * ES; }
-  __device__ __forceinline__ raw load(int which, uint64_t t, uint64_t pitch) const {
-    return load_raw<BF16, C>(row(which, t, pitch), at);
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows(int which, uint32_t t, uint64_t pitch) const {
+    return rows_from(r.w.at[which][w] + t * pitch * ES);
   }
 
   // fp32 rows of the sequences (zeros, or nothing, where the call has none)
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_of(int which, uint32_t sequence) const {
+    return rows_from(r.w.at[which][w] + uint64_t(sequence) * r.channels * 4);
+  }
   __device__ __forceinline__ void get(int which, uint32_t sequence, float* v) const {
 #pragma unroll
     for (int c = 0; c < C; ++c) v[c] = 0.0f;
     if (!r.w.at[which][w]) return;
-    const raw32 x = load_raw<false, C>(r.w.at[which][w] + uint64_t(sequence) * r.channels * 4, at32);
+    const raw32 x = load_raw<false, C>(row_of(which, sequence), at32, 0);
 #pragma unroll
     for (int c = 0; c < C; ++c) v[c] = as_float(x.w[c]);
   }
   __device__ __forceinline__ void put(int which, uint32_t sequence, const float* v) const {
-    if (r.w.at[which][w]) store_channels<false, C>(r.w.at[which][w] + uint64_t(sequence) * r.channels * 4, at32, v);
+    if (r.w.at[which][w]) store_channels<false, C>(row_of(which, sequence), at32, 0, v);
   }
   typedef Raw<false, C> raw32;
   // what a sequence's walk starts from, and where it leaves what it ends with
   static constexpr int kBegin = BACK ? kRecDafter : kRecBefore, kEnd = BACK ? kRecDbefore : kRecAfter;
 
   // a part's map in the workspace: two fp32 rows
-  __device__ __forceinline__ uint64_t map_of(uint32_t parts, uint32_t part) const {
-    return reinterpret_cast<uint64_t>(r.ws) + (uint64_t(w) * parts + part) * r.channels * 8;
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t map_of(uint32_t k) const {
+    return rows_from(reinterpret_cast<uint64_t>(r.ws) + uint64_t(r.first_part[w] + k) * r.channels * 8);
   }
 };
-
-// Where a part begins: at a multiple of `span`, or at the sequence that starts next if that is less than half a part on.
-__device__ __forceinline__ uint32_t border(const Starts& s, uint32_t part, uint32_t span) {
-  const uint32_t x = min(part * span, s.tokens), next = uniform(s.get(s.lower(x)));
-  return part && next >= x && next - x < span / 2 ? min(next, s.tokens) : x;
-}
 
 // The sequence that goes on across the border in front of token x: its number, its first token and the one behind its last.
 struct Crossing {
@@ -230,24 +246,22 @@ struct Crossing {
 __device__ __forceinline__ Crossing crossing(const Starts& s, uint32_t x) {
   const uint32_t next = s.lower(x);  // the first start from x on
   Crossing c;
-  c.behind = uniform(s.get(next));
+  c.behind = s.one(next);
   c.there = next > 0 && next <= s.sequences && c.behind != x;
   c.sequence = next - 1;
-  c.first = c.there ? uniform(s.get(next - 1)) : 0;
+  c.first = c.there ? s.one(next - 1) : 0;
   return c;
 }
 
 // The maps of the parts out of which a sequence goes on: of its tokens there, all of which are inside.  Every wavefront has a stretch of them.
-// blockIdx: x channels, y part, z worker.
 template <bool BF16, int C, bool BACK>
-__global__ void __launch_bounds__(kLanes) k_walk_maps(RecurrenceArgs r, uint32_t span, uint32_t parts) {
+__global__ void __launch_bounds__(kLanes) k_walk_maps(RecurrenceArgs r) {
   __shared__ float maps[kWalkWaves][2][C][64];
   const Walk<BF16, C, BACK> walk(r);
-  const uint32_t n = r.w.tokens[walk.w], part = blockIdx.y, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
-  if (part * span >= n) return;
-  const Starts starts{r.w.at[kRecStarts][walk.w], r.w.more[walk.w], n, r.starts64};
-  uint32_t lo = border(starts, part, span), hi = part + 1 < parts ? border(starts, part + 1, span) : n;
-  if (lo >= hi) return;
+  if (!walk.there) return;
+  const uint32_t n = r.w.tokens[walk.w], part = walk.part, span = r.span, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+  const Starts starts(r.w.at[kRecStarts][walk.w], r.w.more[walk.w], n, r.starts64);
+  uint32_t lo = part * span, hi = min(lo + span, n);
   const Crossing x = crossing(starts, BACK ? lo : hi);
   if (!x.there) return;
   const bool begins = BACK ? x.behind <= hi : x.first >= lo;  // inside the part
@@ -263,11 +277,15 @@ __global__ void __launch_bounds__(kLanes) k_walk_maps(RecurrenceArgs r, uint32_t
   auto steps = [&](uint32_t done, auto count) {
     constexpr int N = decltype(count)::value;
     typename Walk<BF16, C, BACK>::raw gate[N], add[N];
+    const uint32_t t0 = BACK ? to - done - N : from + done;
+    const uint64_t add_pitch = BACK ? r.states_pitch : r.pitch;
+    const __amdgpu_buffer_rsrc_t gates_at = walk.rows(kRecGate, t0, r.pitch);
+    const __amdgpu_buffer_rsrc_t add_at = walk.rows(BACK ? kRecDstates : kRecInput, t0, add_pitch);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const uint32_t t = BACK ? to - 1 - done - k : from + done + k;
-      gate[k] = walk.load(kRecGate, t, r.pitch);
-      add[k] = BACK ? walk.load(kRecDstates, t, r.states_pitch) : walk.load(kRecInput, t, r.pitch);
+      const uint32_t on = BACK ? N - 1 - k : k;
+      gate[k] = load_raw<BF16, C>(gates_at, walk.at, on * uint32_t(r.pitch) * walk.ES);
+      add[k] = load_raw<BF16, C>(add_at, walk.at, on * uint32_t(add_pitch) * walk.ES);
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -299,24 +317,47 @@ __global__ void __launch_bounds__(kLanes) k_walk_maps(RecurrenceArgs r, uint32_t
       B[c] = __builtin_fmaf(maps[v][0][c][lane], B[c], maps[v][1][c][lane]);
     }
   }
-  store_channels<false, C>(walk.map_of(parts, part), walk.at32, A);
-  store_channels<false, C>(walk.map_of(parts, part) + uint64_t(r.channels) * 4, walk.at32, B);
+  store_channels<false, C>(walk.map_of(part), walk.at32, 0, A);
+  store_channels<false, C>(walk.map_of(part), walk.at32, r.channels * 4, B);
 }
 
-// The walk itself.
-template <bool BF16, int C, bool BACK>
-__global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32_t span, uint32_t parts) {
+// The rows of a wavefront's tokens in a tile, from token t0 on; of those from `stop` on, the last one before it.
+template <bool BF16, int C, bool BACK, bool STREAM>
+struct TileRows {
+  Raw<BF16, C> gate[kSteps], input[kSteps], prior[BACK ? kSteps : 1], ds[BACK ? kSteps : 1];
+  __device__ __forceinline__ void load(const Walk<BF16, C, BACK>& walk, uint32_t t0, uint32_t stop) {
+    const RecurrenceArgs& r = walk.r;
+    const uint32_t base = min(t0, stop - 1), more = stop - 1 - base, before = base ? base - 1 : 0;
+    const __amdgpu_buffer_rsrc_t gates_at = walk.rows(kRecGate, base, r.pitch), input_at = walk.rows(kRecInput, base, r.pitch);
+    const __amdgpu_buffer_rsrc_t ds_at = walk.rows(kRecDstates, base, r.states_pitch);
+    const __amdgpu_buffer_rsrc_t prior_at = walk.rows(kRecStates, before, r.states_pitch);
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const uint32_t on = min(uint32_t(k), more), row = on * uint32_t(r.pitch) * walk.ES;
+      gate[k] = load_raw<BF16, C, STREAM>(gates_at, walk.at, row);
+      if constexpr (BACK) ds[k] = load_raw<BF16, C, STREAM>(ds_at, walk.at, on * uint32_t(r.states_pitch) * walk.ES);
+      input[k] = load_raw<BF16, C, STREAM>(input_at, walk.at, row);
+      // (the first token of all has no row before it, and needs none)
+      if constexpr (BACK) prior[k] = load_raw<BF16, C, STREAM>(prior_at, walk.at, (base || !on ? on : on - 1) * uint32_t(r.states_pitch) * walk.ES);
+    }
+  }
+};
+
+// The walk itself.  STREAM: streaming loads and stores, where every workgroup has whole cache lines of the rows.  (Where two share a line, it had
+// better stay in the cache for the other.)
+template <bool BF16, int C, bool BACK, bool STREAM>
+__global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r) {
   typedef float Map __attribute__((ext_vector_type(2 * C)));
   __shared__ Map maps[2][kWalkWaves][64];
   __shared__ uint32_t cuts[2][kWalkWaves];
   const Walk<BF16, C, BACK> walk(r);
-  const uint32_t n = r.w.tokens[walk.w], part = blockIdx.y, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
-  if (part * span >= n) return;
-  const Starts starts{r.w.at[kRecStarts][walk.w], r.w.more[walk.w], n, r.starts64};
-  const uint32_t lo = border(starts, part, span), hi = part + 1 < parts ? border(starts, part + 1, span) : n;
+  if (!walk.there) return;
+  const uint32_t n = r.w.tokens[walk.w], part = walk.part, span = r.span, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
+  const Starts starts(r.w.at[kRecStarts][walk.w], r.w.more[walk.w], n, r.starts64);
+  const uint32_t lo = part * span, hi = min(lo + span, n);
   // sequences without tokens leave what they start from
   if (r.w.at[walk.kEnd][walk.w]) {
-    for (uint32_t s0 = (part * kWalkWaves + wave) * 64; s0 < starts.sequences; s0 += parts * kWalkWaves * 64) {
+    for (uint32_t s0 = (part * kWalkWaves + wave) * 64; s0 < starts.sequences; s0 += walk.parts * kWalkWaves * 64) {
       uint64_t empty = __ballot(s0 + lane < starts.sequences && starts.get(s0 + lane) >= starts.get(s0 + lane + 1));
       while (empty) {
         const uint32_t one = s0 + uint32_t(__builtin_ctzll(empty));
@@ -327,8 +368,7 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
       }
     }
   }
-  if (lo >= hi) return;
-  const uint32_t none_before = uniform(starts.get(0)), none_behind = uniform(starts.get(starts.sequences));
+  const uint32_t none_before = starts.one(0), none_behind = starts.one(starts.sequences);
 
   // the maps that lead up to this part: of the sequence that comes in, from the part where it begins
   float state[C];
@@ -338,16 +378,14 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
   if (x.there) {
     uint32_t from = part, to = part;  // parts, without the last one
     if constexpr (BACK) {
-      uint32_t last = (max(x.behind, 1u) - 1) / span;
-      if (last && x.behind >= last * span && x.behind - last * span < span / 2) --last;  // that part begins where the sequence ends
       from = part + 1;
-      to = min(last + 1, parts);
+      to = min((max(x.behind, 1u) - 1) / span + 1, walk.parts);
     } else {
       from = x.first / span;
     }
     for (uint32_t k = from; k < to; ++k) {
-      const uint64_t map = walk.map_of(parts, BACK ? to - 1 - (k - from) : k);
-      const Raw<false, C> A = load_raw<false, C>(map, walk.at32), B = load_raw<false, C>(map + uint64_t(r.channels) * 4, walk.at32);
+      const __amdgpu_buffer_rsrc_t map = walk.map_of(BACK ? to - 1 - (k - from) : k);
+      const Raw<false, C> A = load_raw<false, C>(map, walk.at32, 0), B = load_raw<false, C>(map, walk.at32, r.channels * 4);
 #pragma unroll
       for (int c = 0; c < C; ++c)
         state[c] = k == from ? as_float(B.w[c]) : __builtin_fmaf(as_float(A.w[c]), state[c], as_float(B.w[c]));
@@ -355,23 +393,22 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
   }
 
   const uint32_t tiles = (hi - lo + kTile - 1) / kTile;
-  const bool whole_list = starts.sequences < 64;
-  Window view = window(starts, 0);  // the list, where it is short
+  Window view = window(starts, 0);  // the whole list, where it is short
+  // the wavefronts' tokens follow each other the way the walk goes
+  auto first_token = [&](uint32_t i) {
+    return lo + (BACK ? tiles - 1 - i : i) * kTile + (BACK ? kWalkWaves - 1 - wave : wave) * kSteps;
+  };
+  typedef TileRows<BF16, C, BACK, STREAM> Rows;
+  Rows next;
+  next.load(walk, first_token(0), hi);
   for (uint32_t i = 0; i < tiles; ++i) {
-    // the wavefronts' tokens follow each other the way the walk goes
-    const uint32_t tile = lo + (BACK ? tiles - 1 - i : i) * kTile;
-    const uint32_t t0 = tile + (BACK ? kWalkWaves - 1 - wave : wave) * kSteps;
+    const uint32_t t0 = first_token(i);
     const uint32_t count = t0 < hi ? min(hi - t0, uint32_t(kSteps)) : 0;
-    typename Walk<BF16, C, BACK>::raw gate[kSteps], input[kSteps], prior[BACK ? kSteps : 1], ds[BACK ? kSteps : 1];
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const uint32_t t = min(t0 + k, hi - 1);
-      gate[k] = walk.load(kRecGate, t, r.pitch);
-      if constexpr (BACK) ds[k] = walk.load(kRecDstates, t, r.states_pitch);
-      input[k] = walk.load(kRecInput, t, r.pitch);
-      if constexpr (BACK) prior[k] = walk.load(kRecStates, t ? t - 1 : 0, r.states_pitch);
-    }
-    if (!whole_list) view = window(starts, t0);
+    const Rows now = next;
+    next.load(walk, first_token(min(i + 1, tiles - 1)), hi);  // the next tile's are on their way while this one is worked on
+    const auto &gate = now.gate, &input = now.input;
+    const auto &prior = now.prior, &ds = now.ds;
+    if (!starts.whole) view = window(starts, t0);
     const Marks mark = marks(starts, view, t0);
     const bool plain = !mark.any && count == kSteps && t0 >= none_before && t0 + kSteps <= none_behind;  // all inside one sequence
 
@@ -429,8 +466,10 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
         state[c] = cut_by >> v & 1 ? m[C + c] : __builtin_fmaf(m[c], state[c], m[C + c]);
       }
     }
+    const uint32_t base = min(t0, hi - 1);
+    const __amdgpu_buffer_rsrc_t to_input = walk.rows(BACK ? kRecDinput : kRecStates, base, BACK ? r.pitch : r.states_pitch);
+    const __amdgpu_buffer_rsrc_t to_gate = walk.rows(kRecDgate, base, r.pitch);
     auto out = [&](int k, const float* before) {
-      const uint64_t t = t0 + k;
       if constexpr (BACK) {
         float du[C], dg[C];
 #pragma unroll
@@ -440,12 +479,12 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
           dg[c] = (a[k][c] * du[c]) * (before[c] - widen<BF16, C>(input[k], c));
           s[c] = a[k][c] * e;
         }
-        store_channels<BF16, C>(walk.row(kRecDinput, t, r.pitch), walk.at, du);
-        store_channels<BF16, C>(walk.row(kRecDgate, t, r.pitch), walk.at, dg);
+        store_channels<BF16, C, STREAM>(to_input, walk.at, k * uint32_t(r.pitch) * walk.ES, du);
+        store_channels<BF16, C, STREAM>(to_gate, walk.at, k * uint32_t(r.pitch) * walk.ES, dg);
       } else {
 #pragma unroll
         for (int c = 0; c < C; ++c) s[c] = __builtin_fmaf(a[k][c], s[c], b[k][c] * widen<BF16, C>(input[k], c));
-        store_channels<BF16, C>(walk.row(kRecStates, t, r.states_pitch), walk.at, s);
+        store_channels<BF16, C, STREAM>(to_input, walk.at, k * uint32_t(r.states_pitch) * walk.ES, s);
       }
     };
     auto before = [&](int k, float* v) {
@@ -480,47 +519,83 @@ __global__ void __launch_bounds__(kLanes) k_walk_tokens(RecurrenceArgs r, uint32
   }
 }
 
-constexpr uint32_t kWalkGroups = 512;   // workgroups of a launch that parts are made for
+// Workgroups of a launch that parts are made for: two to a compute unit, which is what their registers leave room for, so that all of
+// them run at once.
+constexpr uint32_t kWalkGroups = 512;
 constexpr uint32_t kShortest = 2 * kTile;  // tokens of a part, at least
 
-uint32_t slabs(uint32_t channels) { return (channels + 127) / 128; }
-
-uint32_t walk_parts(uint32_t world, uint32_t channels, uint32_t max_tokens) {
-  const uint64_t there = uint64_t(std::min(world, kGroup)) * slabs(channels);
-  const uint32_t most = uint32_t((kWalkGroups + there - 1) / there);
-  return std::max(1u, std::min(most, max_tokens / kShortest));
+// The most parts that the workers of a launch may have together.
+uint32_t most_parts(uint32_t world, uint32_t channels, const uint32_t* tokens) {
+  const uint32_t slabs = (channels + 127) / 128, wanted = (kWalkGroups + slabs - 1) / slabs;
+  uint64_t could = 0, must = 0;
+  for (uint32_t w = 0; w < world; ++w) {
+    could += std::max(tokens[w] ? 1u : 0u, tokens[w] / kShortest);
+    must += tokens[w] ? 1 : 0;
+  }
+  return uint32_t(std::max(must, std::min<uint64_t>(could, wanted)));
+}
+// All workers' parts are equally long, so that they end together: the shortest span that makes no more of them.
+uint32_t span_of(uint32_t world, const uint32_t* tokens, uint32_t most, uint32_t max_tokens) {
+  uint32_t lo = 1, hi = (max_tokens + kTile - 1) / kTile;  // in tiles
+  while (lo < hi) {
+    const uint32_t mid = (lo + hi) / 2;
+    uint64_t parts = 0;
+    for (uint32_t w = 0; w < world; ++w) parts += (tokens[w] + mid * kTile - 1) / (mid * kTile);
+    if (parts <= most) hi = mid;
+    else lo = mid + 1;
+  }
+  return hi * kTile;
 }
 
 template <bool BF16, int C, bool BACK>
-hipError_t launch_walk(const RecurrenceArgs& a, uint32_t span, uint32_t parts, hipStream_t s) {
-  const dim3 grid((a.channels + 64 * C - 1) / (64 * C), parts, a.world);
-  if (parts > 1) {
-    hipLaunchKernelGGL((k_walk_maps<BF16, C, BACK>), grid, dim3(kLanes), 0, s, a, span, parts);
+hipError_t launch_walk(const RecurrenceArgs& a, hipStream_t s) {
+  const uint32_t parts = a.first_part[a.world];
+  if (!parts) return hipSuccess;
+  const dim3 grid((a.channels + 64 * C - 1) / (64 * C) * ((parts + kDies - 1) / kDies * kDies));
+  if (a.cut) {
+    hipLaunchKernelGGL((k_walk_maps<BF16, C, BACK>), grid, dim3(kLanes), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_walk_tokens<BF16, C, BACK>), grid, dim3(kLanes), 0, s, a, span, parts);
+  if (C == 2 && a.lines) hipLaunchKernelGGL((k_walk_tokens<BF16, C, BACK, C == 2>), grid, dim3(kLanes), 0, s, a);
+  else hipLaunchKernelGGL((k_walk_tokens<BF16, C, BACK, false>), grid, dim3(kLanes), 0, s, a);
   return hipGetLastError();
 }
 
 template <bool BACK>
 hipError_t launch_any(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s) {
   if (args.max_tokens == 0) return hipSuccess;
-  const uint32_t most = walk_parts(args.all, args.channels, args.max_tokens);
-  const uint32_t span = ((args.max_tokens + most - 1) / most + kTile - 1) / kTile * kTile;
-  const uint32_t parts = (args.max_tokens + span - 1) / span;  // no more than `most`
-  return in_groups(args, v, [&](RecurrenceArgs a, uint32_t g) {
-    a.ws += uint64_t(g) * parts * a.channels * 2 * 4;
-    if (a.channels == 1) return a.bf16 ? launch_walk<true, 1, BACK>(a, span, parts, s) : launch_walk<false, 1, BACK>(a, span, parts, s);
-    return a.bf16 ? launch_walk<true, 2, BACK>(a, span, parts, s) : launch_walk<false, 2, BACK>(a, span, parts, s);
+  return in_groups(args, v, [&](RecurrenceArgs a, uint32_t) {
+    a.span = span_of(a.world, a.w.tokens, most_parts(a.world, a.channels, a.w.tokens), a.max_tokens);
+    a.cut = false;
+    // all rows begin on cache lines, and their channels fill them
+    const uint64_t es = a.bf16 ? 2 : 4;
+    uint64_t ends = a.channels * es | a.pitch * es | a.states_pitch * es;
+    for (uint32_t w = 0; w < a.world; ++w)
+      for (int which : {kRecGate, kRecInput, kRecStates, kRecDstates, kRecDgate, kRecDinput}) ends |= a.w.tokens[w] ? a.w.at[which][w] : 0;
+    a.lines = ends % 128 == 0;
+    for (uint32_t w = 0; w < kGroup; ++w) {  // (behind the last worker: its end)
+      const uint32_t parts = w < a.world ? (a.w.tokens[w] + a.span - 1) / a.span : 0;
+      a.first_part[w + 1] = a.first_part[w] + parts;
+      a.cut = a.cut || parts > 1;
+    }
+    if (a.channels == 1) return a.bf16 ? launch_walk<true, 1, BACK>(a, s) : launch_walk<false, 1, BACK>(a, s);
+    return a.bf16 ? launch_walk<true, 2, BACK>(a, s) : launch_walk<false, 2, BACK>(a, s);
   });
 }
 
 }  // namespace
 
-uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, uint32_t max_tokens) {
-  const uint32_t parts = walk_parts(world, channels, max_tokens);
-  return parts == 1 ? 0 : uint64_t(world) * parts * channels * 2 * 4;
+// The launches for sixteen workers each follow one another and share it.
+uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, const uint32_t* tokens) {
+  uint64_t bytes = 0;
+  for (uint32_t g = 0; g < world; g += kGroup) {
+    const uint32_t n = std::min(world - g, kGroup);
+    bool cut = false;
+    for (uint32_t w = 0; w < n; ++w) cut = cut || tokens[g + w] / kShortest > 1;
+    if (cut) bytes = std::max(bytes, uint64_t(most_parts(n, channels, tokens + g)) * channels * 8);
+  }
+  return bytes;
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s) {

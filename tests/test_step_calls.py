@@ -131,6 +131,11 @@ def test_recurrence_workspaces_serve_fewer_tokens():
         tokens = sorted(int(2 ** rng.uniform(0, 25)) for _ in range(30))
         sizes = [plan.recurrence_workspace(channels, [n] * plan.cfg.world) for n in tokens]
         assert sizes == sorted(sizes)
+        each = [int(2 ** rng.uniform(0, 16)) for _ in range(plan.cfg.world)]
+        for _ in range(20):
+            fewer = [rng.randint(0, n) for n in each]
+            assert plan.recurrence_workspace(channels, fewer) <= plan.recurrence_workspace(channels, each)
+            each = fewer if rng.random() < 0.3 else each
         plan.close()
 
 
