@@ -160,6 +160,9 @@ constexpr int kBlock = LANES + (PHASE == kWhole ? 64 : 0);
 template <bool BF16, int KIND, int PHASE, int LANES, int HELD, int EXTRA>
 __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_distillation(DistillationArgs a) {
   constexpr int N = kPiece<BF16>, ES = BF16 ? 2 : 4, V = HELD / N, X = EXTRA / N, kWaves = LANES / 64;
+  // fp32 rows that are held are read past the caches: 103.7 and 101.0 us at 8 workers x 256 rows x 30522, 73.2 and 68.7 at
+  // 8 x 1024 x 5000; bf16 ones (8 x 512 x 30522: 108.4 and 109.0; 8 x 512 x 5000: 23.3 and 25.7) are not
+  constexpr bool kPast = !BF16 && PHASE == kWhole;
   constexpr bool kKeep = KIND != kTwo;  // exponentials stay; else distances
   __shared__ float waves[kWaves][3];
   __shared__ Lesson lesson;
@@ -209,7 +212,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
       for (int i = 0; i < X; i += kBatch) {
         u32x4 raw[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) raw[b] = in.get(col + uint32_t(V + i + b) * LANES * N);
+        for (int b = 0; b < kBatch; ++b) raw[b] = in.template get<kPast>(col + uint32_t(V + i + b) * LANES * N);
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
           float y[N];
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
     {
       u32x4 raw[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) raw[i] = in.get(col + uint32_t(i) * LANES * N);
+      for (int i = 0; i < V; ++i) raw[i] = in.template get<kPast>(col + uint32_t(i) * LANES * N);
       if (in.odd() && lane == 0) odd = bf16_low(in.get_last());
 #pragma unroll
       for (int i = 0; i < V; ++i) {

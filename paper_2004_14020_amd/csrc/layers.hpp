@@ -139,7 +139,8 @@ struct NormArgs {
   uint32_t width;
   uint64_t pitch;  // of all rows, elements
   float eps;
-  double inverse_width;  // made by the launch
+  double inverse_width;  // made by the launch, as is
+  bool stream;           // matrices are larger than the caches near the compute units
   bool bf16, gain_bf16, residual, checkpoint;
 };
 hipError_t launch_norm(const NormArgs& args, const AllBuffers<kNormBuffers>& v, hipStream_t s);
@@ -152,6 +153,7 @@ struct NormGradientArgs {
   uint32_t width;
   uint64_t pitch;
   bool bf16, gain_bf16, dsum, accumulate;  // gain_bf16: the plan's dtype, of gain and its gradient
+  bool stream;  // made by the launch
   unsigned char* ws;
 };
 uint64_t norm_gradient_workspace(uint32_t world, uint32_t width, uint32_t max_tokens);

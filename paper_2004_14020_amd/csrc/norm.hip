@@ -27,9 +27,8 @@ struct Pieces {
   uint32_t last;
 
   static __device__ __forceinline__ uint32_t column(uint32_t lane, int v) { return (v * LANES + lane) * N; }
-  __device__ __forceinline__ void load(const Row<BF16>& row, uint32_t lane) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) raw[v] = row.get(column(lane, v));
+  __device__ __forceinline__ void load(const Row<BF16>& row, uint32_t lane, bool stream) {
+    row.get_all(lane * N, LANES * N, stream, raw);
     if (row.odd()) last = row.get_last();
   }
   // before the first use of an odd row's values
@@ -41,10 +40,11 @@ struct Pieces {
   }
 };
 
-template <bool BF16, bool STREAM>
-__device__ __forceinline__ void store_piece(const Row<BF16>& row, uint32_t col, const float* v) {
+template <bool BF16>
+__device__ __forceinline__ void store_piece(const Row<BF16>& row, uint32_t col, const float* v, bool stream) {
   const u32x4 raw = narrow<BF16>(v);
-  row.template put<STREAM>(col, raw);
+  if (stream) row.template put<true>(col, raw);
+  else row.template put<false>(col, raw);
   if (row.odd()) row.put_last(col, raw);
 }
 
@@ -100,6 +100,12 @@ __device__ __forceinline__ float rstd_of(double sum, double inverse_width, float
   return float(m == __builtin_inf() ? 0.0 : r);
 }
 
+// Of matrices of so many bytes a call reads and writes past the caches what nobody reads again soon, so that what somebody does stays
+// there: y, and dx.  Forward, 8 workers x 4096 rows x 1024 bf16: 49.6 us where all go through the caches, 43.7 with x, the residual and
+// the sum past them, 45.7 with y past them too (with an 8-bit copy of y, which reads it again, 92.4, 83.2 and 90.8); its gradient 48.1
+// and 39.7.  Of smaller matrices the inputs are in the caches as often as not: gradient 19.0 us and 20.1 at 8 x 1500 x 1024, 25.6
+// and 23.2 at 8 x 2048 x 1024.
+constexpr uint64_t kLarge = uint64_t(28) << 20;
 constexpr uint32_t kGridGroups = 1u << 20;  // workgroups along x: a grid has less than 2^32 lanes in a direction
 
 // V pieces a lane, TEAM wavefronts to a row.
@@ -116,8 +122,8 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
   using P = Pieces<BF16, V, LANES>;
   const Row<BF16> rx(a.w.at[kNormX][w] + at, a.width), rr(a.w.at[kNormResidual][w] + at, a.width);
   P x, r;
-  x.load(rx, lane);
-  if (a.residual) r.load(rr, lane);
+  x.load(rx, lane, a.stream);
+  if (a.residual) r.load(rr, lane, a.stream);
   const Gains<BF16, V, LANES> gain(a.w.at[kNormGain][w], a.gain_bf16, a.width, lane);
   x.finish(rx, lane);
   float h[V][N];
@@ -135,7 +141,7 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
         h[v][j] += y[j];
         if constexpr (BF16) h[v][j] = bf16_low(bf16_pair(h[v][j], 0.0f));
       }
-      store_piece<BF16, false>(rs, P::column(lane, v), h[v]);
+      store_piece<BF16>(rs, P::column(lane, v), h[v], a.stream);
     }
   }
   double ss = 0.0;
@@ -153,7 +159,7 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm(NormArgs a) {
     gain.get(v, g);
 #pragma unroll
     for (int j = 0; j < N; ++j) h[v][j] = (h[v][j] * rstd) * g[j];
-    store_piece<BF16, false>(ry, P::column(lane, v), h[v]);
+    store_piece<BF16>(ry, P::column(lane, v), h[v], false);
   }
 }
 
@@ -188,9 +194,9 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
     const Row<BF16> rx(a.w.at[kNormGradX][w] + at, a.width), ry(a.w.at[kNormGradDy][w] + at, a.width);
     const Row<BF16> rd(a.w.at[kNormGradDsum][w] + at, a.width), ro(a.w.at[kNormGradDx][w] + at, a.width);
     P x, y, d;
-    x.load(rx, lane);
-    y.load(ry, lane);
-    if (a.dsum && !kLate) d.load(rd, lane);
+    x.load(rx, lane, a.stream);
+    y.load(ry, lane, a.stream);
+    if (a.dsum && !kLate) d.load(rd, lane, a.stream);
     const float r = reinterpret_cast<const CARAMEL_GLOBAL float*>(a.w.at[kNormGradRstd][w])[row];
     x.finish(rx, lane);
     y.finish(ry, lane);
@@ -234,7 +240,7 @@ __global__ void __launch_bounds__(TEAM <= 4 ? 256 : 1024) k_norm_gradient(NormGr
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) o[j] = __builtin_fmaf(r, __builtin_fmaf(-(n[j] * r), c, u[j] * g[j]), o[j]);
-      store_piece<BF16, false>(ro, P::column(lane, v), o);
+      store_piece<BF16>(ro, P::column(lane, v), o, false);
     }
   }
   // the workgroup's teams, one piece of every lane after the other
@@ -344,6 +350,7 @@ hipError_t launch_norm(const NormArgs& all, const AllBuffers<kNormBuffers>& v, h
   if (all.max_tokens == 0) return hipSuccess;
   NormArgs args = all;
   args.inverse_width = 1.0 / double(all.width);
+  args.stream = uint64_t(all.all) * all.max_tokens * all.width * (all.bf16 ? 2 : 4) >= kLarge;
   const hipError_t e = in_groups(args, v, [&](const NormArgs& a, uint32_t) {
     auto rows = [&](auto bf16, auto shape) {
       constexpr int V = decltype(shape)::kV, TEAM = decltype(shape)::kTeam;
@@ -376,7 +383,9 @@ uint64_t norm_gradient_workspace(uint32_t world, uint32_t width, uint32_t max_to
   return uint64_t(world) * norm_parts(world, max_tokens) * width * 4;
 }
 
-hipError_t launch_norm_gradient(const NormGradientArgs& args, const AllBuffers<kNormGradBuffers>& v, hipStream_t s) {
+hipError_t launch_norm_gradient(const NormGradientArgs& all, const AllBuffers<kNormGradBuffers>& v, hipStream_t s) {
+  NormGradientArgs args = all;
+  args.stream = uint64_t(all.all) * all.max_tokens * all.width * (all.bf16 ? 2 : 4) >= kLarge;
   const uint32_t parts = norm_parts(args.all, args.max_tokens), span = std::max(1u, (args.max_tokens + parts - 1) / parts);
   const uint64_t stride = uint64_t(parts) * args.width;
   return in_groups(args, v, [&](NormGradientArgs a, uint32_t g) {

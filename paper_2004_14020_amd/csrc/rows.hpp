@@ -24,8 +24,20 @@ struct Row {
   __device__ __forceinline__ bool odd() const { return BF16 && columns % 2; }
 
   // 16 bytes from column `col` on
+  template <bool STREAM = false>
   __device__ __forceinline__ u32x4 get(uint32_t col) const {
-    return __builtin_amdgcn_raw_buffer_load_b128(at, int(col * ES), 0, 0);
+    return __builtin_amdgcn_raw_buffer_load_b128(at, int(col * ES), 0, STREAM ? kStreaming : 0);
+  }
+  // V of them, `step` columns apart
+  template <int V>
+  __device__ __forceinline__ void get_all(uint32_t col, uint32_t step, bool stream, u32x4 (&v)[V]) const {
+    if (stream) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = get<true>(col + i * step);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = get<false>(col + i * step);
+    }
   }
   template <bool STREAM = false>
   __device__ __forceinline__ void put(uint32_t col, u32x4 v) const {
