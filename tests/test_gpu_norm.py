@@ -101,9 +101,10 @@ def test_norm(world, n, width, gap, dtype, gain_dtype, residual, saved):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
-@pytest.mark.parametrize("n,width,gap", [(4096, 1024, 0), (4099, 1000, 0), (2050, 4096, 0), (1100, 2048, 2), (9000, 130, 0), (300, 8192, 0)])
+@pytest.mark.parametrize("n,width,gap", [(4096, 1024, 0), (4099, 1000, 0), (2050, 4096, 0), (1100, 2048, 2), (9000, 130, 0), (300, 8192, 0),
+                                         (4200, 2049, 1), (8200, 1111, 0)])
 def test_norm_of_many_tokens(n, width, gap, dtype):
-    """As many blocks of 32 tokens as fill the GPU, whole and not."""
+    """As many blocks of 32 tokens as fill the GPU, whole and not; matrices of more than 28 MiB."""
     check_forward(2, n, width, gap, dtype, dtype, True, True, ns=[n, n - 37])
 
 
@@ -139,6 +140,8 @@ GRADIENT = [  # world, tokens, width, gap
     (1, 1, 1, 0), (2, 3, 2, 1), (3, 9, 7, 0), (8, 33, 9, 3), (64, 6, 40, 0), (1, 700, 64, 0), (2, 300, 255, 0), (20, 17, 513, 1),
     (2, 129, 1024, 0), (3, 40, 1025, 2), (2, 31, 2047, 1), (2, 33, 4096, 0), (1, 20, 4097, 3), (2, 9, 8191, 0), (1, 9, 16385, 1),
     (1, 4, 32768, 0), (2, 4100, 100, 0)]
+
+LARGE = [(2, 3700, 2049, 1), (3, 4900, 1024, 0)]   # more than 28 MiB of bf16
 
 
 @pytest.mark.parametrize("accumulate", [False, True], ids=["write", "add"])
@@ -180,6 +183,12 @@ def test_norm_gradient(world, n, width, gap, dtype, gain_dtype, with_dsum, accum
         dx[w][1].fill_(7.0)
         assert bool((dx[w][0] == 7.0).all())
     plan.close()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+@pytest.mark.parametrize("world,n,width,gap", LARGE)
+def test_norm_gradient_of_many_tokens(world, n, width, gap, dtype):
+    test_norm_gradient(world, n, width, gap, dtype, dtype, True, False)
 
 
 def test_norm_gradient_agrees_with_differences():

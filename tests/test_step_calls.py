@@ -1,7 +1,10 @@
 """The calls of a training step around the gradients: sizes and refusals.  No GPU call is made."""
 import ctypes as C
 import math
+import os
 import random
+import shutil
+import subprocess
 
 import pytest
 
@@ -10,6 +13,29 @@ import paper_2004_14020_amd as cm
 from test_layers_host import A, T, refused
 
 E = cm.binding.EINVAL
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_calls_allocate_nothing(tmp_path):
+    if shutil.which("gcc") is None:
+        pytest.skip("gcc not available")
+    exe, libdir = str(tmp_path / "step_alloc_check"), os.path.dirname(cm.binding.LIB_PATH)
+    subprocess.run(["gcc", "-std=gnu99", "-Wall", "-Wextra", "-Werror", "-I", os.path.join(ROOT, "include"),
+                    os.path.join(ROOT, "tests", "host", "step_alloc_check.c"), "-L", libdir, "-l:libcaramel.so",
+                    "-Wl,-rpath," + libdir, "-o", exe], check=True)
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0 and "step_alloc_check ok" in res.stdout, (res.returncode, res.stdout + res.stderr)
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
+def test_overlap_of_rows_of_different_pitch(tmp_path):
+    exe = str(tmp_path / "pitch_check")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan", "-I", os.path.join(ROOT, "include"), "-I",
+                    os.path.join(ROOT, "paper_2004_14020_amd", "csrc"), os.path.join(ROOT, "tests", "host", "pitch_check.cpp"), "-o", exe],
+                   check=True)
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "pitch_check ok" in res.stdout, res.stdout[-2000:] + res.stderr[-2000:]
 
 
 @pytest.fixture
