@@ -405,7 +405,7 @@ int caramel_residual_norm_gradient(caramel_plan* plan, uint32_t gain_tensor, con
  *   before, after        fp32 [sequences][channels], optional: the states in front of every sequence (NULL: zeros) and behind it; an
  *                        empty sequence's after is its before.  Sequences of one token with before and after are a step of serving.
  * States are carried in fp32 and rounded where they are stored.  What a sequence holds, infinities and NaN too, reaches no other.
- * EINVAL besides the above: more than 2^25 sequences at a worker. */
+ * EINVAL besides the above: more than 2^25 sequences at a worker, or any at one without tokens (whose states are not touched). */
 int caramel_recurrence_workspace(const caramel_plan* plan, uint64_t channels, const uint64_t* tokens, uint64_t* bytes);
 int caramel_recurrence(caramel_plan* plan, uint64_t channels, const uint64_t* tokens, const uint64_t* sequences,
                        const void* const* starts, uint32_t id_bytes, const void* const* gate, const void* const* input, uint32_t dtype,

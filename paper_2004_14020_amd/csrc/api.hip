@@ -1503,6 +1503,8 @@ int take_recurrence(caramel_plan* p, uint64_t channels, const uint64_t* tokens, 
   for (uint32_t w = 0; w < a.all; ++w) {
     if (sequences[w] > kMaxTokens)
       return fail(CARAMEL_EINVAL, "sequences[%u] = %llu is more than 2^25", w, (unsigned long long)sequences[w]);
+    if (sequences[w] && !v.tokens[w])
+      return fail(CARAMEL_EINVAL, "sequences[%u] = %llu, but the worker has no tokens", w, (unsigned long long)sequences[w]);
     v.more[w] = uint32_t(sequences[w]);
   }
   if (int rc = check_rows("pitch", pitch, channels, a.max_tokens)) return rc;

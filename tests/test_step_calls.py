@@ -113,7 +113,7 @@ FORWARD = dict(states=[4 * A, 5 * A], after=[6 * A, 7 * A])
 BACKWARD = dict(states=[4 * A, 5 * A], dstates=[6 * A, 7 * A], dgate=[8 * A, 9 * A], dinput=[8 * A + 64, 9 * A + 64],
                 dafter=[10 * A, 11 * A], dbefore=[12 * A, 13 * A])
 BOTH = [dict(channels=0), dict(channels=(1 << 20) + 1, pitch=1 << 22), dict(id_bytes=2), dict(dtype=2), dict(tokens=[T, 1]),
-        dict(sequences=[1, T]), dict(pitch=15), dict(pitch=(1 << 23) + 1), dict(states_pitch=15), dict(states_pitch=(1 << 23) + 1),
+        dict(sequences=[1, T]), dict(tokens=[3, 0]), dict(pitch=15), dict(pitch=(1 << 23) + 1), dict(states_pitch=15), dict(states_pitch=(1 << 23) + 1),
         dict(tokens=[1 << 25, 1], pitch=1 << 23), dict(starts=[A, None]), dict(starts=[A, A + 4]), dict(gate=[None, A]),
         dict(gate=[2 * A + 2, 3 * A]), dict(input=[None, 3 * A]), dict(before=[20 * A, None]), dict(before=[20 * A + 2, 21 * A]),
         dict(states=[4 * A, None]), dict(states=[4 * A + 2, 5 * A]), dict(tokens=[1000, 3]),
