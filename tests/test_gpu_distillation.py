@@ -81,7 +81,9 @@ KINDS = [(1.0, 1.0, 0.0), (1.0, 0.7, 0.5), (2.0, 1.0, 0.5), (4.0, 0.5, 1.0), (3.
 CASES = [  # world, tokens, vocab, top, gap
     (1, 1, 1, 1, 0), (2, 3, 2, 3, 1), (1, 5, 7, 2, 0), (3, 9, 100, 64, 3), (64, 4, 33, 5, 0), (20, 7, 1001, 65, 0), (2, 300, 777, 17, 1),
     (1, 6, 8191, 256, 0), (2, 5, 8192, 32, 0), (1, 3, 30522, 8, 0), (1, 1, 130001, 64, 1), (2, 40, 16387, 12, 5), (1, 250, 8195, 33, 0),
-    (1, 230, 30522, 32, 0), (2, 120, 32769, 16, 1), (1, 200, 65536, 7, 0), (1, 200, 70003, 100, 1)]
+    (1, 230, 30522, 32, 0), (2, 120, 32769, 16, 1), (1, 200, 65536, 7, 0), (1, 200, 70003, 100, 1),
+    # rows that registers do not hold, in parts: few of them, and as many as there may be
+    (1, 3, 61441, 8, 0), (2, 20, 70001, 64, 1), (1, 5, 61442, 256, 3), (1, 96, 61447, 3, 0), (1, 97, 61447, 3, 0)]
 
 
 def case_of(rng, world, n, vocab, top, gap, dtype, teacher_dtype, id_bytes):
@@ -174,7 +176,7 @@ def call(plan, z, ids, t, labels, T, soft, hard, dtype=cm.F32):
     return loss.cpu(), out.cpu()
 
 
-@pytest.mark.parametrize("vocab,n", [(50, 12), (9000, 12), (9000, 300), (70000, 250)])
+@pytest.mark.parametrize("vocab,n", [(50, 12), (9000, 12), (9000, 300), (70000, 250), (70000, 12)])
 @pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
 @pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
 def test_extreme_logits(dtype, T, vocab, n):
@@ -270,7 +272,7 @@ def test_no_tokens_and_logits_more_than_four_gib_apart():
     plan.close()
 
 
-@pytest.mark.parametrize("n,vocab", [(5, 20000), (300, 500)])
+@pytest.mark.parametrize("n,vocab", [(5, 20000), (300, 500), (5, 70000)])
 def test_distillation_captured_into_a_graph(n, vocab):
     """Replayed three times, with new inputs and eager calls of the same buffers in between."""
     W, top = 2, 9
