@@ -165,6 +165,7 @@ class Plan:
         self._h = C.c_void_p()
         self.cfg = Config(world, dtype, batch_threshold_bytes, split_mode, max_depth, split_bytes,
                           align_bytes, num_streams, pattern, 0)
+        self._arrays = {}                                     # array types of one entry per worker
         self.n_tensors = len(elems)
         self.elems = [int(e) for e in elems]
         arr = (C.c_uint64 * max(1, len(elems)))(*[int(e) for e in elems])
@@ -290,7 +291,10 @@ class Plan:
     def _per_worker(self, kind, values, name):
         if len(values) != self.cfg.world:
             raise ValueError(f"{name} must have one entry per worker")
-        return (kind * self.cfg.world)(*values)
+        array = self._arrays.get(kind)                        # making the type takes longer than filling it
+        if array is None:
+            array = self._arrays[kind] = kind * self.cfg.world
+        return array(*values)
 
     def _outputs(self, weight: int, features: int) -> int:
         if not 0 <= weight < self.n_tensors or features < 1:

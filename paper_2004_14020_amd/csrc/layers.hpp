@@ -175,6 +175,7 @@ struct RecurrenceArgs {
   uint32_t span, first_part[kGroup + 1];
   bool cut;    // a worker has more than one
   bool lines;  // rows are whole cache lines
+  uint32_t steps;  // not 0: sequences are short, and there are so many at a worker at most
 };
 uint64_t recurrence_workspace_bytes(uint32_t world, uint32_t channels, const uint32_t* tokens);
 hipError_t launch_recurrence(const RecurrenceArgs& args, const AllBuffers<kRecBuffers>& v, hipStream_t s);

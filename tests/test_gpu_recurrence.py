@@ -82,7 +82,10 @@ CASES = [  # world, tokens, channels, sequences, kind, gap
     (64, 6, 7, 2, "random", 0), (1, 513, 300, 1, "even", 0), (1, 1500, 64, 1, "even", 0), (2, 1100, 40, 3, "random", 3),
     (1, 1300, 70, 90, "random", 0), (1, 700, 20, 300, "random", 0), (1, 1000, 17, 5, "gaps", 0), (1, 900, 1, 4, "random", 0),
     (1, 2000, 9, 20, "empty", 0), (2, 640, 24, 5, "even", 0), (1, 500, 12, 500, "steps", 0), (1, 70, 6, 63, "random", 0),
-    (1, 130, 6, 64, "random", 0), (1, 600, 260, 5, "random", 0)]
+    (1, 130, 6, 64, "random", 0), (1, 600, 260, 5, "random", 0),
+    # two tokens or less to a sequence
+    (2, 65, 127, 60, "random", 1), (1, 100, 5, 90, "gaps", 2), (3, 64, 130, 9, "empty", 1), (1, 1024, 66, 600, "random", 0),
+    (20, 40, 40, 40, "steps", 0), (1, 30, 1, 30, "random", 0), (64, 3, 256, 3, "steps", 0), (1, 2, 300, 1, "even", 0)]
 
 
 def tokens_of(world, n):
