@@ -177,8 +177,8 @@ DIST = dict(vocab=16, tokens=[3, 3], logits=[A, 2 * A], teacher_ids=[3 * A, 4 * 
     dict(pitch=(1 << 23) + 1), dict(dlogits_pitch=15), dict(tokens=[1 << 25, 1], pitch=1 << 23), dict(logits=[None, A]),
     dict(logits=[A + 2, 2 * A]), dict(teacher_ids=[3 * A, None]), dict(teacher_ids=[3 * A + 4, 4 * A]), dict(teacher_logits=[None, A]),
     dict(teacher_logits=[5 * A + 2, 6 * A]), dict(labels=[9 * A, None]), dict(labels=[9 * A + 4, 10 * A]), dict(loss=[None, 8 * A]),
-    dict(loss=[7 * A + 2, 8 * A]), dict(dlogits=[11 * A, None]), dict(dlogits=[11 * A + 1, 12 * A]), dict(vocab=10000, pitch=10000),
-    dict(vocab=10000, ws=20 * A + 8, ws_bytes=1 << 20), dict(vocab=10000, ws=20 * A, ws_bytes=64),
+    dict(loss=[7 * A + 2, 8 * A]), dict(dlogits=[11 * A, None]), dict(dlogits=[11 * A + 1, 12 * A]), dict(vocab=61448, pitch=61448),
+    dict(vocab=61448, ws=20 * A + 8, ws_bytes=1 << 20), dict(vocab=61448, ws=20 * A, ws_bytes=64),
     # what is written overlaps: the other worker's, inputs; the logits with another pitch or place than theirs
     dict(dlogits=[11 * A, 11 * A]), dict(dlogits=[3 * A, 12 * A]), dict(loss=[7 * A, 7 * A]), dict(loss=[A, 8 * A]),
     dict(dlogits=[2 * A, A]), dict(dlogits=[A, 2 * A], dlogits_pitch=17), dict(dlogits=[A + 64, 2 * A]),
