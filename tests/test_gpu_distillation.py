@@ -83,7 +83,7 @@ CASES = [  # world, tokens, vocab, top, gap
     (1, 6, 8191, 256, 0), (2, 5, 8192, 32, 0), (1, 3, 30522, 8, 0), (1, 1, 130001, 64, 1), (2, 40, 16387, 12, 5), (1, 250, 8195, 33, 0),
     (1, 230, 30522, 32, 0), (2, 120, 32769, 16, 1), (1, 200, 65536, 7, 0), (1, 200, 70003, 100, 1),
     # rows that registers do not hold, in parts: few of them, and as many as there may be
-    (1, 3, 61441, 8, 0), (2, 20, 70001, 64, 1), (1, 5, 61442, 256, 3), (1, 96, 61447, 3, 0), (1, 97, 61447, 3, 0)]
+    (1, 3, 61441, 8, 0), (2, 20, 70001, 64, 1), (1, 5, 61442, 256, 3), (1, 96, 61447, 3, 0), (1, 97, 61447, 3, 0), (20, 4, 61443, 5, 0)]
 
 
 def case_of(rng, world, n, vocab, top, gap, dtype, teacher_dtype, id_bytes):

@@ -283,7 +283,7 @@ def test_recurrence_gradient_agrees_with_differences():
     plan.close()
 
 
-@pytest.mark.parametrize("n", [40, 3000])
+@pytest.mark.parametrize("n", [9, 40, 3000])
 def test_recurrence_calls_captured_into_a_graph(n):
     """Replayed three times, with new inputs and starts and eager calls of the same buffers in between."""
     ch, S, W = 33, 6, 2
