@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -128,7 +129,8 @@ def lib() -> C.CDLL:
     L.caramel_version.argtypes = []
     L.caramel_allreduce_loop.argtypes = [P, P, C.c_uint32, C.POINTER(C.c_double), C.POINTER(C.c_double)]
     L.caramel_stream_probe.argtypes = [C.c_uint32, C.POINTER(P), C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, P]
-    U32, U64, PU64, PP = C.c_uint32, C.c_uint64, C.POINTER(C.c_uint64), C.POINTER(P)
+    U32, U64 = C.c_uint32, C.c_uint64
+    PU64 = PP = P                                             # lists of numbers and of pointers come as bytes or as arrays
     L.caramel_embedding_lookup.argtypes = [P, PP, U64, U64, C.c_float, PP, U32, PU64, PP, U64, P]
     L.caramel_embedding_workspace.argtypes = [P, U32, U64, PU64, PU64]
     L.caramel_embedding_gradient.argtypes = [P, U32, U64, C.c_float, PP, U32, PU64, PP, U32, U64, C.c_int, P, U64, P]
@@ -165,7 +167,6 @@ class Plan:
         self._h = C.c_void_p()
         self.cfg = Config(world, dtype, batch_threshold_bytes, split_mode, max_depth, split_bytes,
                           align_bytes, num_streams, pattern, 0)
-        self._arrays = {}                                     # array types of one entry per worker
         self.n_tensors = len(elems)
         self.elems = [int(e) for e in elems]
         arr = (C.c_uint64 * max(1, len(elems)))(*[int(e) for e in elems])
@@ -177,6 +178,7 @@ class Plan:
             rt = (C.c_double * max(1, len(elems)))(*[float(t) for t in ready_time])
             _check(lib().caramel_plan_create_timed(C.byref(self.cfg), arr, len(elems), rt, float(net_a),
                                                    float(net_b), C.byref(self._h)))
+        self._pack = struct.Struct(f"{world}Q").pack
 
     # -- lifetime
     def close(self) -> None:
@@ -291,10 +293,10 @@ class Plan:
     def _per_worker(self, kind, values, name):
         if len(values) != self.cfg.world:
             raise ValueError(f"{name} must have one entry per worker")
-        array = self._arrays.get(kind)                        # making the type takes longer than filling it
-        if array is None:
-            array = self._arrays[kind] = kind * self.cfg.world
-        return array(*values)
+        try:
+            return self._pack(*values)                        # a fraction of the time of making an array
+        except struct.error:                                  # of pointers, None among them
+            return (kind * self.cfg.world)(*values)
 
     def _outputs(self, weight: int, features: int) -> int:
         if not 0 <= weight < self.n_tensors or features < 1:

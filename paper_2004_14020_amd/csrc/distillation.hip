@@ -8,10 +8,13 @@
 // All exponentials are 2^(d log2(e) / T) of the distance d <= 0 to the row's largest logit.  Where T is 1, Q and q are one; where it
 // is 2 or 4, an exponential of q is that of Q squared, once or twice.
 //
-// A row is read once: a workgroup holds it in registers, as numbers, then as distances or exponentials.  What does not fit (more than
-// 65536 logits) is read again for the gradient.  The gradient is written as if there were no teacher; behind a barrier the few logits
-// that the teacher or the label names are written once more.  With few rows, each is cut into parts: one launch leaves every part's
-// largest logit and sums, and the next one joins them.
+// A row is read once: a workgroup holds it in registers, as numbers, then as distances or exponentials, and a part of a long one in LDS.
+// What does not fit (from 115200 bf16 or 130560 fp32 logits on) is read again for the gradient.  The gradient is written as if there were no
+// teacher; behind a barrier the few logits that the teacher or the label names are written once more.  Where few rows do not fit registers, each
+// is cut into parts: one launch leaves every part's largest logit and sums, and the next one joins them.
+//
+// Bound by memory and by how much of a workgroup's reading, computing and writing lies beside another's: 8 workers x 512 rows x 30522 bf16
+// logits, T = 2 with labels, 105 us, 4.8 TB/s (a copy of 1 GiB: 6.08); the vector units are busy about half of that time.
 #include <algorithm>
 
 #include "layers.hpp"
