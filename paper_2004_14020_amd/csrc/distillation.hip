@@ -4,7 +4,10 @@
 //   loss = soft sum_k P_k (ln P_k - ln Q_id(k)) + hard (- ln q_label)
 //   dz_j = scale (soft / T (Q_j - sum of P_k with id(k) = j) + hard (q_j - [j = label]))
 //
-// ln P_k = (t_k - max t) / T - ln sum: no logarithm but of sums, which is taken in 64 bits, as the few products of the loss are.
+// ln P_k = (t_k - max t) / T - ln sum: no logarithm but of sums, which are fp32, as the exponentials are.  What else the loss is made of is added up
+// in 64 bits: distances between logits, never logits, weighted by the teacher's exponentials over their sum, so that the weights add up to 1 and
+// nothing hangs on what all logits have in common (with weights rounded to fp32, whose sum is off by 1e-7 or so, the loss was off by as much of the
+// largest logit over T: by 0.1 next to logits of 10^6).
 // All exponentials are 2^(d log2(e) / T) of the distance d <= 0 to the row's largest logit.  Where T is 1, Q and q are one; where it
 // is 2 or 4, an exponential of q is that of Q squared, once or twice.
 //
@@ -38,18 +41,20 @@ __device__ __forceinline__ uint32_t known(uint64_t id, uint32_t vocab) { return 
 
 __device__ __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// The natural logarithm of a sum, whose exponent is taken apart: the rest is in [1/2, 1), and its logarithm off by 2^-25 at most.
+// The natural logarithm of a sum, whose exponent is taken apart: the rest is in [1/2, 1), and its logarithm off by less than 2^-23 (measured over
+// all of these numbers: 1.54 * 2^-24).
 __device__ __forceinline__ double ln(float v) {
   return double(__builtin_amdgcn_frexp_expf(v)) * 0.69314718055994531 + double(logf(__builtin_amdgcn_frexp_mantf(v)));
 }
 
 // What a row's teacher and label ask for: of entry k (the label: entry `top`) its id, the student's logit there, and what is taken
-// from the gradient there; taught: the loss without the logarithms of sums over the vocabulary; terms: bit 0 the teacher's, bit 1
-// the label's.
+// from the gradient there; best: the largest logit that the teacher asks for; taught: the loss without the logarithms of sums over the
+// vocabulary, as if best were the row's largest logit; terms: bit 0 the teacher's, bit 1 the label's.
 struct Lesson {
   uint32_t id[kEntries];
   float logit[kEntries], weight[kEntries];
   uint32_t terms;
+  float best;
   double taught;
 };
 
@@ -99,23 +104,29 @@ struct Student {
     }
     most = wave_max(most);
     const bool has_teacher = a.soft > 0.0f && (__ballot(any) || __ballot(bad));
-    float p[kEach], total = 0.0f;
+    float p[kEach], total = 0.0f, best = kLowest;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       p[i] = 0.0f;
       if (uint32_t(i) * 64 >= a.top) continue;
       if (has_teacher && t[i] != -__builtin_inff()) p[i] = exp2((t[i] - most) * a.warm_rate);
       total += p[i];
+      best = fmaxf(best, p[i] != 0.0f ? v[i] : kLowest);
     }
     total = wave_sum(total);
-    double part = 0.0;  // sum of P (ln P - z / T), with ln P but for the sum's logarithm
+    best = wave_max(best);
+    // sums of the exponentials, and of their products with T (ln P - ln Q) but for the logarithms of sums; best is never -infinity, so a logit
+    // of -infinity makes the loss infinite, not NaN
+    double part = 0.0, whole = 0.0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const uint32_t k = i * 64 + lane;
       if (uint32_t(i) * 64 >= a.top) continue;
+      if (p[i] != 0.0f) {
+        part += double(p[i]) * ((double(t[i]) - double(most)) - (double(v[i]) - double(best)));
+        whole += double(p[i]);
+      }
       p[i] /= total;
-      if (id[i] != kNone && p[i] != 0.0f && has_teacher)
-        part += double(p[i]) * ((double(t[i]) - double(most)) - double(v[i])) * a.inverse;
       if (k < a.top) {
         out.id[k] = has_teacher ? id[i] : kNone;
         out.logit[k] = v[i];
@@ -123,12 +134,14 @@ struct Student {
       }
     }
     part = wave_sum(part);
+    whole = wave_sum(whole);
     if (lane == 0) {
       out.id[a.top] = label;
       out.logit[a.top] = label_logit;
       out.weight[a.top] = a.hard;
       out.terms = (has_teacher ? 1u : 0u) | (label != kNone ? 2u : 0u);
-      out.taught = has_teacher ? part - ln(total) : 0.0;
+      out.best = best;
+      out.taught = has_teacher ? part / whole * a.inverse - ln(total) : 0.0;
     }
   }
 };
@@ -288,6 +301,7 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
       }
       if (lane == 0) {
         lesson.terms = kept->terms;
+        lesson.best = kept->best;
         lesson.taught = kept->taught;
       }
       largest = wave_max(m);
@@ -424,7 +438,8 @@ __global__ void __launch_bounds__((kBlock<PHASE, LANES>), HELD <= 32 ? 8 : 4) k_
     if (PHASE == kWhole ? lane == LANES : lane == 0 && blockIdx.y == 0) {
       double loss = 0.0;
       if (has_teacher)
-        loss += double(a.soft) * (lesson.taught + double(largest) * a.inverse + (ln(warm) - double(from.warm_rest) * 0.69314718055994531));
+        loss += double(a.soft) * (lesson.taught + (double(largest) - double(lesson.best)) * a.inverse +
+                                  (ln(warm) - double(from.warm_rest) * 0.69314718055994531));
       if (has_label)
         loss += double(a.hard) *
                 ((ln(cold) - double(from.cold_rest) * 0.69314718055994531) - (double(lesson.logit[a.top]) - double(largest)));
