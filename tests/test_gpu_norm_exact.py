@@ -1,11 +1,11 @@
-"""Where the norm's results are known to the last bit: 1 / sqrt of a mean square that is exact in 64 bits, or nearly."""
+"""Where the norm's results are known to the last bit: 1 / sqrt of a mean square that is exact in 64 bits or nearly, and sums of small whole numbers."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2004_14020_amd as cm
 
-from layer_util import DEV, stream
+from layer_util import DEV, bound_plan, stream, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,29 @@ def test_rstd_next_to_where_two_numbers_meet(side):
     near = np.abs(1 / np.sqrt(m.astype(np.longdouble)) / middle - 1)
     assert np.median(near) < np.longdouble(2) ** -45
     check(rstd_of(x, float(eps)), m.astype(np.longdouble))
+
+
+@pytest.mark.parametrize("dtype", [cm.F32, cm.BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,width", [(4 * (1 << 20) + 4 * 777 + 3, 4), (600_001, 9), (50_001, 1030), (20_000, 4100)])
+def test_every_row_counts_once_in_the_gains_gradient(n, width, dtype):
+    """rstd = 1 and whole numbers, none of which is 0 or below, with a sum below 2^24: exact in fp32 in any order, so that no row is lost and none
+    counted twice."""
+    plan, grads = bound_plan(1, [width], cm.F32)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    t = torch.float32 if dtype == cm.F32 else torch.bfloat16
+    x = torch.randint(1, 3, (n, width), device=DEV, generator=g).to(t)
+    dy = torch.ones_like(x)
+    some = torch.randint(0, n, (1000,), device=DEV, generator=g)
+    dy[some] = torch.randint(1, 9, (1000, width), device=DEV, generator=g).to(t)
+    gain, rstd, dx = torch.ones(width, device=DEV), torch.ones(n, device=DEV), torch.empty_like(x)
+    want = sum((x[i:i + (1 << 20)].double() * dy[i:i + (1 << 20)].double()).sum(0) for i in range(0, n, 1 << 20))
+    assert float(want.max()) < 2 ** 24
+    for accumulate in (False, True):
+        need = plan.residual_norm_workspace(0, [n])
+        ws = workspace(need)
+        plan.residual_norm_gradient(0, [gain.data_ptr()], [n], [x.data_ptr()], [rstd.data_ptr()], [dy.data_ptr()], [dx.data_ptr()],
+                                    ws.data_ptr(), need, dtype=dtype, accumulate=accumulate, stream=stream())
+        torch.cuda.synchronize()
+        assert torch.equal(grads[0][0].double(), want * (2 if accumulate else 1))
+    plan.close()
