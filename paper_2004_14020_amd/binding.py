@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+from numbers import Integral
+from operator import countOf
 from typing import List, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -178,6 +180,7 @@ class Plan:
             rt = (C.c_double * max(1, len(elems)))(*[float(t) for t in ready_time])
             _check(lib().caramel_plan_create_timed(C.byref(self.cfg), arr, len(elems), rt, float(net_a),
                                                    float(net_b), C.byref(self._h)))
+        self._world = self.cfg.world
         self._pack = struct.Struct(f"{world}Q").pack
 
     # -- lifetime
@@ -291,12 +294,15 @@ class Plan:
 
     # -- filling the gradient tensors: one device address and one token count per worker
     def _per_worker(self, kind, values, name):
-        if len(values) != self.cfg.world:
+        if len(values) != self._world:
             raise ValueError(f"{name} must have one entry per worker")
         try:
-            return self._pack(*values)                        # a fraction of the time of making an array
-        except struct.error:                                  # of pointers, None among them
-            return (kind * self.cfg.world)(*values)
+            # (a tensor of one element packs too, as what it holds, which is no address)
+            if kind is C.c_uint64 or countOf(map(type, values), int) == self._world or all(isinstance(v, Integral) for v in values):
+                return self._pack(*values)                    # a fraction of the time of making an array
+        except struct.error:
+            pass
+        return (kind * self._world)(*values)                  # None among them, or nothing that is an address
 
     def _outputs(self, weight: int, features: int) -> int:
         if not 0 <= weight < self.n_tensors or features < 1:
