@@ -131,8 +131,14 @@ def lib() -> C.CDLL:
     L.caramel_version.argtypes = []
     L.caramel_allreduce_loop.argtypes = [P, P, C.c_uint32, C.POINTER(C.c_double), C.POINTER(C.c_double)]
     L.caramel_stream_probe.argtypes = [C.c_uint32, C.POINTER(P), C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, P]
-    U32, U64 = C.c_uint32, C.c_uint64
-    PU64 = PP = P                                             # lists of numbers and of pointers come as bytes or as arrays
+    _lists_of_workers(L, C.POINTER(C.c_uint64), C.POINTER(P))
+    _lib = L
+    return L
+
+
+def _lists_of_workers(L: C.CDLL, PU64, PP) -> None:
+    """Argument types of the calls that take a count or an address of every worker, for lists of these types."""
+    P, F, U32, U64 = C.c_void_p, C.c_float, C.c_uint32, C.c_uint64
     L.caramel_embedding_lookup.argtypes = [P, PP, U64, U64, C.c_float, PP, U32, PU64, PP, U64, P]
     L.caramel_embedding_workspace.argtypes = [P, U32, U64, PU64, PU64]
     L.caramel_embedding_gradient.argtypes = [P, U32, U64, C.c_float, PP, U32, PU64, PP, U32, U64, C.c_int, P, U64, P]
@@ -147,11 +153,23 @@ def lib() -> C.CDLL:
     L.caramel_recurrence_workspace.argtypes = [P, U64, PU64, PU64]
     L.caramel_recurrence.argtypes = [P, U64, PU64, PU64, PP, U32, PP, PP, U32, U64, PP, PP, U64, PP, P, U64, P]
     L.caramel_recurrence_gradient.argtypes = [P, U64, PU64, PU64, PP, U32, PP, PP, U32, U64, PP, PP, PP, U64, PP, PP, PP, PP, P, U64, P]
-    F = C.c_float
     L.caramel_distillation_workspace.argtypes = [P, U64, U32, PU64, PU64]
     L.caramel_distillation.argtypes = [P, U64, PU64, PP, U32, U64, PP, PP, U32, PP, U32, U32, F, F, F, F, PP, PP, U64, P, U64, P]
-    _lib = L
-    return L
+
+
+_packed = None
+
+
+def packed() -> C.CDLL:
+    """The library for Plan's own calls, whose lists of every worker's count or address may also be bytes.  (From `lib` they are arrays of the right
+    type, which is checked; bytes are made in a fraction of an array's time.)"""
+    global _packed
+    if _packed is None:
+        lib()
+        L = C.CDLL(LIB_PATH)
+        _lists_of_workers(L, C.c_void_p, C.c_void_p)
+        _packed = L
+    return _packed
 
 
 def _check(status: int) -> None:
@@ -313,15 +331,15 @@ class Plan:
                          out: Sequence[int], scale: float = 1.0, id_bytes: int = 8, out_pitch: Optional[int] = None,
                          stream: int = 0) -> None:
         per = self._per_worker
-        _check(lib().caramel_embedding_lookup(
+        _check(packed().caramel_embedding_lookup(
             self._h, per(C.c_void_p, table, "table"), vocab, width, scale, per(C.c_void_p, ids, "ids"), id_bytes,
             per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, out, "out"), width if out_pitch is None else out_pitch, stream))
 
     def embedding_workspace(self, tensor: int, width: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that embedding_gradient needs for these sizes."""
         n = C.c_uint64()
-        _check(lib().caramel_embedding_workspace(self._h, tensor, width, self._per_worker(C.c_uint64, tokens, "tokens"),
-                                                 C.byref(n)))
+        _check(packed().caramel_embedding_workspace(self._h, tensor, width, self._per_worker(C.c_uint64, tokens, "tokens"),
+                                                    C.byref(n)))
         return n.value
 
     def embedding_gradient(self, tensor: int, width: int, ids: Sequence[int], tokens: Sequence[int], dy: Sequence[int],
@@ -329,7 +347,7 @@ class Plan:
                            dy_pitch: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
         """dy_dtype None: the plan's."""
         per = self._per_worker
-        _check(lib().caramel_embedding_gradient(
+        _check(packed().caramel_embedding_gradient(
             self._h, tensor, width, scale, per(C.c_void_p, ids, "ids"), id_bytes, per(C.c_uint64, tokens, "tokens"),
             per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype, width if dy_pitch is None else dy_pitch,
             int(accumulate), ws, ws_bytes, stream))
@@ -337,7 +355,7 @@ class Plan:
     def checkpoint_store(self, x: Sequence[int], tokens: Sequence[int], features: int, checkpoint: Sequence[int],
                          dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
         per = self._per_worker
-        _check(lib().caramel_checkpoint_store(
+        _check(packed().caramel_checkpoint_store(
             self._h, per(C.c_uint64, tokens, "tokens"), features, per(C.c_void_p, x, "x"),
             self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch,
             per(C.c_void_p, checkpoint, "checkpoint"), stream))
@@ -345,15 +363,15 @@ class Plan:
     def checkpoint_load(self, checkpoint: Sequence[int], tokens: Sequence[int], features: int, x: Sequence[int],
                         dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
         per = self._per_worker
-        _check(lib().caramel_checkpoint_load(
+        _check(packed().caramel_checkpoint_load(
             self._h, per(C.c_uint64, tokens, "tokens"), features, per(C.c_void_p, checkpoint, "checkpoint"),
             per(C.c_void_p, x, "x"), self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch, stream))
 
     def weight_gradient_workspace(self, weight: int, features: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that weight_gradient needs for these sizes (may be 0)."""
         n = C.c_uint64()
-        _check(lib().caramel_weight_gradient_workspace(self._h, weight, features,
-                                                       self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        _check(packed().caramel_weight_gradient_workspace(self._h, weight, features,
+                                                          self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
         return n.value
 
     def weight_gradient(self, weight: int, bias: Optional[int], checkpoint: Sequence[int], tokens: Sequence[int],
@@ -363,7 +381,7 @@ class Plan:
         per = self._per_worker
         if bias is not None and not 0 <= bias < self.n_tensors:
             raise ValueError("the plan has no such tensor")
-        _check(lib().caramel_weight_gradient(
+        _check(packed().caramel_weight_gradient(
             self._h, weight, NO_TENSOR if bias is None else bias, features, per(C.c_void_p, checkpoint, "checkpoint"),
             per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype,
             self._outputs(weight, features) if dy_pitch is None else dy_pitch, int(accumulate), ws, ws_bytes, stream))
@@ -378,7 +396,7 @@ class Plan:
                       dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
         """dtype None: the plan's; pitch None: rows without gaps."""
         per, opt = self._per_worker, self._optional
-        _check(lib().caramel_residual_norm(
+        _check(packed().caramel_residual_norm(
             self._h, per(C.c_void_p, gain, "gain"), width, eps, per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, x, "x"),
             opt(residual, "residual"), self.cfg.dtype if dtype is None else dtype, width if pitch is None else pitch,
             opt(sum, "sum"), per(C.c_void_p, y, "y"), per(C.c_void_p, rstd, "rstd"), opt(checkpoint, "checkpoint"), stream))
@@ -386,8 +404,8 @@ class Plan:
     def residual_norm_workspace(self, gain_tensor: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that residual_norm_gradient needs for these sizes."""
         n = C.c_uint64()
-        _check(lib().caramel_residual_norm_workspace(self._h, gain_tensor, self._per_worker(C.c_uint64, tokens, "tokens"),
-                                                     C.byref(n)))
+        _check(packed().caramel_residual_norm_workspace(self._h, gain_tensor, self._per_worker(C.c_uint64, tokens, "tokens"),
+                                                        C.byref(n)))
         return n.value
 
     def residual_norm_gradient(self, gain_tensor: int, gain: Sequence[int], tokens: Sequence[int], x: Sequence[int],
@@ -396,7 +414,7 @@ class Plan:
                                accumulate: bool = False, stream: int = 0) -> None:
         """dtype None: the plan's; pitch None: rows without gaps."""
         per = self._per_worker
-        _check(lib().caramel_residual_norm_gradient(
+        _check(packed().caramel_residual_norm_gradient(
             self._h, gain_tensor, per(C.c_void_p, gain, "gain"), per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, x, "x"),
             per(C.c_void_p, rstd, "rstd"), per(C.c_void_p, dy, "dy"), self._optional(dsum, "dsum"),
             self.cfg.dtype if dtype is None else dtype, self._outputs(gain_tensor, 1) if pitch is None else pitch,
@@ -405,7 +423,7 @@ class Plan:
     def recurrence_workspace(self, channels: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that recurrence and recurrence_gradient need for these sizes (may be 0)."""
         n = C.c_uint64()
-        _check(lib().caramel_recurrence_workspace(self._h, channels, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        _check(packed().caramel_recurrence_workspace(self._h, channels, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
         return n.value
 
     def recurrence(self, channels: int, tokens: Sequence[int], sequences: Sequence[int], starts: Sequence[int],
@@ -415,7 +433,7 @@ class Plan:
                    stream: int = 0) -> None:
         """dtype None: the plan's; pitches None: rows without gaps."""
         per, opt = self._per_worker, self._optional
-        _check(lib().caramel_recurrence(
+        _check(packed().caramel_recurrence(
             self._h, channels, per(C.c_uint64, tokens, "tokens"), per(C.c_uint64, sequences, "sequences"),
             per(C.c_void_p, starts, "starts"), id_bytes, per(C.c_void_p, gate, "gate"), per(C.c_void_p, input, "input"),
             self.cfg.dtype if dtype is None else dtype, channels if pitch is None else pitch, opt(before, "before"),
@@ -430,7 +448,7 @@ class Plan:
                             pitch: Optional[int] = None, states_pitch: Optional[int] = None, stream: int = 0) -> None:
         """dtype None: the plan's; pitches None: rows without gaps."""
         per, opt = self._per_worker, self._optional
-        _check(lib().caramel_recurrence_gradient(
+        _check(packed().caramel_recurrence_gradient(
             self._h, channels, per(C.c_uint64, tokens, "tokens"), per(C.c_uint64, sequences, "sequences"),
             per(C.c_void_p, starts, "starts"), id_bytes, per(C.c_void_p, gate, "gate"), per(C.c_void_p, input, "input"),
             self.cfg.dtype if dtype is None else dtype, channels if pitch is None else pitch, opt(before, "before"),
@@ -441,7 +459,7 @@ class Plan:
     def distillation_workspace(self, vocab: int, top: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that distillation needs for these sizes (may be 0)."""
         n = C.c_uint64()
-        _check(lib().caramel_distillation_workspace(self._h, vocab, top, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        _check(packed().caramel_distillation_workspace(self._h, vocab, top, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
         return n.value
 
     def distillation(self, vocab: int, tokens: Sequence[int], logits: Sequence[int], teacher_ids: Sequence[int],
@@ -453,7 +471,7 @@ class Plan:
         """dlogits None: the loss alone; dtype None: the plan's; teacher_dtype None: dtype; pitches None: rows without gaps."""
         per, opt = self._per_worker, self._optional
         dtype = self.cfg.dtype if dtype is None else dtype
-        _check(lib().caramel_distillation(
+        _check(packed().caramel_distillation(
             self._h, vocab, per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, logits, "logits"), dtype,
             vocab if pitch is None else pitch, per(C.c_void_p, teacher_ids, "teacher_ids"), opt(labels, "labels"), id_bytes,
             per(C.c_void_p, teacher_logits, "teacher_logits"), dtype if teacher_dtype is None else teacher_dtype, top, temperature,

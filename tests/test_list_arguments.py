@@ -52,3 +52,22 @@ def test_addresses_of_other_kinds(plan):
     refused(cm.binding.EINVAL, plan.residual_norm, **{**NORM, "tokens": [-1, 3]})
     with pytest.raises(ValueError):
         plan.residual_norm(**{**NORM, "x": [A]})
+
+
+LAYER_CALLS = [name for name in cm.binding.EXPORTS
+               if any(word in name for word in ("embedding", "checkpoint", "weight_gradient", "residual_norm", "recurrence", "distillation"))]
+
+
+@pytest.mark.parametrize("name", LAYER_CALLS)
+def test_arrays_of_another_type_are_refused(name):
+    """By the functions of the library as it is loaded: a list of 32-bit counts would be read past its end."""
+    call = getattr(cm.lib(), name)
+    numbers, pointers = C.POINTER(C.c_uint64), C.POINTER(C.c_void_p)
+    fit = {numbers: (C.c_uint64 * 2)(), pointers: (C.c_void_p * 2)(), C.c_void_p: None, C.c_float: 1.0, C.c_uint64: 1, C.c_uint32: 1, C.c_int: 1}
+    lists = [i for i, kind in enumerate(call.argtypes) if kind in (numbers, pointers)]
+    assert lists
+    for i in lists:
+        other = (C.c_void_p * 2)() if call.argtypes[i] == numbers else (C.c_uint64 * 2)()
+        for wrong in ((C.c_uint32 * 2)(), (C.c_float * 2)(), other, bytes(16), A):
+            with pytest.raises(C.ArgumentError):
+                call(*[wrong if k == i else fit[kind] for k, kind in enumerate(call.argtypes)])
