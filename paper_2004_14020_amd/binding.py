@@ -311,16 +311,26 @@ class Plan:
         return host.value, dev.value
 
     # -- filling the gradient tensors: one device address and one token count per worker
-    def _per_worker(self, kind, values, name):
-        if len(values) != self._world:
-            raise ValueError(f"{name} must have one entry per worker")
+    # (bytes are made in a fraction of the time of making an array; what does not pack, None among it, goes into one, or is refused there)
+    def _addresses(self, values, name):
         try:
-            # (a tensor of one element packs too, as what it holds, which is no address)
-            if kind is C.c_uint64 or countOf(map(type, values), int) == self._world or all(isinstance(v, Integral) for v in values):
-                return self._pack(*values)                    # a fraction of the time of making an array
+            # (a tensor of one element would pack too, as what it holds, which is no address)
+            if countOf(map(type, values), int) == self._world or all(isinstance(v, Integral) for v in values):
+                return self._pack(*values)
         except struct.error:
             pass
-        return (kind * self._world)(*values)                  # None among them, or nothing that is an address
+        return self._array(C.c_void_p, values, name)
+
+    def _counts(self, values, name):
+        try:
+            return self._pack(*values)
+        except struct.error:
+            return self._array(C.c_uint64, values, name)
+
+    def _array(self, kind, values, name):
+        if len(values) != self._world:
+            raise ValueError(f"{name} must have one entry per worker")
+        return (kind * self._world)(*values)
 
     def _outputs(self, weight: int, features: int) -> int:
         if not 0 <= weight < self.n_tensors or features < 1:
@@ -330,15 +340,15 @@ class Plan:
     def embedding_lookup(self, table: Sequence[int], vocab: int, width: int, ids: Sequence[int], tokens: Sequence[int],
                          out: Sequence[int], scale: float = 1.0, id_bytes: int = 8, out_pitch: Optional[int] = None,
                          stream: int = 0) -> None:
-        per = self._per_worker
+        at, count = self._addresses, self._counts
         _check(packed().caramel_embedding_lookup(
-            self._h, per(C.c_void_p, table, "table"), vocab, width, scale, per(C.c_void_p, ids, "ids"), id_bytes,
-            per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, out, "out"), width if out_pitch is None else out_pitch, stream))
+            self._h, at(table, "table"), vocab, width, scale, at(ids, "ids"), id_bytes,
+            count(tokens, "tokens"), at(out, "out"), width if out_pitch is None else out_pitch, stream))
 
     def embedding_workspace(self, tensor: int, width: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that embedding_gradient needs for these sizes."""
         n = C.c_uint64()
-        _check(packed().caramel_embedding_workspace(self._h, tensor, width, self._per_worker(C.c_uint64, tokens, "tokens"),
+        _check(packed().caramel_embedding_workspace(self._h, tensor, width, self._counts(tokens, "tokens"),
                                                     C.byref(n)))
         return n.value
 
@@ -346,65 +356,65 @@ class Plan:
                            ws: int, ws_bytes: int, scale: float = 1.0, id_bytes: int = 8, dy_dtype: Optional[int] = None,
                            dy_pitch: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
         """dy_dtype None: the plan's."""
-        per = self._per_worker
+        at, count = self._addresses, self._counts
         _check(packed().caramel_embedding_gradient(
-            self._h, tensor, width, scale, per(C.c_void_p, ids, "ids"), id_bytes, per(C.c_uint64, tokens, "tokens"),
-            per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype, width if dy_pitch is None else dy_pitch,
+            self._h, tensor, width, scale, at(ids, "ids"), id_bytes, count(tokens, "tokens"),
+            at(dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype, width if dy_pitch is None else dy_pitch,
             int(accumulate), ws, ws_bytes, stream))
 
     def checkpoint_store(self, x: Sequence[int], tokens: Sequence[int], features: int, checkpoint: Sequence[int],
                          dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
-        per = self._per_worker
+        at, count = self._addresses, self._counts
         _check(packed().caramel_checkpoint_store(
-            self._h, per(C.c_uint64, tokens, "tokens"), features, per(C.c_void_p, x, "x"),
+            self._h, count(tokens, "tokens"), features, at(x, "x"),
             self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch,
-            per(C.c_void_p, checkpoint, "checkpoint"), stream))
+            at(checkpoint, "checkpoint"), stream))
 
     def checkpoint_load(self, checkpoint: Sequence[int], tokens: Sequence[int], features: int, x: Sequence[int],
                         dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
-        per = self._per_worker
+        at, count = self._addresses, self._counts
         _check(packed().caramel_checkpoint_load(
-            self._h, per(C.c_uint64, tokens, "tokens"), features, per(C.c_void_p, checkpoint, "checkpoint"),
-            per(C.c_void_p, x, "x"), self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch, stream))
+            self._h, count(tokens, "tokens"), features, at(checkpoint, "checkpoint"),
+            at(x, "x"), self.cfg.dtype if dtype is None else dtype, features if pitch is None else pitch, stream))
 
     def weight_gradient_workspace(self, weight: int, features: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that weight_gradient needs for these sizes (may be 0)."""
         n = C.c_uint64()
         _check(packed().caramel_weight_gradient_workspace(self._h, weight, features,
-                                                          self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+                                                          self._counts(tokens, "tokens"), C.byref(n)))
         return n.value
 
     def weight_gradient(self, weight: int, bias: Optional[int], checkpoint: Sequence[int], tokens: Sequence[int],
                         features: int, dy: Sequence[int], ws: Optional[int], ws_bytes: int, dy_dtype: Optional[int] = None,
                         dy_pitch: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
         """bias None: no bias gradient; dy_dtype None: the plan's; dy_pitch None: rows without gaps."""
-        per = self._per_worker
+        at, count = self._addresses, self._counts
         if bias is not None and not 0 <= bias < self.n_tensors:
             raise ValueError("the plan has no such tensor")
         _check(packed().caramel_weight_gradient(
-            self._h, weight, NO_TENSOR if bias is None else bias, features, per(C.c_void_p, checkpoint, "checkpoint"),
-            per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype,
+            self._h, weight, NO_TENSOR if bias is None else bias, features, at(checkpoint, "checkpoint"),
+            count(tokens, "tokens"), at(dy, "dy"), self.cfg.dtype if dy_dtype is None else dy_dtype,
             self._outputs(weight, features) if dy_pitch is None else dy_pitch, int(accumulate), ws, ws_bytes, stream))
 
     # -- a training step around them
     def _optional(self, values, name):
-        return None if values is None else self._per_worker(C.c_void_p, values, name)
+        return None if values is None else self._addresses(values, name)
 
     def residual_norm(self, gain: Sequence[int], width: int, tokens: Sequence[int], x: Sequence[int], y: Sequence[int],
                       rstd: Sequence[int], eps: float = 1e-5, residual: Optional[Sequence[int]] = None,
                       sum: Optional[Sequence[int]] = None, checkpoint: Optional[Sequence[int]] = None,
                       dtype: Optional[int] = None, pitch: Optional[int] = None, stream: int = 0) -> None:
         """dtype None: the plan's; pitch None: rows without gaps."""
-        per, opt = self._per_worker, self._optional
+        at, count, opt = self._addresses, self._counts, self._optional
         _check(packed().caramel_residual_norm(
-            self._h, per(C.c_void_p, gain, "gain"), width, eps, per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, x, "x"),
+            self._h, at(gain, "gain"), width, eps, count(tokens, "tokens"), at(x, "x"),
             opt(residual, "residual"), self.cfg.dtype if dtype is None else dtype, width if pitch is None else pitch,
-            opt(sum, "sum"), per(C.c_void_p, y, "y"), per(C.c_void_p, rstd, "rstd"), opt(checkpoint, "checkpoint"), stream))
+            opt(sum, "sum"), at(y, "y"), at(rstd, "rstd"), opt(checkpoint, "checkpoint"), stream))
 
     def residual_norm_workspace(self, gain_tensor: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that residual_norm_gradient needs for these sizes."""
         n = C.c_uint64()
-        _check(packed().caramel_residual_norm_workspace(self._h, gain_tensor, self._per_worker(C.c_uint64, tokens, "tokens"),
+        _check(packed().caramel_residual_norm_workspace(self._h, gain_tensor, self._counts(tokens, "tokens"),
                                                         C.byref(n)))
         return n.value
 
@@ -413,17 +423,17 @@ class Plan:
                                dsum: Optional[Sequence[int]] = None, dtype: Optional[int] = None, pitch: Optional[int] = None,
                                accumulate: bool = False, stream: int = 0) -> None:
         """dtype None: the plan's; pitch None: rows without gaps."""
-        per = self._per_worker
+        at, count = self._addresses, self._counts
         _check(packed().caramel_residual_norm_gradient(
-            self._h, gain_tensor, per(C.c_void_p, gain, "gain"), per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, x, "x"),
-            per(C.c_void_p, rstd, "rstd"), per(C.c_void_p, dy, "dy"), self._optional(dsum, "dsum"),
+            self._h, gain_tensor, at(gain, "gain"), count(tokens, "tokens"), at(x, "x"),
+            at(rstd, "rstd"), at(dy, "dy"), self._optional(dsum, "dsum"),
             self.cfg.dtype if dtype is None else dtype, self._outputs(gain_tensor, 1) if pitch is None else pitch,
-            per(C.c_void_p, dx, "dx"), int(accumulate), ws, ws_bytes, stream))
+            at(dx, "dx"), int(accumulate), ws, ws_bytes, stream))
 
     def recurrence_workspace(self, channels: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that recurrence and recurrence_gradient need for these sizes (may be 0)."""
         n = C.c_uint64()
-        _check(packed().caramel_recurrence_workspace(self._h, channels, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        _check(packed().caramel_recurrence_workspace(self._h, channels, self._counts(tokens, "tokens"), C.byref(n)))
         return n.value
 
     def recurrence(self, channels: int, tokens: Sequence[int], sequences: Sequence[int], starts: Sequence[int],
@@ -432,12 +442,12 @@ class Plan:
                    dtype: Optional[int] = None, pitch: Optional[int] = None, states_pitch: Optional[int] = None,
                    stream: int = 0) -> None:
         """dtype None: the plan's; pitches None: rows without gaps."""
-        per, opt = self._per_worker, self._optional
+        at, count, opt = self._addresses, self._counts, self._optional
         _check(packed().caramel_recurrence(
-            self._h, channels, per(C.c_uint64, tokens, "tokens"), per(C.c_uint64, sequences, "sequences"),
-            per(C.c_void_p, starts, "starts"), id_bytes, per(C.c_void_p, gate, "gate"), per(C.c_void_p, input, "input"),
+            self._h, channels, count(tokens, "tokens"), count(sequences, "sequences"),
+            at(starts, "starts"), id_bytes, at(gate, "gate"), at(input, "input"),
             self.cfg.dtype if dtype is None else dtype, channels if pitch is None else pitch, opt(before, "before"),
-            per(C.c_void_p, states, "states"), channels if states_pitch is None else states_pitch, opt(after, "after"), ws, ws_bytes,
+            at(states, "states"), channels if states_pitch is None else states_pitch, opt(after, "after"), ws, ws_bytes,
             stream))
 
     def recurrence_gradient(self, channels: int, tokens: Sequence[int], sequences: Sequence[int], starts: Sequence[int],
@@ -447,19 +457,19 @@ class Plan:
                             dbefore: Optional[Sequence[int]] = None, id_bytes: int = 8, dtype: Optional[int] = None,
                             pitch: Optional[int] = None, states_pitch: Optional[int] = None, stream: int = 0) -> None:
         """dtype None: the plan's; pitches None: rows without gaps."""
-        per, opt = self._per_worker, self._optional
+        at, count, opt = self._addresses, self._counts, self._optional
         _check(packed().caramel_recurrence_gradient(
-            self._h, channels, per(C.c_uint64, tokens, "tokens"), per(C.c_uint64, sequences, "sequences"),
-            per(C.c_void_p, starts, "starts"), id_bytes, per(C.c_void_p, gate, "gate"), per(C.c_void_p, input, "input"),
+            self._h, channels, count(tokens, "tokens"), count(sequences, "sequences"),
+            at(starts, "starts"), id_bytes, at(gate, "gate"), at(input, "input"),
             self.cfg.dtype if dtype is None else dtype, channels if pitch is None else pitch, opt(before, "before"),
-            per(C.c_void_p, states, "states"), per(C.c_void_p, dstates, "dstates"), channels if states_pitch is None else states_pitch,
-            opt(dafter, "dafter"), per(C.c_void_p, dgate, "dgate"), per(C.c_void_p, dinput, "dinput"), opt(dbefore, "dbefore"), ws,
+            at(states, "states"), at(dstates, "dstates"), channels if states_pitch is None else states_pitch,
+            opt(dafter, "dafter"), at(dgate, "dgate"), at(dinput, "dinput"), opt(dbefore, "dbefore"), ws,
             ws_bytes, stream))
 
     def distillation_workspace(self, vocab: int, top: int, tokens: Sequence[int]) -> int:
         """Bytes of workspace that distillation needs for these sizes (may be 0)."""
         n = C.c_uint64()
-        _check(packed().caramel_distillation_workspace(self._h, vocab, top, self._per_worker(C.c_uint64, tokens, "tokens"), C.byref(n)))
+        _check(packed().caramel_distillation_workspace(self._h, vocab, top, self._counts(tokens, "tokens"), C.byref(n)))
         return n.value
 
     def distillation(self, vocab: int, tokens: Sequence[int], logits: Sequence[int], teacher_ids: Sequence[int],
@@ -469,13 +479,13 @@ class Plan:
                      teacher_dtype: Optional[int] = None, pitch: Optional[int] = None, dlogits_pitch: Optional[int] = None,
                      stream: int = 0) -> None:
         """dlogits None: the loss alone; dtype None: the plan's; teacher_dtype None: dtype; pitches None: rows without gaps."""
-        per, opt = self._per_worker, self._optional
+        at, count, opt = self._addresses, self._counts, self._optional
         dtype = self.cfg.dtype if dtype is None else dtype
         _check(packed().caramel_distillation(
-            self._h, vocab, per(C.c_uint64, tokens, "tokens"), per(C.c_void_p, logits, "logits"), dtype,
-            vocab if pitch is None else pitch, per(C.c_void_p, teacher_ids, "teacher_ids"), opt(labels, "labels"), id_bytes,
-            per(C.c_void_p, teacher_logits, "teacher_logits"), dtype if teacher_dtype is None else teacher_dtype, top, temperature,
-            soft, hard, scale, per(C.c_void_p, loss, "loss"), opt(dlogits, "dlogits"),
+            self._h, vocab, count(tokens, "tokens"), at(logits, "logits"), dtype,
+            vocab if pitch is None else pitch, at(teacher_ids, "teacher_ids"), opt(labels, "labels"), id_bytes,
+            at(teacher_logits, "teacher_logits"), dtype if teacher_dtype is None else teacher_dtype, top, temperature,
+            soft, hard, scale, at(loss, "loss"), opt(dlogits, "dlogits"),
             vocab if dlogits_pitch is None else dlogits_pitch, ws, ws_bytes, stream))
 
     def profile(self, level: int) -> None:
