@@ -40,6 +40,11 @@ __device__ __forceinline__ uint64_t load_id(uint64_t at, uint64_t i, bool wide) 
 __device__ __forceinline__ uint32_t known(uint64_t id, uint32_t vocab) { return id < vocab ? uint32_t(id) : kNone; }  // negative: huge
 
 __device__ __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
+// Also far below the smallest fp32 numbers; v is 0 or less, or NaN.
+__device__ __forceinline__ double exp2_wide(float v) {
+  const float whole = rintf(fmaxf(v, -1100.0f));
+  return __builtin_amdgcn_ldexp(double(exp2(v - whole)), int(whole));
+}
 
 // The natural logarithm of a sum, whose exponent is taken apart: the rest is in [1/2, 1), and its logarithm off by less than 2^-23 (measured over
 // all of these numbers: 1.54 * 2^-24).
@@ -109,22 +114,25 @@ struct Student {
     for (int i = 0; i < kEach; ++i) {
       p[i] = 0.0f;
       if (uint32_t(i) * 64 >= a.top) continue;
-      if (has_teacher && t[i] != -__builtin_inff()) p[i] = exp2((t[i] - most) * a.warm_rate);
+      const bool asks = has_teacher && t[i] != -__builtin_inff();
+      if (asks) p[i] = exp2((t[i] - most) * a.warm_rate);
       total += p[i];
-      best = fmaxf(best, p[i] != 0.0f ? v[i] : kLowest);
+      best = fmaxf(best, asks ? v[i] : kLowest);
     }
     total = wave_sum(total);
     best = wave_max(best);
     // sums of the exponentials, and of their products with T (ln P - ln Q) but for the logarithms of sums; best is never -infinity, so a logit
-    // of -infinity makes the loss infinite, not NaN
+    // of -infinity makes the loss infinite, not NaN.  A P that fp32 has no number for still counts: next to a masked logit, the type's lowest
+    // number, 10^-38 of it is a loss of some units
     double part = 0.0, whole = 0.0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const uint32_t k = i * 64 + lane;
       if (uint32_t(i) * 64 >= a.top) continue;
-      if (p[i] != 0.0f) {
-        part += double(p[i]) * ((double(t[i]) - double(most)) - (double(v[i]) - double(best)));
-        whole += double(p[i]);
+      if (has_teacher && t[i] != -__builtin_inff()) {
+        const double e = exp2_wide((t[i] - most) * a.warm_rate);
+        if (e != 0.0) part += e * ((double(t[i]) - double(most)) - (double(v[i]) - double(best)));
+        whole += e;
       }
       p[i] /= total;
       if (k < a.top) {

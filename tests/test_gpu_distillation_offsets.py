@@ -65,3 +65,33 @@ def test_equal_logits_as_large_as_can_be(dtype, T, vocab, n):
     want, dg, off_loss, off = formulas(z, ids, f64(t), labels, T, 1.0, 0.5, 1.0, vocab, T == 2.0)
     close(f64(loss), want, off_loss, "loss")
     close(f64(g), dg, off + (HALF_STEP[cm.BF16] * (np.abs(dg) + off) if dtype == cm.BF16 else 0), "dlogits")
+
+
+@pytest.mark.parametrize("vocab,n", [(50, 24), (9000, 24), (70000, 24), (70000, 100)])
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
+@pytest.mark.parametrize("dtype", DTYPES, ids=dtype_id)
+def test_what_the_teacher_hardly_asks_for(dtype, T, vocab, n):
+    """A P as small as the smallest fp32 numbers, and smaller, counts where the student's logit is the type's lowest number, or -infinity."""
+    rng = np.random.default_rng(vocab)
+    low = float(torch.finfo(TORCH[dtype]).min)
+    x = torch.tensor(rng.standard_normal((n, vocab)), dtype=torch.float32).to(TORCH[dtype])
+    ids = np.stack([rng.permutation(vocab)[:4] for _ in range(n)])
+    labels = ids[:, 0]
+    t = np.zeros((n, 4))
+    t[:, 1] = -1.0
+    t[:, 2] = -T * (70 + np.arange(n) % 24 * 2.0)                  # P from 10^-31 to 10^-51
+    t[:, 3] = -T * 90.0
+    t = torch.tensor(t, dtype=torch.float32)
+    rows = torch.arange(n)
+    x[rows, torch.tensor(ids[:, 2])] = low
+    nothing = np.arange(n) % 5 == 3
+    x[torch.tensor(nothing), torch.tensor(ids[nothing, 3])] = -float("inf")
+    loss, g = call(cm.Plan(1, [1]), x, torch.tensor(ids), t, torch.tensor(labels), T, 1.0, 0.5, dtype)
+    z = x.double().numpy()
+    z -= z.max(1, keepdims=True)
+    some = ~nothing
+    want, dg, off_loss, off = formulas(z[some], ids[some], f64(t)[some], labels[some], T, 1.0, 0.5, 1.0, vocab, T == 2.0)
+    assert want.max() > 1e3 and want.min() < 20
+    close(f64(loss)[some], want, off_loss, "loss")
+    close(f64(g)[some], dg, off + (HALF_STEP[cm.BF16] * (np.abs(dg) + off) if dtype == cm.BF16 else 0), "dlogits")
+    assert bool((loss[torch.tensor(nothing)] == float("inf")).all()) and bool(g.isfinite().all())
