@@ -435,6 +435,7 @@ int caramel_recurrence_gradient(caramel_plan* plan, uint64_t channels, const uin
  *   teacher_logits   [tokens][top] values of teacher_dtype; an entry of -infinity has P = 0, as if it were not there
  *   labels           [tokens], as teacher_ids; one outside the vocabulary is none.  Not read if hard is 0, and may be NULL then
  *   loss             fp32 [tokens]; not scaled
+ * The loss does not hang on a number that all logits of a token have in common, and every P above 10^-300 counts in it.
  * A term with weight 0 is left out.  A token whose teacher has no entry has no first term, one without a label no second; a token with neither
  * has a loss of 0 and a gradient of zeros, whatever its logits.  Where P or q ask for a logit of -infinity the loss is infinite;
  * logits of which one is NaN or +infinity, or all are -infinity, give NaN.

@@ -17,7 +17,7 @@
 // is cut into parts: one launch leaves every part's largest logit and sums, and the next one joins them.
 //
 // Bound by memory and by how much of a workgroup's reading, computing and writing lies beside another's: 8 workers x 512 rows x 30522 bf16
-// logits, T = 2 with labels, 105 us, 4.8 TB/s (a copy of 1 GiB: 6.08); the vector units issue in 52 % of that time.
+// logits, T = 2 with labels, 106 us, 4.7 TB/s (a copy of 1 GiB: 6.08); the vector units issue in 52 % of that time.
 #include <algorithm>
 
 #include "layers.hpp"

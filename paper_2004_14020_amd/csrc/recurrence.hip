@@ -592,8 +592,8 @@ __global__ void __launch_bounds__(64 * kStepWaves) k_steps(RecurrenceArgs r) {
   walk.put(walk.kEnd, s, state);
 }
 
-// Workgroups of a launch that parts are made for: two to a compute unit, which is what their registers leave room for, so that all of
-// them run at once.
+// Workgroups of a launch that parts are made for: two to a compute unit, which is what the registers of the gradient (81 and 108) leave room for, so
+// that all of them run at once.  The forward walk (60 and 73) has room for three, and was measured with two.
 constexpr uint32_t kWalkGroups = 512;
 constexpr uint32_t kShortest = 2 * kTile;  // tokens of a part, at least
 
